@@ -503,6 +503,195 @@ int cascade_tier_reclaim_chain(const cascade_tier_chain_t *chain, void *index,
                                int32_t index_capacity, void *workspace, size_t workspace_bytes,
                                int32_t *status_dev, void *stream);
 
+/* The 8-bit KV cache inside the pool (Section 5 serves with FP8 KV): the new
+   tokens' keys and values are written by cascade_kv_append and read by
+   cascade_attention.  A chunk (one layer's K or V of one block) holds, for
+   kv_heads heads of head_dim and block_tokens tokens:
+     - kv_heads * block_tokens * head_dim bytes of E4M3 codes (OCP FP8: 4
+       exponent and 3 mantissa bits, largest 448), heads one behind the other,
+       each head as sub-blocks of 16 tokens in token order;
+     - then kv_heads float32 scales, each a power of two: a code stands for
+       code * scale;
+     - zero padding to a multiple of 16 bytes
+   (cascade_kv_chunk_bytes).  The scales lie in the chunk, so cascade_pack,
+   cascade_unpack and the host tier move a block whole.  Codes of a sub-block
+   (16 tokens t, head_dim dims d) lie as the matrix instructions take them:
+     K  ((d / 64) * 16 + t) * 64 + d % 64
+     V  (((d / 64) * 4 + t / 4) * 16 + d % 16) * 16 + (d % 64) / 16 * 4 + t % 4
+   A power of two makes a code's value exact in bfloat16 and lets a block's
+   scale grow by exact steps.  The pool's chunk_bytes is at least
+   cascade_kv_chunk_bytes(format).  Places past a request's last token may
+   hold anything, NaN codes included; codes before it must be finite, as
+   cascade_kv_append leaves them. */
+typedef struct {
+  int32_t block_tokens; /* 16, 32, 64 or 128 */
+  int32_t kv_heads;     /* 1 .. 256 */
+  int32_t head_dim;     /* 64, 128 or 256 */
+} cascade_kv_format_t;
+/* 0 for a format outside the domain. */
+size_t cascade_kv_chunk_bytes(const cascade_kv_format_t *format);
+
+#define CASCADE_BF16 0
+#define CASCADE_F16 1
+
+/* A ragged batch: request i's new tokens are the rows token_offsets[i] ..
+   token_offsets[i+1] of the row arrays, and kv_len[i] counts its cached
+   tokens, the new ones included: new token j of its c sits at cache index
+   kv_len[i] - c + j.  Its blocks are the first ceil(kv_len[i]/block_tokens)
+   entries of its row of the block table, which may be longer. */
+typedef struct {
+  int32_t n;                    /* requests, 0 .. 2048 */
+  int32_t n_tokens;             /* rows of the row arrays (>= token_offsets[n]) */
+  int32_t max_new;              /* most new tokens of one request */
+  int32_t n_entries;            /* entries of table->slots */
+  const int32_t *token_offsets; /* [n + 1], ascending from >= 0 */
+  const int32_t *kv_len;        /* [n], 0 .. 2^30 */
+} cascade_kv_batch_t;
+
+/* 16-bit rows: element d of head h of token t at
+   data[t * token_stride + h * head_stride + d] (strides in elements).  data
+   is 16-byte aligned, the strides are multiples of 8 and not negative. */
+typedef struct {
+  void *data;
+  int64_t token_stride, head_stride;
+} cascade_rows_t;
+
+/* Rotary positions of the first rotary_dim dims of a head: pair j of token
+   position p turns by the angle 2 pi p freq[j] / 2^64 (whole turns drop out
+   of the integer product, so the angle is exact at any position) and is
+   multiplied by `scale`.  Pair j is dims (j, j + rotary_dim/2), or (2j, 2j+1)
+   with `interleaved`.  rotary_dim is a multiple of 16 up to head_dim, or 0
+   for none. */
+typedef struct {
+  int32_t rotary_dim, interleaved;
+  const uint64_t *freq; /* device [rotary_dim / 2], turns per position in 2^-64 */
+  float scale;
+} cascade_rope_t;
+
+/* Frequency tables for cascade_rope_t, on the host: theta_j = base^(-2j/R)
+   radians per position, then for a context stretched `factor` (>= 1) times
+   over original_len positions
+     PLAIN   theta_j
+     LINEAR  theta_j / factor
+     BASE    theta_j with base * factor^(R/(R-2)) (R > 2)
+     BANDS   by wavelengths L_j = 2 pi / theta_j: theta_j / factor for those over
+             original_len/low, theta_j for those under original_len/high,
+             between them (1-s) theta_j/factor + s theta_j with
+             s = (original_len/L_j - low) / (high - low)
+     RAMP    by pair numbers j(b) = R ln(original_len/(2 pi b)) / (2 ln base):
+             (1-s) theta_j/factor + s theta_j, where s falls from 1 at
+             max(floor(j(high)), 0) to 0 at min(ceil(j(low)), R-1); the rotation is scaled by
+             0.1 ln(factor) + 1.
+   Writes freq[R/2] and *scale (1 except for RAMP).  CASCADE_EINVAL for NULL
+   pointers, rotary_dim not a multiple of 16 in 16 .. 256, base <= 1, factor < 1, and for BANDS and RAMP
+   original_len < 1 or not 0 < low < high. */
+#define CASCADE_ROPE_PLAIN 0
+#define CASCADE_ROPE_LINEAR 1
+#define CASCADE_ROPE_BASE 2
+#define CASCADE_ROPE_BANDS 3
+#define CASCADE_ROPE_RAMP 4
+typedef struct {
+  int32_t kind, rotary_dim;
+  double base, factor, original_len, low, high;
+} cascade_rope_spec_t;
+int cascade_rope_frequencies(const cascade_rope_spec_t *spec, uint64_t *freq, float *scale);
+
+/* Writes a batch's new keys and values into layer `layer` of the pool, in
+   one launch.  q and k get the rotary positions of positions[t] (device
+   int32[n_tokens], >= 0; a request that lost blocks to cascade_kv_evict
+   keeps counting its own); the turned queries go to q_out (which may be q),
+   in their type.  A block's scale per head becomes the smallest power of two
+   (at least 2^-100) that keeps its new elements within 448 scales, or the
+   scale of its older tokens where that is larger; where it grows, the older
+   codes are divided by the growth, and every element is rounded once, to nearest
+   even, from 32 bits.  q and q_out may both be NULL (no queries), rope NULL
+   (no rotation; positions may be NULL then).
+   A pool slot may be written for one request only: blocks that requests
+   share hold no new tokens.  Requests outside the domain above, slots
+   outside [0, num_slots) and negative positions set *status_dev =
+   CASCADE_EINVAL and are not written; a NaN or infinite key or value sets it too and
+   is stored as 0 (status_dev may be NULL).  Returns CASCADE_EINVAL for NULL
+   pointers, formats, sizes, strides or alignments outside the domain, CASCADE_EHIP on a
+   failed launch. */
+int cascade_kv_append(const cascade_kv_pool_t *pool, int32_t layer,
+                      const cascade_kv_format_t *format, const cascade_kv_batch_t *batch,
+                      const cascade_block_table_t *table, int32_t dtype, int32_t q_heads,
+                      const cascade_rows_t *q, const cascade_rows_t *q_out,
+                      const cascade_rows_t *k, const cascade_rows_t *v,
+                      const cascade_rope_t *rope, const int32_t *positions,
+                      int32_t *status_dev, void *stream);
+
+/* Attention of a batch's new tokens over layer `layer` of the pool:
+     out = sum_j softmax_j(s_j) v_j,  s_j = cap(scale * q . k_j)
+   over the cached tokens up to and including the token itself (cache indices
+   0 .. kv_len - c + j of new token j); query head h reads KV head
+   h / (q_heads / kv_heads).  cap(x) = softcap * tanh(x / softcap), or x when
+   softcap is 0.  A token that sees nothing gets zeros and lse -infinity.
+   Decodes, drafts of several tokens and prefill chunks may share a batch.
+   Products of 16-bit operands are summed in 32 bits, as are the softmax
+   sums; the weights are rounded to the rows' type for the second product.
+     lse           optional device float[n_tokens * q_heads]: the natural log
+                   of each row's sum of exp(s_j)
+     block_weight  optional device float[n_entries], parallel to table->slots:
+                   the softmax weights that the last
+                   min(weight_window, c) tokens of a request give to a
+                   block's tokens, summed over tokens and query heads, are
+                   added (weight_window in 1 .. 64 then, else 0)
+   workspace: device memory of cascade_attention_workspace_bytes(...) bytes,
+   256-byte aligned, of any content; it grows with the batch's n_entries and
+   n_tokens only where block_weight is given, and one made for the largest
+   batch serves all.  Results do not depend on its content or on timing.
+   A request outside the domain, or whose row names a slot outside
+   [0, num_slots), sets *status_dev = CASCADE_EINVAL (status_dev may be NULL).
+   Returns CASCADE_EINVAL for NULL pointers or arguments outside the domain, CASCADE_ENOSPC when
+   workspace_bytes is too small, CASCADE_EHIP on a failed launch. */
+typedef struct {
+  int32_t dtype, q_heads; /* CASCADE_BF16 or _F16; a multiple of kv_heads, at
+                             most 128 per KV head */
+  float scale, softcap;   /* finite; softcap >= 0 */
+  cascade_rows_t q, out;
+  float *lse;
+  float *block_weight;
+  int32_t weight_window;
+} cascade_attention_t;
+size_t cascade_attention_workspace_bytes(const cascade_kv_format_t *format,
+                                         const cascade_kv_batch_t *batch, int32_t q_heads,
+                                         int32_t weight_window);
+int cascade_attention(const cascade_kv_pool_t *pool, int32_t layer,
+                      const cascade_kv_format_t *format, const cascade_kv_batch_t *batch,
+                      const cascade_block_table_t *table, const cascade_attention_t *args,
+                      void *workspace, size_t workspace_bytes, int32_t *status_dev,
+                      void *stream);
+
+/* Drops blocks from inside requests under HBM pressure: of request i's
+   b = ceil(kv_len[i]/block_tokens) blocks, the first `sink` and the last
+   `recent` (>= 1: the block being filled stays) are kept, and of the others the
+   max(0, b - keep_blocks[i]) with the least block_weight go, all of them if
+   they are fewer (equal weights: the lower index first; NaN counts as the
+   largest).  The remaining table is written tightly, in order: row_offsets_out[n + 1],
+   slots_out and weight_out (n_entries each), kv_len_out[n] (block_tokens
+   less per dropped block); the dropped slots are listed in freed (capacity n_entries) by
+   request and index, *n_freed of them, for the pool's free list.  The outputs must
+   not overlap the inputs.  Entries past the totals are left as they are.  To
+   cascade_step such a request has as many prompt tokens as it has cached.
+   A bad request (kv_len, keep_blocks or row outside the domain) sets
+   *status_dev = CASCADE_EINVAL, a total over n_entries CASCADE_ENOSPC (status_dev may be
+   NULL).  Returns CASCADE_EINVAL for NULL pointers or sizes outside the
+   domain, CASCADE_EHIP on a failed launch. */
+typedef struct {
+  int32_t n, n_entries;        /* 0 .. 2048; entries of table->slots */
+  int32_t block_tokens;        /* >= 1 */
+  int32_t sink, recent;        /* >= 0; >= 1 */
+  const int32_t *kv_len;       /* [n] */
+  const int32_t *keep_blocks;  /* [n], >= 0 */
+  const float *block_weight;   /* [n_entries] */
+  int32_t *kv_len_out, *row_offsets_out, *slots_out;
+  float *weight_out;
+  int32_t *freed, *n_freed;
+} cascade_evict_t;
+int cascade_kv_evict(const cascade_block_table_t *table, const cascade_evict_t *args,
+                     int32_t *status_dev, void *stream);
+
 /* Short English text for a return code or status value. */
 const char *cascade_strerror(int code);
 

@@ -28,8 +28,12 @@ EXPORTED = ["cascade_step_workspace_bytes", "cascade_step", "cascade_step_noallo
             "cascade_prefix_index_insert", "cascade_prefix_probe", "cascade_restore_from_host",
             "cascade_spill_to_host", "cascade_reclaim_workspace_bytes", "cascade_tier_reclaim",
             "cascade_tier_chain_workspace_bytes", "cascade_tier_reclaim_chain",
+            "cascade_kv_chunk_bytes", "cascade_rope_frequencies", "cascade_kv_append",
+            "cascade_attention_workspace_bytes", "cascade_attention", "cascade_kv_evict",
             "cascade_strerror"]
 INDEX_SLOT_BYTES = 16
+BF16, F16 = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BANDS, ROPE_RAMP = 0, 1, 2, 3, 4
 
 
 class TierTable(C.Structure):
@@ -100,6 +104,45 @@ class KvPool(C.Structure):
     _fields_ = [("base", C.c_void_p), ("num_layers", C.c_int32), ("num_slots", C.c_int32),
                 ("chunk_bytes", C.c_int64), ("layer_stride", C.c_int64),
                 ("kv_stride", C.c_int64), ("slot_stride", C.c_int64)]
+
+
+class KvFormat(C.Structure):
+    _fields_ = [("block_tokens", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class KvBatch(C.Structure):
+    _fields_ = [("n", C.c_int32), ("n_tokens", C.c_int32), ("max_new", C.c_int32),
+                ("n_entries", C.c_int32), ("token_offsets", C.c_void_p), ("kv_len", C.c_void_p)]
+
+
+class Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class Rope(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("freq", C.c_void_p),
+                ("scale", C.c_float)]
+
+
+class RopeSpec(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("rotary_dim", C.c_int32), ("base", C.c_double),
+                ("factor", C.c_double), ("original_len", C.c_double), ("low", C.c_double),
+                ("high", C.c_double)]
+
+
+class Attention(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("q_heads", C.c_int32), ("scale", C.c_float),
+                ("softcap", C.c_float), ("q", Rows), ("out", Rows), ("lse", C.c_void_p),
+                ("block_weight", C.c_void_p), ("weight_window", C.c_int32)]
+
+
+class Evict(C.Structure):
+    _fields_ = [("n", C.c_int32), ("n_entries", C.c_int32), ("block_tokens", C.c_int32),
+                ("sink", C.c_int32), ("recent", C.c_int32), ("kv_len", C.c_void_p),
+                ("keep_blocks", C.c_void_p), ("block_weight", C.c_void_p),
+                ("kv_len_out", C.c_void_p), ("row_offsets_out", C.c_void_p),
+                ("slots_out", C.c_void_p), ("weight_out", C.c_void_p), ("freed", C.c_void_p),
+                ("n_freed", C.c_void_p)]
 
 
 _lib = None
@@ -301,6 +344,78 @@ def cascade_tier_reclaim_chain(chain: TierChain, index: int, index_capacity: int
     return int(load().cascade_tier_reclaim_chain(C.byref(chain), v(index), index_capacity,
                                                  v(workspace), workspace_bytes, v(status_dev),
                                                  v(stream)))
+
+
+_kv_lib = None
+
+
+def _kv() -> C.CDLL:
+    """The library with the prototypes of the 8-bit KV cache's calls."""
+    global _kv_lib
+    L = load()
+    if _kv_lib is not L:
+        P, v, i32 = C.POINTER, C.c_void_p, C.c_int32
+        L.cascade_kv_chunk_bytes.restype = C.c_size_t
+        L.cascade_kv_chunk_bytes.argtypes = [P(KvFormat)]
+        L.cascade_rope_frequencies.restype = C.c_int
+        L.cascade_rope_frequencies.argtypes = [P(RopeSpec), v, P(C.c_float)]
+        L.cascade_kv_append.restype = C.c_int
+        L.cascade_kv_append.argtypes = [P(KvPool), i32, P(KvFormat), P(KvBatch), P(BlockTable),
+                                        i32, i32, P(Rows), P(Rows), P(Rows), P(Rows), P(Rope), v,
+                                        v, v]
+        L.cascade_attention_workspace_bytes.restype = C.c_size_t
+        L.cascade_attention_workspace_bytes.argtypes = [P(KvFormat), P(KvBatch), i32, i32]
+        L.cascade_attention.restype = C.c_int
+        L.cascade_attention.argtypes = [P(KvPool), i32, P(KvFormat), P(KvBatch), P(BlockTable),
+                                        P(Attention), v, C.c_size_t, v, v]
+        L.cascade_kv_evict.restype = C.c_int
+        L.cascade_kv_evict.argtypes = [P(BlockTable), P(Evict), v, v]
+        _kv_lib = L
+    return L
+
+
+def _ref(s):
+    return None if s is None else C.byref(s)
+
+
+def cascade_kv_chunk_bytes(fmt: KvFormat) -> int:
+    return int(_kv().cascade_kv_chunk_bytes(C.byref(fmt)))
+
+
+def cascade_rope_frequencies(spec: RopeSpec):
+    """(return code, frequencies as uint64[rotary_dim / 2], scale)."""
+    freq = np.zeros(max(int(spec.rotary_dim) // 2, 1), np.uint64)
+    scale = C.c_float(0.0)
+    rc = int(_kv().cascade_rope_frequencies(C.byref(spec), freq.ctypes.data_as(C.c_void_p),
+                                            C.byref(scale)))
+    return rc, freq, float(scale.value)
+
+
+def cascade_kv_append(pool: KvPool, layer: int, fmt: KvFormat, batch: KvBatch, table: BlockTable,
+                      dtype: int, q_heads: int, q: Rows | None, q_out: Rows | None, k: Rows,
+                      v: Rows, rope: Rope | None, positions: int, status_dev: int,
+                      stream: int) -> int:
+    return int(_kv().cascade_kv_append(_ref(pool), layer, _ref(fmt), _ref(batch), _ref(table),
+                                       dtype, q_heads, _ref(q), _ref(q_out), _ref(k), _ref(v),
+                                       _ref(rope), positions, status_dev, stream))
+
+
+def cascade_attention_workspace_bytes(fmt: KvFormat, batch: KvBatch, q_heads: int,
+                                      weight_window: int) -> int:
+    return int(_kv().cascade_attention_workspace_bytes(_ref(fmt), _ref(batch), q_heads,
+                                                       weight_window))
+
+
+def cascade_attention(pool: KvPool, layer: int, fmt: KvFormat, batch: KvBatch, table: BlockTable,
+                      args: Attention, workspace: int, workspace_bytes: int, status_dev: int,
+                      stream: int) -> int:
+    return int(_kv().cascade_attention(_ref(pool), layer, _ref(fmt), _ref(batch), _ref(table),
+                                       _ref(args), workspace, workspace_bytes, status_dev,
+                                       stream))
+
+
+def cascade_kv_evict(table: BlockTable, args: Evict, status_dev: int, stream: int) -> int:
+    return int(_kv().cascade_kv_evict(_ref(table), _ref(args), status_dev, stream))
 
 
 def cascade_strerror(code: int) -> str:

@@ -363,3 +363,203 @@ class DeviceTiers:
         if self.index is not None:
             res["index"] = index_contents(self.index.cpu().numpy())
         return res
+
+
+# ------------------------------------------------------- the 8-bit KV cache
+
+def kv_chunk_bytes(kv_heads: int, head_dim: int, block_tokens: int = 16) -> int:
+    """Bytes of one block's K or V of one layer in the 8-bit cache."""
+    size = cx.cascade_kv_chunk_bytes(cx.KvFormat(block_tokens, kv_heads, head_dim))
+    if size == 0:
+        raise ValueError(f"no 8-bit cache of {kv_heads} heads of {head_dim} dims in blocks of "
+                         f"{block_tokens} tokens")
+    return size
+
+
+def _raise(rc: int) -> None:
+    if rc:
+        raise RuntimeError(cx.cascade_strerror(rc))
+
+
+def _dtype(t) -> int:
+    torch = _torch()
+    try:
+        return {torch.bfloat16: cx.BF16, torch.float16: cx.F16}[t.dtype]
+    except KeyError:
+        raise TypeError(f"rows are bfloat16 or float16, not {t.dtype}") from None
+
+
+def kv_rows(t) -> cx.Rows:
+    """A [tokens, heads, dims] tensor of 16-bit elements, dims contiguous."""
+    _dtype(t)
+    if t.dim() != 3 or t.stride(2) != 1:
+        raise ValueError("rows are [tokens, heads, dims] with the dims side by side")
+    return cx.Rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _check_array(t, dtype, size: int, name: str) -> int:
+    if t.dtype != dtype or not t.is_contiguous() or t.numel() < size:
+        raise ValueError(f"{name}: a contiguous tensor of at least {size} {dtype} is needed")
+    return t.data_ptr()
+
+
+class DeviceKvPool:
+    """A pool of the 8-bit cache over a byte tensor [layers, 2 (K, V), slots,
+    bytes]; the last dimension holds at least a chunk and may be padded."""
+
+    def __init__(self, pool, kv_heads: int, head_dim: int, block_tokens: int = 16):
+        torch = _torch()
+        size = kv_chunk_bytes(kv_heads, head_dim, block_tokens)
+        if pool.dtype != torch.uint8 or pool.dim() != 4 or pool.shape[1] != 2 or \
+                pool.shape[3] < size or pool.stride(3) != 1:
+            raise ValueError(f"a uint8 tensor [layers, 2, slots, bytes >= {size}] is needed")
+        self.pool, self.kv_heads, self.head_dim = pool, kv_heads, head_dim
+        self.block_tokens, self.chunk_bytes = block_tokens, size
+        self.c_format = cx.KvFormat(block_tokens, kv_heads, head_dim)
+        self.c_pool = cx.KvPool(pool.data_ptr(), pool.shape[0], pool.shape[2], size,
+                                pool.stride(0), pool.stride(1), pool.stride(2))
+        self.status = torch.zeros(1, dtype=torch.int32, device=pool.device)
+
+    @classmethod
+    def empty(cls, layers: int, slots: int, kv_heads: int, head_dim: int, block_tokens: int = 16,
+              device="cuda:0"):
+        """A new pool of zeros."""
+        size = kv_chunk_bytes(kv_heads, head_dim, block_tokens)
+        return cls(_torch().zeros(layers, 2, slots, size, dtype=_torch().uint8, device=device),
+                   kv_heads, head_dim, block_tokens)
+
+    def check(self) -> None:
+        """Synchronise and raise if a call found bad device data."""
+        _raise(int(self.status.item()))
+
+
+class KvBatch:
+    """A ragged batch over device tensors (int32): token_offsets[n + 1],
+    kv_len[n], and the block table's row_offsets[n + 1] and slots.  `tokens`
+    rows, at most `most_new` of one request."""
+
+    def __init__(self, token_offsets, kv_len, row_offsets, slots, tokens: int, most_new: int):
+        i32 = _torch().int32
+        n = int(kv_len.numel())
+        self.tensors = (token_offsets, kv_len, row_offsets, slots)
+        self.n, self.tokens = n, int(tokens)
+        self.c_batch = cx.KvBatch(n, tokens, most_new, slots.numel(),
+                                  _check_array(token_offsets, i32, n + 1, "token_offsets"),
+                                  _check_array(kv_len, i32, n, "kv_len"))
+        self.c_table = cx.BlockTable(_check_array(row_offsets, i32, n + 1, "row_offsets"),
+                                     _check_array(slots, i32, 0, "slots"))
+
+
+def rope_frequencies(rotary_dim: int, base: float = 10000.0, kind: int = cx.ROPE_PLAIN,
+                     factor: float = 1.0, original_len: float = 0.0, low: float = 1.0,
+                     high: float = 4.0, device="cuda:0"):
+    """(frequency tensor, scale) of rotary positions, see
+    cascade_rope_frequencies."""
+    rc, freq, scale = cx.cascade_rope_frequencies(
+        cx.RopeSpec(kind, rotary_dim, base, factor, original_len, low, high))
+    _raise(rc)
+    return to_device(freq, device), scale
+
+
+class DeviceKvAppend:
+    """cascade_kv_append with its arguments laid out: `run` writes k and v
+    [tokens, KV heads, dims] into `layer` and the turned queries into q_out.
+    freq None: no rotation; q None: no queries."""
+
+    def __init__(self, kv: DeviceKvPool, batch: KvBatch, q, k, v, q_out=None, positions=None,
+                 freq=None, interleaved: bool = False, rope_scale: float = 1.0, layer: int = 0):
+        torch = _torch()
+        for t, heads in ((k, kv.kv_heads), (v, kv.kv_heads), (q, None), (q_out, None)):
+            if t is not None and (t.shape[0] < batch.tokens or t.shape[2] != kv.head_dim or
+                                  t.dtype != k.dtype or t.shape[1] != (heads or q.shape[1])):
+                raise ValueError("rows do not fit the batch, the heads or each other")
+        self.kv, self.batch, self.layer = kv, batch, layer
+        self.tensors = (q, k, v, q_out, positions, freq)
+        self.dtype, self.q_heads = _dtype(k), 0 if q is None else q.shape[1]
+        self.c_rows = [None if t is None else kv_rows(t) for t in (q, q_out, k, v)]
+        self.c_rope, self.positions = None, None
+        if freq is not None:
+            self.c_rope = cx.Rope(2 * freq.numel(), int(interleaved),
+                                  _check_array(freq, torch.int64, 0, "freq"), rope_scale)
+            self.positions = _check_array(positions, torch.int32, batch.tokens, "positions")
+
+    def run(self, stream=None) -> None:
+        b = self.batch
+        _raise(cx.cascade_kv_append(self.kv.c_pool, self.layer, self.kv.c_format, b.c_batch,
+                                    b.c_table, self.dtype, self.q_heads, *self.c_rows,
+                                    self.c_rope, self.positions, self.kv.status.data_ptr(),
+                                    stream_handle(stream)))
+
+
+class DeviceAttention:
+    """cascade_attention with its arguments and workspace laid out: `run`
+    writes the attention of q [tokens, query heads, dims] over `layer` to out,
+    and lse [tokens, query heads] and block_weight (one per table entry, added
+    to) where they are given.  A workspace may be shared by calls that follow
+    each other on one stream."""
+
+    def __init__(self, kv: DeviceKvPool, batch: KvBatch, q, out, scale: float,
+                 softcap: float = 0.0, lse=None, block_weight=None, weight_window: int = 0,
+                 layer: int = 0, workspace=None):
+        torch = _torch()
+        if q.shape != out.shape or q.dtype != out.dtype or q.shape[0] < batch.tokens or \
+                q.shape[2] != kv.head_dim:
+            raise ValueError("q and out do not fit the batch, the pool or each other")
+        self.kv, self.batch, self.layer = kv, batch, layer
+        self.tensors = (q, out, lse, block_weight)
+        heads, f32 = q.shape[1], torch.float32
+        self.c_args = cx.Attention(
+            _dtype(q), heads, scale, softcap, kv_rows(q), kv_rows(out),
+            None if lse is None else _check_array(lse, f32, batch.tokens * heads, "lse"),
+            None if block_weight is None else
+            _check_array(block_weight, f32, batch.c_batch.n_entries, "block_weight"),
+            weight_window if block_weight is not None else 0)
+        self.ws_bytes = cx.cascade_attention_workspace_bytes(kv.c_format, batch.c_batch, heads,
+                                                             self.c_args.weight_window)
+        if self.ws_bytes == 0:
+            raise ValueError("query heads or weight_window outside the domain")
+        if workspace is None:
+            workspace = torch.empty(self.ws_bytes + 256, dtype=torch.uint8, device=q.device)
+        self.workspace = workspace
+        self.ws_ptr = (workspace.data_ptr() + 255) & ~255
+        self.ws_bytes = workspace.data_ptr() + workspace.numel() - self.ws_ptr
+
+    def run(self, stream=None) -> None:
+        b = self.batch
+        _raise(cx.cascade_attention(self.kv.c_pool, self.layer, self.kv.c_format, b.c_batch,
+                                    b.c_table, self.c_args, self.ws_ptr, self.ws_bytes,
+                                    self.kv.status.data_ptr(), stream_handle(stream)))
+
+
+class DeviceKvEvict:
+    """cascade_kv_evict with its arguments laid out: `run` writes the tight
+    table of what stays to kv_len_out, row_offsets_out, slots_out and
+    weight_out, and the dropped slots to freed, n_freed of them (`out`: these
+    six tensors, else new ones)."""
+
+    def __init__(self, block_tokens: int, kv_len, row_offsets, slots, block_weight, keep_blocks,
+                 sink: int = 0, recent: int = 1, out=None):
+        torch = _torch()
+        i32, n, entries = torch.int32, int(kv_len.numel()), int(slots.numel())
+        if out is None:
+            new = lambda k, dt=i32: torch.zeros(max(k, 1), dtype=dt, device=kv_len.device)
+            out = (new(n), new(n + 1), new(entries), new(entries, torch.float32), new(entries),
+                   new(1))
+        self.tensors = (kv_len, row_offsets, slots, block_weight, keep_blocks)
+        self.kv_len_out, self.row_offsets_out, self.slots_out = out[:3]
+        self.weight_out, self.freed, self.n_freed = out[3:]
+        p = _check_array
+        self.status = torch.zeros(1, dtype=i32, device=kv_len.device)
+        self.c_table = cx.BlockTable(p(row_offsets, i32, n + 1, "row_offsets"),
+                                     p(slots, i32, 0, "slots"))
+        self.c_args = cx.Evict(
+            n, entries, block_tokens, sink, recent, p(kv_len, i32, n, "kv_len"),
+            p(keep_blocks, i32, n, "keep_blocks"),
+            p(block_weight, torch.float32, entries, "block_weight"),
+            p(out[0], i32, n, "kv_len_out"), p(out[1], i32, n + 1, "row_offsets_out"),
+            p(out[2], i32, entries, "slots_out"), p(out[3], torch.float32, entries, "weight_out"),
+            p(out[4], i32, entries, "freed"), p(out[5], i32, 1, "n_freed"))
+
+    def run(self, stream=None) -> None:
+        _raise(cx.cascade_kv_evict(self.c_table, self.c_args, self.status.data_ptr(),
+                                   stream_handle(stream)))
