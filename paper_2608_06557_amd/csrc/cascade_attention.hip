@@ -103,8 +103,9 @@ struct Attention {
   const int32_t *row_offsets, *slots;
   Rows q, out;
   int q_heads, group;      // query heads, and those of one KV head
-  float scale;             // of q.k, in log2 units (softcap 0)
-  float cap_in, cap_out;   // softcap: exp2 argument per q.k, cap in log2 units
+  float scale;             // of q.k, or of the capped score; in log2 units, >= 0
+  float cap_in;            // softcap: exp2 argument per q.k
+  unsigned keep, flip;     // q's bits: none where the scale was 0, turned signs where it was negative
   float *lse;              // [n_tokens][q_heads] or NULL
   float *logs;             // [sub-block][window][q_heads]: log2 of a sub-block's weight, or NULL
   int window;
@@ -191,13 +192,6 @@ __device__ __forceinline__ Place uniform(const Place &p, int lane) {
 
 // ------------------------------------------------------------- one wave
 
-// 32 cached tokens of one head as they lie in the cache: two sub-blocks.
-template <int kDim>
-struct Codes {
-  u4 k[2][kDim / 64], v[2][kDim / 64];
-  float ks[2], vs[2];
-};
-
 // What a wave keeps of 16 * kTiles query rows.
 template <int kType, int kDim, int kTiles, bool kCap>
 struct Rowset {
@@ -218,9 +212,14 @@ struct Rowset {
     }
   }
 
-  template <bool kMask, bool kLogs>
-  __device__ __forceinline__ void step(const Attention &a, const Codes<kDim> &c, int key, int len,
-                                       int64_t log_row) {
+  // 32 tokens from `key` on: `codes_k(b, c)` and `codes_v(b, c)` give the
+  // lane's 16 codes of sub-block b and dims 64 c, `ks` and `vs` their scales.
+  // `masked`: some row does not see all of them, or the cache ends before.
+  // `after_k` is called once the K codes have been taken.
+  template <typename KCodes, typename VCodes, typename AfterK>
+  __device__ __forceinline__ void step(const Attention &a, KCodes codes_k, VCodes codes_v, AfterK after_k,
+                                       const float (&ks)[2], const float (&vs)[2], int key, int len,
+                                       bool masked, bool logs, int64_t log_row) {
     const int lane = lane_id(), g = lane >> 4;
     f4 s[kTiles][2];
 #pragma unroll
@@ -228,31 +227,46 @@ struct Rowset {
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) s[t][b] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int d = 0; d < kDim / 32; ++d) {
-        const u4 w = c.k[b][d >> 1];
-        const v8 k = (d & 1) ? widen8<kType>(w[2], w[3], c.ks[b], c.ks[b])
-                             : widen8<kType>(w[0], w[1], c.ks[b], c.ks[b]);
+      for (int c = 0; c < kDim / 64; ++c) {
+        const u4 w = codes_k(b, c);
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) s[t][b] = El<kType>::mfma(k, q[t][d], s[t][b]);
+        for (int h = 0; h < 2; ++h) {
+          const v8 k = widen8<kType>(w[2 * h], w[2 * h + 1], ks[b], ks[b]);
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) s[t][b] = El<kType>::mfma(k, q[t][2 * c + h], s[t][b]);
+        }
+      }
+    }
+    after_k();
+    if (kCap) {
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)  // tanh(x) = 1 - 2 / (exp(2 x) + 1)
+            s[t][b][i] = 1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[t][b][i] * a.cap_in) + 1.f);
+    }
+    unsigned mask[2] = {~0u, ~0u};
+    if (masked) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int at = key + 16 * b + 4 * g, live = len - at;
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[t][b][i] = at + i <= limit[t] ? s[t][b][i] : -__builtin_inff();
+        // tokens past the cache's end may be anything: their V codes become 0
+        mask[b] = live >= 4 ? ~0u : live <= 0 ? 0u : (1u << 8 * live) - 1;
       }
     }
     v8 p[kTiles];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      float top = kLowest;
+      float top = s[t][0][0];
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float x = s[t][b][i];
-          if (kCap)  // cap * tanh(x / cap) = cap - 2 cap / (exp(2 x / cap) + 1)
-            x = a.cap_out - 2.f * a.cap_out * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * a.cap_in) + 1.f);
-          else
-            x *= a.scale;
-          if (kMask) x = key + 16 * b + 4 * g + i <= limit[t] ? x : -__builtin_inff();
-          s[t][b][i] = x;
-          top = fmaxf(top, x);
-        }
+      for (int i = 1; i < 8; ++i) top = fmaxf(top, s[t][i >> 2][i & 3]);
+      top *= a.scale;
       if (__any(top > m[t] + kSlack)) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
@@ -265,14 +279,14 @@ struct Rowset {
       float e[8], half[2] = {0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        e[i] = __builtin_amdgcn_exp2f(s[t][i >> 2][i & 3] - m[t]);
+        e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i >> 2][i & 3], a.scale, -m[t]));
         half[i >> 2] += e[i];
       }
       sum[t] += half[0] + half[1];
       const u4 w = {narrow2<kType>(e[0], e[1]), narrow2<kType>(e[2], e[3]), narrow2<kType>(e[4], e[5]),
                     narrow2<kType>(e[6], e[7])};
       p[t] = __builtin_bit_cast(v8, w);
-      if (kLogs) {
+      if (logs) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
           float x = half[b];
@@ -283,61 +297,94 @@ struct Rowset {
         }
       }
     }
-    // tokens past the cache's end may be anything: their codes become 0
-    unsigned mask[2] = {~0u, ~0u};
-    if (kMask) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const int live = len - (key + 16 * b + 4 * g);
-        mask[b] = live >= 4 ? ~0u : live <= 0 ? 0u : (1u << 8 * live) - 1;
+    for (int c = 0; c < kDim / 64; ++c) {
+      const u4 w0 = codes_v(0, c), w1 = codes_v(1, c);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const v8 v = widen8<kType>(w0[i] & mask[0], w1[i] & mask[1], vs[0], vs[1]);
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) o[t][4 * c + i] = El<kType>::mfma(v, p[t], o[t][4 * c + i]);
       }
-    }
-#pragma unroll
-    for (int d = 0; d < kDim / 16; ++d) {
-      const unsigned lo = c.v[0][d >> 2][d & 3] & mask[0], hi = c.v[1][d >> 2][d & 3] & mask[1];
-      const v8 v = widen8<kType>(lo, hi, c.vs[0], c.vs[1]);
-#pragma unroll
-      for (int t = 0; t < kTiles; ++t) o[t][d] = El<kType>::mfma(v, p[t], o[t][d]);
     }
   }
 };
 
-// Tokens key .. key + 32 of head `head` of a request (key < len).
+// Where a request's head lies in the cache.
 template <int kDim>
-__device__ __forceinline__ void fetch(const Attention &a, int row, int len, int head, int key,
-                                      Codes<kDim> &c) {
-  const int shift = a.kv.block_shift, last = (len - 1) >> 4;
-  const int64_t scales = (int64_t)a.kv.kv_heads * kDim << shift;
-#pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    const int sub = min((key >> 4) + b, last);
-    int slot = a.slots[row + (sub >> (shift - 4))];
-    if ((unsigned)slot >= (unsigned)a.kv.num_slots) {
-      kv_report(a.status);
+struct Cache {
+  const char *base;    // the head's codes in slot 0
+  int64_t kv_stride, slot_stride, scales;  // `scales`: from the codes to the head's scale
+  const int32_t *slots;
+  int num_slots, shift, last;  // log2 of sub-blocks a block, last sub-block
+  int32_t *status;
+  __device__ __forceinline__ Cache(const Attention &a, const KvRequest &r, int head)
+      : base(a.kv.base + ((int64_t)head << a.kv.block_shift) * kDim), kv_stride(a.kv.kv_stride),
+        slot_stride(a.kv.slot_stride),
+        scales(((int64_t)(a.kv.kv_heads - head) << a.kv.block_shift) * kDim + 4 * head),
+        slots(a.slots + r.row), num_slots(a.kv.num_slots), shift(a.kv.block_shift - 4),
+        last((r.len - 1) >> 4), status(a.status) {}
+  // the slot of sub-block `sub`, or of the last one
+  __device__ __forceinline__ int slot(int sub) const { return uniform_load(slots + (min(sub, last) >> shift)); }
+  // the head's codes in a slot; a slot outside the pool is reported and read as slot 0
+  __device__ __forceinline__ const char *block(int slot) const {
+    if ((unsigned)slot >= (unsigned)num_slots) {
+      kv_report(status);
       slot = 0;
     }
-    const char *chunk = a.kv.base + slot * a.kv.slot_stride;
-    const char *at = chunk + (((int64_t)head << shift) + 16 * (sub & ((1 << (shift - 4)) - 1))) * kDim;
-    // a lane's token is lane % 16; its 16 dims of 64 are those of lane / 16
-    const u4 *k = reinterpret_cast<const u4 *>(at) + (lane_id() & 15) * 4 + (lane_id() >> 4);
-    const u4 *v = reinterpret_cast<const u4 *>(at + a.kv.kv_stride) + lane_id();
-#pragma unroll
-    for (int i = 0; i < kDim / 64; ++i) {
-      c.k[b][i] = k[64 * i];
-      c.v[b][i] = v[64 * i];
-    }
-    const float *s = reinterpret_cast<const float *>(chunk + scales) + head;
-    c.ks[b] = *s;
-    c.vs[b] = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(s) + a.kv.kv_stride);
+    return base + slot * slot_stride;
   }
-}
+  __device__ __forceinline__ const char *codes(const char *block, int sub) const {
+    return block + (min(sub, last) & ((1 << shift) - 1)) * 16 * kDim;
+  }
+  __device__ __forceinline__ float k_scale(const char *block) const {
+    return uniform_load(reinterpret_cast<const float *>(block + scales));
+  }
+  __device__ __forceinline__ float v_scale(const char *block) const {
+    return uniform_load(reinterpret_cast<const float *>(block + scales + kv_stride));
+  }
+};
+// Byte of a lane's 16 codes within 1024: of K its token is lane % 16 and its
+// dims those of lane / 16, V lies in lane order.
+__device__ __forceinline__ int k_place() { return (lane_id() & 15) * 64 + (lane_id() >> 4) * 16; }
+__device__ __forceinline__ int v_place() { return lane_id() * 16; }
+
+// 32 cached tokens of one head in registers: two sub-blocks.
+template <int kDim>
+struct Codes {
+  u4 k[2][kDim / 64], v[2][kDim / 64];
+  float ks[2], vs[2];
+  __device__ __forceinline__ void fetch_k(const Cache<kDim> &c, const int (&slot)[2], int key) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const char *block = c.block(slot[b]), *at = c.codes(block, (key >> 4) + b);
+#pragma unroll
+      for (int i = 0; i < kDim / 64; ++i) k[b][i] = *reinterpret_cast<const u4 *>(at + 1024 * i + k_place());
+      ks[b] = c.k_scale(block);
+    }
+  }
+  __device__ __forceinline__ void fetch_v(const Cache<kDim> &c, const int (&slot)[2], int key) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const char *block = c.block(slot[b]), *at = c.codes(block, (key >> 4) + b) + c.kv_stride;
+#pragma unroll
+      for (int i = 0; i < kDim / 64; ++i) v[b][i] = *reinterpret_cast<const u4 *>(at + 1024 * i + v_place());
+      vs[b] = c.v_scale(block);
+    }
+  }
+};
 
 // ------------------------------------------------------------- the kernel
 
 // kKeyWaves waves share a row tile's tokens and combine in LDS; the
 // kWaves / kKeyWaves groups of them each have rows of their own.
+constexpr int waves_per_simd(int dim, int tiles, int key_waves) {
+  if (key_waves == 1) return dim == 256 ? 1 : 2;
+  const int held = dim * tiles;  // of q, o and codes in registers
+  return held <= 64 ? 5 : tiles == 1 && held <= 128 ? 4 : held <= 128 ? 3 : held <= 256 ? 2 : 1;
+}
 template <int kType, int kDim, int kTiles, int kKeyWaves, bool kCap>
-__global__ __launch_bounds__(kBlock) void attention_kernel(Attention a) {
+__global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles, kKeyWaves)) void attention_kernel(Attention a) {
   constexpr int kRows = 16 * kTiles * (kWaves / kKeyWaves);
   constexpr int kPart = kDim < 128 ? kDim : 128;  // dims that one combination takes
   constexpr int kPitch = kPart + 4;
@@ -413,7 +460,7 @@ __global__ __launch_bounds__(kBlock) void attention_kernel(Attention a) {
   const int key_wave = wave % kKeyWaves;
   while (at.item < n) {
     const int id = __builtin_amdgcn_readfirstlane(ids[at.item]);
-    const KvRequest req = kv_request(a.batch, a.row_offsets, a.kv.block_shift, id);
+    const KvRequest req = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, id);
     const Segments seg(req, a.tile_tokens);
     const int length = (int)seg.length(at.tile);
     const bool last = end.item == at.item && end.head == at.head && end.tile == at.tile;
@@ -439,6 +486,7 @@ __global__ __launch_bounds__(kBlock) void attention_kernel(Attention a) {
       for (int d = 0; d < kDim / 32; ++d) {
         u4 x = *reinterpret_cast<const u4 *>(q + 128 * (d >> 1) + 16 * (d & 1));
         if (!valid[t]) x = u4{0, 0, 0, 0};
+        x = (x & a.keep) ^ a.flip;
         r.q[t][d] = __builtin_bit_cast(typename El<kType>::v8, x);
       }
       r.log_at[t] = nullptr;
@@ -458,31 +506,101 @@ __global__ __launch_bounds__(kBlock) void attention_kernel(Attention a) {
     const int key_end =
         row0 >= tile_rows || first_token >= req.count ? 0 : min(min(stop, req.len), shown + last_token + 1);
     const int clear_end = shown + first_token + 1;  // every row sees the tokens before it
-    auto step = [&](const Codes<kDim> &c, int key) {
-      const bool masked = key + 32 > clear_end;
-      if (logs) {
-        r.template step<true, true>(a, c, key, req.len, log_row);
-      } else if (masked) {
-        r.template step<true, false>(a, c, key, req.len, log_row);
-      } else {
-        r.template step<false, false>(a, c, key, req.len, log_row);
+    const Cache<kDim> cache(a, req, at.head);
+    if (kKeyWaves > 1) {
+      // each wave takes every kKeyWaves-th 32 tokens, straight into registers:
+      // the next K codes leave when these have been taken, V codes likewise,
+      // and the slots are known a step ahead of them
+      constexpr int kStride = 32 * kKeyWaves;
+      int key = at.key + 32 * key_wave;
+      if (key < key_end) {
+        Codes<kDim> c;
+        int slot[2];
+        auto look = [&](int key) {
+          slot[0] = cache.slot(key >> 4);
+          slot[1] = cache.slot((key >> 4) + 1);
+        };
+        look(key);
+        c.fetch_k(cache, slot, key);
+        c.fetch_v(cache, slot, key);
+        look(key + kStride);
+        while (true) {
+          const int next = key + kStride;
+          r.step(a, [&](int b, int i) { return c.k[b][i]; }, [&](int b, int i) { return c.v[b][i]; },
+                 [&] { if (next < key_end) c.fetch_k(cache, slot, next); }, c.ks, c.vs, key, req.len,
+                 key + 32 > clear_end, logs, log_row);
+          if (next >= key_end) break;
+          c.fetch_v(cache, slot, next);
+          look(next + kStride);
+          key = next;
+        }
       }
-    };
-    constexpr int kStride = 32 * kKeyWaves;
-    int key = at.key + 32 * key_wave;
-    if (key < key_end) {
-      Codes<kDim> c0, c1;
-      fetch<kDim>(a, req.row, req.len, at.head, key, c0);
-      while (true) {
-        if (key + kStride < key_end) fetch<kDim>(a, req.row, req.len, at.head, key + kStride, c1);
-        step(c0, key);
-        key += kStride;
-        if (key >= key_end) break;
-        if (key + kStride < key_end) fetch<kDim>(a, req.row, req.len, at.head, key + kStride, c0);
-        step(c1, key);
-        key += kStride;
-        if (key >= key_end) break;
+    } else {
+      // the waves share the tokens through LDS, kStage of them at a time, in
+      // operand order; the next stage's codes cross in registers meanwhile
+      constexpr int kSubs = kDim == 256 ? 2 : 4, kStage = 16 * kSubs;
+      constexpr int kSub = 16 * kDim, kPieces = kSubs * 2 * kDim / 64;  // of 1 KiB: sub-block, K or V, 64 dims
+      constexpr int kOwn = kPieces / kWaves;
+      char *stage = lds + ((12 * a.batch.n + 8 + 15) & ~15);
+      const int block_end = min(stop, min(req.len, shown + min((at.tile + 1) * a.tile_tokens, req.count)));
+      u4 own[kOwn];
+      float ks[2][kSubs], vs[2][kSubs];
+      auto fetch = [&](int key, float (&k)[kSubs], float (&v)[kSubs]) {
+        const char *block[kSubs];
+#pragma unroll
+        for (int b = 0; b < kSubs; ++b) {
+          block[b] = cache.block(cache.slot((key >> 4) + b));
+          k[b] = cache.k_scale(block[b]);
+          v[b] = cache.v_scale(block[b]);
+        }
+        // piece p of a stage: sub-block p / (2 kDim / 64), then K before V
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+          const int p = wave * kOwn + i, b = p / (2 * kDim / 64), side = p / (kDim / 64) & 1;
+          const char *from = block[0];
+#pragma unroll
+          for (int j = 1; j < kSubs; ++j) from = b == j ? block[j] : from;
+          own[i] = *reinterpret_cast<const u4 *>(cache.codes(from, (key >> 4) + b) + side * cache.kv_stride +
+                                                 p % (kDim / 64) * 1024 + (side ? v_place() : k_place()));
+        }
+      };
+      auto put = [&](int buffer) {
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i)
+          *reinterpret_cast<u4 *>(stage + buffer * kPieces * 1024 + (wave * kOwn + i) * 1024 + lane * 16) = own[i];
+      };
+      auto compute = [&](int buffer, int key, const float (&k)[kSubs], const float (&v)[kSubs]) {
+#pragma unroll
+        for (int h = 0; h < kSubs / 2; ++h) {
+          if (key + 32 * h >= key_end) break;
+          const char *from = stage + buffer * kPieces * 1024 + h * 4 * kSub + lane * 16;
+          const float k2[2] = {k[2 * h], k[2 * h + 1]}, v2[2] = {v[2 * h], v[2 * h + 1]};
+          r.step(a, [&](int b, int i) { return *reinterpret_cast<const u4 *>(from + b * 2 * kSub + i * 1024); },
+                 [&](int b, int i) { return *reinterpret_cast<const u4 *>(from + b * 2 * kSub + kSub + i * 1024); },
+                 [] {}, k2, v2, key + 32 * h, req.len, key + 32 * h + 32 > clear_end, logs, log_row);
+        }
+      };
+      int key = at.key;
+      if (key < block_end) {
+        fetch(key, ks[0], vs[0]);
+        put(0);
+        __syncthreads();
+        while (true) {
+          if (key + kStage < block_end) fetch(key + kStage, ks[1], vs[1]);
+          compute(0, key, ks[0], vs[0]);
+          key += kStage;
+          if (key >= block_end) break;
+          put(1);
+          __syncthreads();
+          if (key + kStage < block_end) fetch(key + kStage, ks[0], vs[0]);
+          compute(1, key, ks[1], vs[1]);
+          key += kStage;
+          if (key >= block_end) break;
+          put(0);
+          __syncthreads();
+        }
       }
+      __syncthreads();
     }
 
 #pragma unroll
@@ -664,7 +782,7 @@ __global__ __launch_bounds__(kBlock) void weight_kernel(Attention a, float *bloc
 constexpr int kGroups = 1024;      // workgroups of the kernel that splits tokens over waves
 constexpr int kTileGroups = 512;   // of the kernel that splits rows over waves
 constexpr int kTileRows = 128;     // its row tile
-constexpr int kMostRows = 64;      // of the former's
+constexpr int most_rows(int dim) { return dim == 256 ? 32 : 64; }  // of a request in the former
 
 struct Workspace {
   size_t splits, tile_splits, parts, tile_parts, sums, tile_sums, lse, logs, total;
@@ -682,9 +800,9 @@ Workspace layout(const cascade_kv_format_t *f, const cascade_kv_batch_t *b, int 
   };
   w.splits = take(sizeof(Split) * kGroups);
   w.tile_splits = take(sizeof(Split) * kTileGroups);
-  w.parts = take(sizeof(float) * kGroups * 2 * kMostRows * f->head_dim);
+  w.parts = take(sizeof(float) * kGroups * 2 * most_rows(f->head_dim) * f->head_dim);
   w.tile_parts = take(sizeof(float) * kTileGroups * 2 * kTileRows * f->head_dim);
-  w.sums = take(sizeof(float) * kGroups * 2 * kMostRows * 2);
+  w.sums = take(sizeof(float) * kGroups * 2 * most_rows(f->head_dim) * 2);
   w.tile_sums = take(sizeof(float) * kTileGroups * 2 * kTileRows * 2);
   w.lse = take(window ? sizeof(float) * b->n_tokens * q_heads : 0);
   w.logs = take(window ? sizeof(float) * b->n_entries * (f->block_tokens / 16) * window * q_heads : 0);
@@ -699,8 +817,9 @@ bool heads_ok(const cascade_kv_format_t *f, int q_heads) {
 template <int kType, int kDim, int kTiles, int kKeyWaves>
 void start(const Attention &a, int grid, bool cap, hipStream_t stream) {
   const size_t list = (12 * (size_t)a.batch.n + 8 + 15) & ~(size_t)15;
-  const size_t mix =
-      kKeyWaves > 1 ? sizeof(float) * kWaves * 16 * (2 + (kDim < 128 ? kDim : 128) + 4) : 0;
+  // combination of the waves, or two stages of codes
+  const size_t mix = kKeyWaves > 1 ? sizeof(float) * kWaves * 16 * (2 + (kDim < 128 ? kDim : 128) + 4)
+                                   : 2 * (kDim == 256 ? 32 : 64) * 2 * kDim;
   auto kernel = cap ? attention_kernel<kType, kDim, kTiles, kKeyWaves, true>
                     : attention_kernel<kType, kDim, kTiles, kKeyWaves, false>;
   hipLaunchKernelGGL(kernel, dim3(grid), dim3(kBlock), list + mix, stream, a);
@@ -710,9 +829,9 @@ template <int kType, int kDim>
 int run(Attention a, char *ws, const Workspace &w, bool cap, float *block_weight, hipStream_t s) {
   const int64_t most = (int64_t)a.batch.max_new * a.group;  // rows of a request and KV head
   const int64_t keys = ((int64_t)a.batch.n_entries << a.kv.block_shift) * a.kv.kv_heads;
-  // few rows: 4 waves share a tile's tokens.  More than 64: row tiles of 128,
+  // few rows: 4 waves share a tile's tokens.  More: row tiles of 128,
   // and requests of up to 32 rows beside them in the first kernel
-  const bool tiled = most > kMostRows;
+  const bool tiled = most > most_rows(kDim);
   const int small = most <= 16 ? 16 : most <= 32 || tiled ? 32 : 64;
   a.min_rows = 0;
   a.max_rows = small;
@@ -728,7 +847,7 @@ int run(Attention a, char *ws, const Workspace &w, bool cap, float *block_weight
     start<kType, kDim, 1, 4>(a, (int)grid, cap, s);
   else if (small == 32)
     start<kType, kDim, 2, 4>(a, (int)grid, cap, s);
-  else
+  else if constexpr (kDim < 256)
     start<kType, kDim, 4, 4>(a, (int)grid, cap, s);
   hipLaunchKernelGGL((join_kernel<kType, kDim>), dim3((int)grid, small / kWaves), dim3(kBlock), 0, s, a,
                      small);
@@ -800,9 +919,13 @@ extern "C" int cascade_attention(const cascade_kv_pool_t *pool, int32_t layer,
   a.q_heads = args->q_heads;
   a.group = args->q_heads / format->kv_heads;
   const bool cap = args->softcap > 0;
-  a.scale = args->scale * kLog2e;
-  a.cap_in = cap ? 2 * kLog2e * args->scale / args->softcap : 0.f;
-  a.cap_out = args->softcap * kLog2e;
+  // softmax(-s q.k) is softmax(s (-q).k): the largest score is then that of
+  // the largest product
+  const float scale = std::fabs(args->scale);
+  a.flip = args->scale < 0 ? 0x80008000u : 0u;
+  a.keep = scale > 0 ? ~0u : 0u;
+  a.scale = (cap ? args->softcap : scale > 0 ? scale : 1.f) * kLog2e;
+  a.cap_in = cap ? 2 * kLog2e * scale / args->softcap : 0.f;
   char *ws = static_cast<char *>(workspace);
   a.window = args->weight_window;
   a.lse = args->lse ? args->lse : a.window ? reinterpret_cast<float *>(ws + w.lse) : nullptr;

@@ -67,6 +67,14 @@ inline KvView kv_view(const cascade_kv_pool_t *p, int32_t layer, const cascade_k
   return v;
 }
 
+// A load from memory that no kernel of the launch writes, at an address that
+// is the same in all lanes: through the constant address space it goes to the
+// scalar unit, whatever the kernel stores elsewhere.
+template <typename T>
+__device__ __forceinline__ T uniform_load(const T *p) {
+  return *(const __attribute__((address_space(4))) T *)(p);
+}
+
 // A request of a batch, checked against the arrays it points into.
 struct KvRequest {
   int first, count;  // new tokens: rows first .. first + count
@@ -75,15 +83,17 @@ struct KvRequest {
   bool ok;
 };
 
+template <bool kUniform = false>
 __device__ __forceinline__ KvRequest kv_request(const cascade_kv_batch_t &b,
                                                 const int32_t *row_offsets, int block_shift,
                                                 int i) {
+  const auto load = [](const int32_t *p) { return kUniform ? uniform_load(p) : *p; };
   KvRequest r;
-  r.first = b.token_offsets[i];
-  const int end = b.token_offsets[i + 1];
-  r.len = b.kv_len[i];
-  r.row = row_offsets[i];
-  const int row_end = row_offsets[i + 1];
+  r.first = load(b.token_offsets + i);
+  const int end = load(b.token_offsets + i + 1);
+  r.len = load(b.kv_len + i);
+  r.row = load(row_offsets + i);
+  const int row_end = load(row_offsets + i + 1);
   r.count = (int)((unsigned)end - (unsigned)r.first);
   r.ok = r.first >= 0 && end >= r.first && end <= b.n_tokens && r.count <= b.max_new &&
          r.len >= 0 && r.len <= kMaxKvLen && r.row >= 0 && row_end >= r.row &&
