@@ -112,7 +112,8 @@ struct Attention {
   int64_t min_rows, max_rows;  // requests with min_rows < rows <= max_rows are taken
   int tile_tokens;         // tokens of one row tile
   int atomic_keys;         // segments up to this long are not cut
-  int range_keys;          // least tokens of one workgroup
+  int cut_keys;            // cuts are at multiples of this power of two, the tokens of a step
+  int range_keys;          // least tokens of one workgroup, at least two steps
   Split *splits;           // [gridDim]
   float *parts;            // [gridDim][2][rows][kDim]
   float *part_sums;        // [gridDim][2][rows][2]: m and sum
@@ -145,8 +146,7 @@ struct Place {
   int item, head, tile, key;
 };
 
-// Where the range of cost `c` begins: a segment and a token of it, a multiple
-// of 32.
+// Where the range of cost `c` begins: a segment and a token of it.
 __device__ __forceinline__ Place locate(const Attention &a, const long long *before, const int *ids,
                                         int n, long long c) {
   Place p = {n, 0, 0, 0};
@@ -171,7 +171,7 @@ __device__ __forceinline__ Place locate(const Attention &a, const long long *bef
   left -= s.start(t0);
   const long long length = s.length(t0);
   if (length > a.atomic_keys) {
-    p.key = (int)(left & ~31ll);
+    p.key = (int)left & -a.cut_keys;
   } else if (2 * left >= length) {  // not cut: the nearer end
     p.tile = t0 + 1;
     if (p.tile == s.tiles()) {
@@ -212,29 +212,25 @@ struct Rowset {
     }
   }
 
-  // 32 tokens from `key` on: `codes_k(b, c)` and `codes_v(b, c)` give the
-  // lane's 16 codes of sub-block b and dims 64 c, `ks` and `vs` their scales.
-  // `masked`: some row does not see all of them, or the cache ends before.
-  // `after_k` is called once the K codes have been taken.
-  template <typename KCodes, typename VCodes, typename AfterK>
-  __device__ __forceinline__ void step(const Attention &a, KCodes codes_k, VCodes codes_v, AfterK after_k,
-                                       const float (&ks)[2], const float (&vs)[2], int key, int len,
+  // kB sub-blocks of 16 tokens from `key` on.  `k(b, d)` gives the operand of
+  // sub-block b and dims step d, `v(b, d)` that of sub-blocks 2 b and 2 b + 1
+  // and dims 16 d, with 0 for tokens past the cache's end, which may be
+  // anything.  `masked`: some row does not see all of the tokens.  `after_k`
+  // is called once K's operands have been taken.
+  template <int kB, typename KOp, typename VOp, typename AfterK>
+  __device__ __forceinline__ void step(const Attention &a, KOp k, VOp v, AfterK after_k, int key, int len,
                                        bool masked, bool logs, int64_t log_row) {
     const int lane = lane_id(), g = lane >> 4;
-    f4 s[kTiles][2];
+    f4 s[kTiles][kB];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < kB; ++b) {
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) s[t][b] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int c = 0; c < kDim / 64; ++c) {
-        const u4 w = codes_k(b, c);
+      for (int d = 0; d < kDim / 32; ++d) {
+        const v8 x = k(b, d);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const v8 k = widen8<kType>(w[2 * h], w[2 * h + 1], ks[b], ks[b]);
-#pragma unroll
-          for (int t = 0; t < kTiles; ++t) s[t][b] = El<kType>::mfma(k, q[t][2 * c + h], s[t][b]);
-        }
+        for (int t = 0; t < kTiles; ++t) s[t][b] = El<kType>::mfma(x, q[t][d], s[t][b]);
       }
     }
     after_k();
@@ -242,30 +238,27 @@ struct Rowset {
 #pragma unroll
       for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < kB; ++b)
 #pragma unroll
           for (int i = 0; i < 4; ++i)  // tanh(x) = 1 - 2 / (exp(2 x) + 1)
             s[t][b][i] = 1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[t][b][i] * a.cap_in) + 1.f);
     }
-    unsigned mask[2] = {~0u, ~0u};
     if (masked) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const int at = key + 16 * b + 4 * g, live = len - at;
+      for (int t = 0; t < kTiles; ++t) {
+        const int seen = limit[t] - key - 4 * g;
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t)
+        for (int b = 0; b < kB; ++b)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[t][b][i] = at + i <= limit[t] ? s[t][b][i] : -__builtin_inff();
-        // tokens past the cache's end may be anything: their V codes become 0
-        mask[b] = live >= 4 ? ~0u : live <= 0 ? 0u : (1u << 8 * live) - 1;
+          for (int i = 0; i < 4; ++i) s[t][b][i] = 16 * b + i <= seen ? s[t][b][i] : -__builtin_inff();
       }
     }
-    v8 p[kTiles];
+    v8 p[kTiles][kB / 2];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
       float top = s[t][0][0];
 #pragma unroll
-      for (int i = 1; i < 8; ++i) top = fmaxf(top, s[t][i >> 2][i & 3]);
+      for (int i = 1; i < 4 * kB; ++i) top = fmaxf(top, s[t][i >> 2][i & 3]);
       top *= a.scale;
       if (__any(top > m[t] + kSlack)) {
         top = fmaxf(top, __shfl_xor(top, 16));
@@ -276,20 +269,26 @@ struct Rowset {
 #pragma unroll
         for (int d = 0; d < kDim / 16; ++d) o[t][d] *= f;
       }
-      float e[8], half[2] = {0.f, 0.f};
+      float part[kB];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i >> 2][i & 3], a.scale, -m[t]));
-        half[i >> 2] += e[i];
+      for (int b = 0; b < kB; ++b) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          s[t][b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][b][i], a.scale, -m[t]));
+        part[b] = (s[t][b][0] + s[t][b][1]) + (s[t][b][2] + s[t][b][3]);
+        sum[t] += part[b];
       }
-      sum[t] += half[0] + half[1];
-      const u4 w = {narrow2<kType>(e[0], e[1]), narrow2<kType>(e[2], e[3]), narrow2<kType>(e[4], e[5]),
-                    narrow2<kType>(e[6], e[7])};
-      p[t] = __builtin_bit_cast(v8, w);
+#pragma unroll
+      for (int b = 0; b < kB; b += 2) {
+        const u4 w = {narrow2<kType>(s[t][b][0], s[t][b][1]), narrow2<kType>(s[t][b][2], s[t][b][3]),
+                      narrow2<kType>(s[t][b + 1][0], s[t][b + 1][1]),
+                      narrow2<kType>(s[t][b + 1][2], s[t][b + 1][3])};
+        p[t][b / 2] = __builtin_bit_cast(v8, w);
+      }
       if (logs) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          float x = half[b];
+        for (int b = 0; b < kB; ++b) {
+          float x = part[b];
           x += __shfl_xor(x, 16);
           x += __shfl_xor(x, 32);
           if (g == 0 && log_at[t] && key + 16 * b < len)
@@ -298,13 +297,12 @@ struct Rowset {
       }
     }
 #pragma unroll
-    for (int c = 0; c < kDim / 64; ++c) {
-      const u4 w0 = codes_v(0, c), w1 = codes_v(1, c);
+    for (int b = 0; b < kB / 2; ++b) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const v8 v = widen8<kType>(w0[i] & mask[0], w1[i] & mask[1], vs[0], vs[1]);
+      for (int d = 0; d < kDim / 16; ++d) {
+        const v8 x = v(b, d);
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) o[t][4 * c + i] = El<kType>::mfma(v, p[t], o[t][4 * c + i]);
+        for (int t = 0; t < kTiles; ++t) o[t][d] = El<kType>::mfma(x, p[t][b], o[t][d]);
       }
     }
   }
@@ -349,6 +347,12 @@ struct Cache {
 __device__ __forceinline__ int k_place() { return (lane_id() & 15) * 64 + (lane_id() >> 4) * 16; }
 __device__ __forceinline__ int v_place() { return lane_id() * 16; }
 
+// Of 4 tokens `at` .. at + 4, the bytes of those before `len`.
+__device__ __forceinline__ unsigned live_bytes(int at, int len) {
+  const int n = len - at;
+  return n >= 4 ? ~0u : n <= 0 ? 0u : (1u << 8 * n) - 1;
+}
+
 // 32 cached tokens of one head in registers: two sub-blocks.
 template <int kDim>
 struct Codes {
@@ -378,6 +382,10 @@ struct Codes {
 
 // kKeyWaves waves share a row tile's tokens and combine in LDS; the
 // kWaves / kKeyWaves groups of them each have rows of their own.
+// Bytes of the list of requests at the head of a workgroup's LDS.
+__host__ __device__ constexpr int list_bytes(int n) { return (12 * n + 8 + 15) & ~15; }
+// Tokens that a row tile's waves share at a time.
+__host__ __device__ constexpr int stage_tokens(int dim) { return dim == 256 ? 32 : 64; }
 constexpr int waves_per_simd(int dim, int tiles, int key_waves) {
   if (key_waves == 1) return dim == 256 ? 1 : 2;
   const int held = dim * tiles;  // of q, o and codes in registers
@@ -388,11 +396,12 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles, kKeyWaves)) vo
   constexpr int kRows = 16 * kTiles * (kWaves / kKeyWaves);
   constexpr int kPart = kDim < 128 ? kDim : 128;  // dims that one combination takes
   constexpr int kPitch = kPart + 4;
+  typedef typename El<kType>::v8 v8;
   extern __shared__ __align__(16) char lds[];
   __shared__ unsigned long long scan[2 * kWaves];
   long long *before = reinterpret_cast<long long *>(lds);
   int *ids = reinterpret_cast<int *>(before + a.batch.n + 1);
-  float *mix = reinterpret_cast<float *>(lds + ((12 * a.batch.n + 8 + 15) & ~15));
+  float *mix = reinterpret_cast<float *>(lds + list_bytes(a.batch.n));
   const int lane = lane_id(), g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(wave_id());
   const int kv_heads = a.kv.kv_heads;
@@ -526,9 +535,24 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles, kKeyWaves)) vo
         look(key + kStride);
         while (true) {
           const int next = key + kStride;
-          r.step(a, [&](int b, int i) { return c.k[b][i]; }, [&](int b, int i) { return c.v[b][i]; },
-                 [&] { if (next < key_end) c.fetch_k(cache, slot, next); }, c.ks, c.vs, key, req.len,
-                 key + 32 > clear_end, logs, log_row);
+          if (key + 32 > req.len) {
+            const unsigned live[2] = {live_bytes(key + 4 * g, req.len), live_bytes(key + 16 + 4 * g, req.len)};
+#pragma unroll
+            for (int i = 0; i < kDim / 64; ++i)
+#pragma unroll
+              for (int b = 0; b < 2; ++b) c.v[b][i] &= live[b];
+          }
+          r.template step<2>(
+              a,
+              [&](int b, int d) {
+                const u4 w = c.k[b][d >> 1];
+                return widen8<kType>(w[2 * (d & 1)], w[2 * (d & 1) + 1], c.ks[b], c.ks[b]);
+              },
+              [&](int, int d) {
+                return widen8<kType>(c.v[0][d >> 2][d & 3], c.v[1][d >> 2][d & 3], c.vs[0], c.vs[1]);
+              },
+              [&] { if (next < key_end) c.fetch_k(cache, slot, next); }, key, req.len, key + 32 > clear_end,
+              logs, log_row);
           if (next >= key_end) break;
           c.fetch_v(cache, slot, next);
           look(next + kStride);
@@ -536,67 +560,79 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles, kKeyWaves)) vo
         }
       }
     } else {
-      // the waves share the tokens through LDS, kStage of them at a time, in
-      // operand order; the next stage's codes cross in registers meanwhile
-      constexpr int kSubs = kDim == 256 ? 2 : 4, kStage = 16 * kSubs;
-      constexpr int kSub = 16 * kDim, kPieces = kSubs * 2 * kDim / 64;  // of 1 KiB: sub-block, K or V, 64 dims
-      constexpr int kOwn = kPieces / kWaves;
-      char *stage = lds + ((12 * a.batch.n + 8 + 15) & ~15);
+      // the waves share the tokens through LDS, kStage of them at a time,
+      // widened once and in operand order; the next stage's codes cross in
+      // registers meanwhile.  Pieces of 1 KiB of codes: sub-block, K or V, 64
+      // dims; a wave carries kOwn, all of one sub-block and side or both.
+      constexpr int kSubs = stage_tokens(kDim) / 16, kStage = 16 * kSubs;
+      constexpr int kSlices = kDim / 64, kOwn = kSubs * 2 * kSlices / kWaves;
+      constexpr int kBytes = kStage * kDim * 4;  // of a stage: K's operands, then V's
+      char *stage = lds + list_bytes(a.batch.n);
       const int block_end = min(stop, min(req.len, shown + min((at.tile + 1) * a.tile_tokens, req.count)));
+      const int sub = wave * kOwn / (2 * kSlices);
       u4 own[kOwn];
-      float ks[2][kSubs], vs[2][kSubs];
-      auto fetch = [&](int key, float (&k)[kSubs], float (&v)[kSubs]) {
-        const char *block[kSubs];
-#pragma unroll
-        for (int b = 0; b < kSubs; ++b) {
-          block[b] = cache.block(cache.slot((key >> 4) + b));
-          k[b] = cache.k_scale(block[b]);
-          v[b] = cache.v_scale(block[b]);
-        }
-        // piece p of a stage: sub-block p / (2 kDim / 64), then K before V
+      float ks, vs;
+      int live_key;
+      auto fetch = [&](int key) {
+        const char *block = cache.block(cache.slot((key >> 4) + sub));
+        const char *from = cache.codes(block, (key >> 4) + sub);
+        ks = cache.k_scale(block);
+        vs = cache.v_scale(block);
+        live_key = key + 16 * sub;
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) {
-          const int p = wave * kOwn + i, b = p / (2 * kDim / 64), side = p / (kDim / 64) & 1;
-          const char *from = block[0];
-#pragma unroll
-          for (int j = 1; j < kSubs; ++j) from = b == j ? block[j] : from;
-          own[i] = *reinterpret_cast<const u4 *>(cache.codes(from, (key >> 4) + b) + side * cache.kv_stride +
-                                                 p % (kDim / 64) * 1024 + (side ? v_place() : k_place()));
+          const int p = (wave * kOwn + i) % (2 * kSlices), side = p / kSlices;
+          own[i] = *reinterpret_cast<const u4 *>(from + side * cache.kv_stride + p % kSlices * 1024 +
+                                                 (side ? v_place() : k_place()));
         }
       };
-      auto put = [&](int buffer) {
+      // K: operand [sub-block][dims step][lane]; V: [pair of sub-blocks][16 dims][lane],
+      // the pair's halves side by side
+      auto put = [&](char *to) {
+        const unsigned live = live_bytes(live_key + 4 * g, req.len);
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i)
-          *reinterpret_cast<u4 *>(stage + buffer * kPieces * 1024 + (wave * kOwn + i) * 1024 + lane * 16) = own[i];
-      };
-      auto compute = [&](int buffer, int key, const float (&k)[kSubs], const float (&v)[kSubs]) {
+        for (int i = 0; i < kOwn; ++i) {
+          const int p = (wave * kOwn + i) % (2 * kSlices), side = p / kSlices, c = p % kSlices;
+          if (side == 0) {
+            char *at = to + ((sub * kSlices + c) * 2 * 64 + lane) * 16;
 #pragma unroll
-        for (int h = 0; h < kSubs / 2; ++h) {
-          if (key + 32 * h >= key_end) break;
-          const char *from = stage + buffer * kPieces * 1024 + h * 4 * kSub + lane * 16;
-          const float k2[2] = {k[2 * h], k[2 * h + 1]}, v2[2] = {v[2 * h], v[2 * h + 1]};
-          r.step(a, [&](int b, int i) { return *reinterpret_cast<const u4 *>(from + b * 2 * kSub + i * 1024); },
-                 [&](int b, int i) { return *reinterpret_cast<const u4 *>(from + b * 2 * kSub + kSub + i * 1024); },
-                 [] {}, k2, v2, key + 32 * h, req.len, key + 32 * h + 32 > clear_end, logs, log_row);
+            for (int h = 0; h < 2; ++h)
+              *reinterpret_cast<v8 *>(at + h * 1024) = widen8<kType>(own[i][2 * h], own[i][2 * h + 1], ks, ks);
+          } else {
+            char *at = to + kBytes / 2 + (((sub >> 1) * 4 * kSlices + 4 * c) * 64 + lane) * 16 + (sub & 1) * 8;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const unsigned w = own[i][j] & live;
+              *reinterpret_cast<u2 *>(at + j * 1024) = u2{El<kType>::widen_lo(w, vs), El<kType>::widen_hi(w, vs)};
+            }
+          }
         }
       };
-      int key = at.key;
-      if (key < block_end) {
-        fetch(key, ks[0], vs[0]);
-        put(0);
+      auto compute = [&](const char *from, int key) {
+        if (key >= key_end) return;
+        r.template step<kSubs>(
+            a,
+            [&](int b, int d) {
+              return *reinterpret_cast<const v8 *>(from + ((b * 2 * kSlices + d) * 64 + lane) * 16);
+            },
+            [&](int b, int d) {
+              return *reinterpret_cast<const v8 *>(from + kBytes / 2 + ((b * 4 * kSlices + d) * 64 + lane) * 16);
+            },
+            [] {}, key, req.len, key + kStage > clear_end, logs, log_row);
+      };
+      if (at.key < block_end) {
+        fetch(at.key);
+        put(stage);
         __syncthreads();
-        while (true) {
-          if (key + kStage < block_end) fetch(key + kStage, ks[1], vs[1]);
-          compute(0, key, ks[0], vs[0]);
-          key += kStage;
-          if (key >= block_end) break;
-          put(1);
-          __syncthreads();
-          if (key + kStage < block_end) fetch(key + kStage, ks[0], vs[0]);
-          compute(1, key, ks[1], vs[1]);
-          key += kStage;
-          if (key >= block_end) break;
-          put(0);
+        int buffer = 0;
+        for (int key = at.key;;) {
+          const int next = key + kStage;
+          if (next < block_end) fetch(next);
+          compute(stage + buffer * kBytes, key);
+          if (next >= block_end) break;
+          key = next;
+          buffer ^= 1;
+          put(stage + buffer * kBytes);
           __syncthreads();
         }
       }
@@ -816,13 +852,12 @@ bool heads_ok(const cascade_kv_format_t *f, int q_heads) {
 
 template <int kType, int kDim, int kTiles, int kKeyWaves>
 void start(const Attention &a, int grid, bool cap, hipStream_t stream) {
-  const size_t list = (12 * (size_t)a.batch.n + 8 + 15) & ~(size_t)15;
-  // combination of the waves, or two stages of codes
+  // combination of the waves, or two stages of operands
   const size_t mix = kKeyWaves > 1 ? sizeof(float) * kWaves * 16 * (2 + (kDim < 128 ? kDim : 128) + 4)
-                                   : 2 * (kDim == 256 ? 32 : 64) * 2 * kDim;
+                                   : 2 * stage_tokens(kDim) * 4 * kDim;
   auto kernel = cap ? attention_kernel<kType, kDim, kTiles, kKeyWaves, true>
                     : attention_kernel<kType, kDim, kTiles, kKeyWaves, false>;
-  hipLaunchKernelGGL(kernel, dim3(grid), dim3(kBlock), list + mix, stream, a);
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(kBlock), list_bytes(a.batch.n) + mix, stream, a);
 }
 
 template <int kType, int kDim>
@@ -837,6 +872,7 @@ int run(Attention a, char *ws, const Workspace &w, bool cap, float *block_weight
   a.max_rows = small;
   a.tile_tokens = small / a.group > 0 ? small / a.group : 1;
   a.atomic_keys = 0;
+  a.cut_keys = 32;
   a.range_keys = 256;
   a.splits = reinterpret_cast<Split *>(ws + w.splits);
   a.parts = reinterpret_cast<float *>(ws + w.parts);
@@ -856,6 +892,7 @@ int run(Attention a, char *ws, const Workspace &w, bool cap, float *block_weight
     a.max_rows = INT64_MAX;
     a.tile_tokens = kTileRows / a.group;
     a.atomic_keys = 2048;
+    a.cut_keys = stage_tokens(kDim);
     a.range_keys = 256;
     a.splits = reinterpret_cast<Split *>(ws + w.tile_splits);
     a.parts = reinterpret_cast<float *>(ws + w.tile_parts);
