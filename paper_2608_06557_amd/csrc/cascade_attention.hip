@@ -36,6 +36,7 @@ namespace {
 
 typedef float f2 __attribute__((ext_vector_type(2)));
 typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f16v __attribute__((ext_vector_type(16)));
 typedef unsigned u2 __attribute__((ext_vector_type(2)));
 typedef unsigned u4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
@@ -60,6 +61,9 @@ template <> struct El<CASCADE_BF16> {
   static __device__ __forceinline__ f4 mfma(v8 a, v8 b, f4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
   }
+  static __device__ __forceinline__ f16v mfma(v8 a, v8 b, f16v c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
 };
 template <> struct El<CASCADE_F16> {
   typedef h2 v2;
@@ -72,6 +76,9 @@ template <> struct El<CASCADE_F16> {
   }
   static __device__ __forceinline__ f4 mfma(v8 a, v8 b, f4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f16v mfma(v8 a, v8 b, f16v c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
   }
 };
 
@@ -185,10 +192,94 @@ __device__ __forceinline__ Place locate(const Attention &a, const long long *bef
   return p;
 }
 
-__device__ __forceinline__ Place uniform(const Place &p, int lane) {
+// A lane's place, as wave-uniform numbers.
+__device__ __forceinline__ Place uniform(const Place &p, int lane = 0) {
   return {__builtin_amdgcn_readlane(p.item, lane), __builtin_amdgcn_readlane(p.head, lane),
           __builtin_amdgcn_readlane(p.tile, lane), __builtin_amdgcn_readlane(p.key, lane)};
 }
+
+__device__ __forceinline__ long long first_lane(unsigned long long x) {
+  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)x);
+  return (long long)((unsigned long long)__builtin_amdgcn_readfirstlane((unsigned)(x >> 32)) << 32 | lo);
+}
+
+// The part of the work that a workgroup takes.
+struct Range {
+  Place begin, end;
+  int items;  // requests in the list
+  int group;  // which range it is
+
+  // Fills the list (`before`: cost before each of its requests, and the total;
+  // `ids`: their numbers; both in LDS) and finds the range; false if there is
+  // none.  Called by all threads.  Records the segment that the range's begin
+  // is the first cut of.
+  template <int kW>
+  __device__ __forceinline__ bool find(const Attention &a, long long *before, int *ids,
+                                       unsigned long long *scan) {
+    const int lane = lane_id();
+    // the list of requests with rows of this kernel's kind, and the cost before each
+    int n = 0;
+    long long total = 0;
+    for (int i0 = 0; i0 < a.batch.n; i0 += 64 * kW) {
+      const int i = i0 + threadIdx.x;
+      unsigned long long v[2] = {0, 0}, all[2];
+      if (i < a.batch.n) {
+        const KvRequest r = kv_request(a.batch, a.row_offsets, a.kv.block_shift, i);
+        if (!r.ok) {
+          kv_report(a.status);
+        } else {
+          const int64_t rows = (int64_t)r.count * a.group;
+          if (rows > a.min_rows && rows <= a.max_rows)
+            v[0] = Segments(r, a.tile_tokens).total() * a.kv.kv_heads;
+        }
+      }
+      const unsigned long long cost = v[0];
+      v[1] = cost > 0;
+      block_exclusive_scan<2, unsigned long long, kW>(v, all, scan);
+      if (cost) {
+        before[n + v[1]] = total + v[0];
+        ids[n + v[1]] = i;
+      }
+      n += __builtin_amdgcn_readfirstlane((int)all[1]);
+      total += first_lane(all[0]);
+    }
+    if (threadIdx.x == 0) before[n] = total;
+    __syncthreads();
+
+    // this workgroup's range: neighbours in cost on one XCD (workgroups go to
+    // the 8 XCDs in turn), where heads and row tiles of a request share its L2
+    const int cap = (int)min((long long)gridDim.x, total / a.range_keys);
+    const int groups = cap >= 8 ? cap & ~7 : max(cap, 1);
+    const int block = blockIdx.x;
+    if (block >= groups || n == 0) {
+      if (threadIdx.x == 0) a.splits[block] = Split{-1, 0, 0, 0};
+      return false;
+    }
+    const int w = groups >= 8 ? (block & 7) * (groups >> 3) + (block >> 3) : block;
+    // lanes 0, 1, 2: this range's begin, its end, the one before's begin
+    const int which = lane == 1 ? w + 1 : lane == 2 ? max(w - 1, 0) : w;
+    const Place found = locate(a, before, ids, n, total * which / groups);
+    const Place at = uniform(found, 0), prev = uniform(found, 2);
+    begin = at;
+    end = uniform(found, 1);
+    items = n;
+    group = w;
+
+    if (threadIdx.x == 0) {
+      Split s = {-1, 0, 0, 0};
+      const bool inside = at.key > 0 && !(prev.key > 0 && prev.item == at.item && prev.head == at.head &&
+                                          prev.tile == at.tile);
+      if (inside) {
+        const int id = ids[at.item];
+        const Segments seg(kv_request(a.batch, a.row_offsets, a.kv.block_shift, id), a.tile_tokens);
+        const long long stop = before[at.item] + at.head * seg.total() + seg.start(at.tile) + seg.length(at.tile);
+        s = {id, at.head, at.tile, (int)((stop * groups + total - 1) / total) - 1};
+      }
+      a.splits[w] = s;
+    }
+    return true;
+  }
+};
 
 // ------------------------------------------------------------- one wave
 
@@ -212,16 +303,10 @@ struct Rowset {
     }
   }
 
-  // kB sub-blocks of 16 tokens from `key` on.  `k(b, d)` gives the operand of
-  // sub-block b and dims step d, `v(b, d)` that of sub-blocks 2 b and 2 b + 1
-  // and dims 16 d, with 0 for tokens past the cache's end, which may be
-  // anything.  `masked`: some row does not see all of the tokens.  `after_k`
-  // is called once K's operands have been taken.
-  template <int kB, typename KOp, typename VOp, typename AfterK>
-  __device__ __forceinline__ void step(const Attention &a, KOp k, VOp v, AfterK after_k, int key, int len,
-                                       bool masked, bool logs, int64_t log_row) {
-    const int lane = lane_id(), g = lane >> 4;
-    f4 s[kTiles][kB];
+  // Scores of kB sub-blocks of 16 tokens; `k(b, d)` gives the operand of
+  // sub-block b and dims step d.
+  template <int kB, typename KOp>
+  __device__ __forceinline__ void scores(KOp k, f4 (&s)[kTiles][kB]) const {
 #pragma unroll
     for (int b = 0; b < kB; ++b) {
 #pragma unroll
@@ -233,7 +318,14 @@ struct Rowset {
         for (int t = 0; t < kTiles; ++t) s[t][b] = El<kType>::mfma(x, q[t][d], s[t][b]);
       }
     }
-    after_k();
+  }
+
+  // Their weights, for tokens from `key` on; m, sum and o follow.  `masked`:
+  // some row does not see all of the tokens.
+  template <int kB>
+  __device__ __forceinline__ void weights(const Attention &a, f4 (&s)[kTiles][kB], v8 (&p)[kTiles][kB / 2],
+                                          int key, int len, bool masked, bool logs, int64_t log_row) {
+    const int lane = lane_id(), g = lane >> 4;
     if (kCap) {
 #pragma unroll
       for (int t = 0; t < kTiles; ++t)
@@ -253,30 +345,38 @@ struct Rowset {
           for (int i = 0; i < 4; ++i) s[t][b][i] = 16 * b + i <= seen ? s[t][b][i] : -__builtin_inff();
       }
     }
-    v8 p[kTiles][kB / 2];
+    float top[kTiles];
+    bool over = false;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      float top = s[t][0][0];
+      top[t] = s[t][0][0];
 #pragma unroll
-      for (int i = 1; i < 4 * kB; ++i) top = fmaxf(top, s[t][i >> 2][i & 3]);
-      top *= a.scale;
-      if (__any(top > m[t] + kSlack)) {
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float now = fmaxf(m[t], top), f = __builtin_amdgcn_exp2f(m[t] - now);
+      for (int i = 1; i < 4 * kB; ++i) top[t] = fmaxf(top[t], s[t][i >> 2][i & 3]);
+      top[t] *= a.scale;
+      over |= top[t] > m[t] + kSlack;
+    }
+    if (__any(over)) {
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) {
+        top[t] = fmaxf(top[t], __shfl_xor(top[t], 16));
+        top[t] = fmaxf(top[t], __shfl_xor(top[t], 32));
+        const float now = fmaxf(m[t], top[t]), f = __builtin_amdgcn_exp2f(m[t] - now);
         m[t] = now;
         sum[t] *= f;
 #pragma unroll
         for (int d = 0; d < kDim / 16; ++d) o[t][d] *= f;
       }
-      float part[kB];
+    }
+    float part[kTiles][kB];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
 #pragma unroll
       for (int b = 0; b < kB; ++b) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           s[t][b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][b][i], a.scale, -m[t]));
-        part[b] = (s[t][b][0] + s[t][b][1]) + (s[t][b][2] + s[t][b][3]);
-        sum[t] += part[b];
+        part[t][b] = (s[t][b][0] + s[t][b][1]) + (s[t][b][2] + s[t][b][3]);
+        sum[t] += part[t][b];
       }
 #pragma unroll
       for (int b = 0; b < kB; b += 2) {
@@ -285,25 +385,30 @@ struct Rowset {
                       narrow2<kType>(s[t][b + 1][2], s[t][b + 1][3])};
         p[t][b / 2] = __builtin_bit_cast(v8, w);
       }
-      if (logs) {
+    }
+    if (logs) {
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
 #pragma unroll
         for (int b = 0; b < kB; ++b) {
-          float x = part[b];
+          float x = part[t][b];
           x += __shfl_xor(x, 16);
           x += __shfl_xor(x, 32);
           if (g == 0 && log_at[t] && key + 16 * b < len)
             log_at[t][(int64_t)((key >> 4) + b) * log_row] = __builtin_amdgcn_logf(x) + m[t];
         }
-      }
     }
+  }
+
+  // O of 32 tokens; `v(d)` gives the operand of dims 16 d, with 0 for tokens
+  // past the cache's end, which may be anything.
+  template <typename VOp>
+  __device__ __forceinline__ void add(VOp v, const v8 (&p)[kTiles][1]) {
 #pragma unroll
-    for (int b = 0; b < kB / 2; ++b) {
+    for (int d = 0; d < kDim / 16; ++d) {
+      const v8 x = v(d);
 #pragma unroll
-      for (int d = 0; d < kDim / 16; ++d) {
-        const v8 x = v(b, d);
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) o[t][d] = El<kType>::mfma(x, p[t][b], o[t][d]);
-      }
+      for (int t = 0; t < kTiles; ++t) o[t][d] = El<kType>::mfma(x, p[t][0], o[t][d]);
     }
   }
 };
@@ -315,26 +420,26 @@ struct Cache {
   int64_t kv_stride, slot_stride, scales;  // `scales`: from the codes to the head's scale
   const int32_t *slots;
   int num_slots, shift, last;  // log2 of sub-blocks a block, last sub-block
-  int32_t *status;
   __device__ __forceinline__ Cache(const Attention &a, const KvRequest &r, int head)
       : base(a.kv.base + ((int64_t)head << a.kv.block_shift) * kDim), kv_stride(a.kv.kv_stride),
         slot_stride(a.kv.slot_stride),
         scales(((int64_t)(a.kv.kv_heads - head) << a.kv.block_shift) * kDim + 4 * head),
         slots(a.slots + r.row), num_slots(a.kv.num_slots), shift(a.kv.block_shift - 4),
-        last((r.len - 1) >> 4), status(a.status) {}
-  // the slot of sub-block `sub`, or of the last one
-  __device__ __forceinline__ int slot(int sub) const { return uniform_load(slots + (min(sub, last) >> shift)); }
-  // the head's codes in a slot; a slot outside the pool is reported and read as slot 0
-  __device__ __forceinline__ const char *block(int slot) const {
-    if ((unsigned)slot >= (unsigned)num_slots) {
-      kv_report(status);
-      slot = 0;
-    }
-    return base + slot * slot_stride;
+        last((r.len - 1) >> 4) {}
+  // table entry and slot of sub-block `sub`, or of the last one
+  __device__ __forceinline__ int entry(int sub) const { return min(sub, last) >> shift; }
+  __device__ __forceinline__ int slot(int sub) const { return uniform_load(slots + entry(sub)); }
+  // from slot 0 to a slot
+  __device__ __forceinline__ int64_t offset(int slot, bool &bad) const {
+    const bool fine = (unsigned)slot < (unsigned)num_slots;
+    bad |= !fine;
+    return (fine ? slot : 0) * slot_stride;
   }
-  __device__ __forceinline__ const char *codes(const char *block, int sub) const {
-    return block + (min(sub, last) & ((1 << shift) - 1)) * 16 * kDim;
-  }
+  // the head's codes in a slot; one outside the pool counts as slot 0 and sets `bad`
+  __device__ __forceinline__ const char *block(int slot, bool &bad) const { return base + offset(slot, bad); }
+  // a sub-block within its block's codes
+  __device__ __forceinline__ int place(int sub) const { return (min(sub, last) & ((1 << shift) - 1)) * 16 * kDim; }
+  __device__ __forceinline__ const char *codes(const char *block, int sub) const { return block + place(sub); }
   __device__ __forceinline__ float k_scale(const char *block) const {
     return uniform_load(reinterpret_cast<const float *>(block + scales));
   }
@@ -358,10 +463,11 @@ template <int kDim>
 struct Codes {
   u4 k[2][kDim / 64], v[2][kDim / 64];
   float ks[2], vs[2];
+  bool bad = false;
   __device__ __forceinline__ void fetch_k(const Cache<kDim> &c, const int (&slot)[2], int key) {
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const char *block = c.block(slot[b]), *at = c.codes(block, (key >> 4) + b);
+      const char *block = c.block(slot[b], bad), *at = c.codes(block, (key >> 4) + b);
 #pragma unroll
       for (int i = 0; i < kDim / 64; ++i) k[b][i] = *reinterpret_cast<const u4 *>(at + 1024 * i + k_place());
       ks[b] = c.k_scale(block);
@@ -370,7 +476,7 @@ struct Codes {
   __device__ __forceinline__ void fetch_v(const Cache<kDim> &c, const int (&slot)[2], int key) {
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const char *block = c.block(slot[b]), *at = c.codes(block, (key >> 4) + b) + c.kv_stride;
+      const char *block = c.block(slot[b], bad), *at = c.codes(block, (key >> 4) + b) + c.kv_stride;
 #pragma unroll
       for (int i = 0; i < kDim / 64; ++i) v[b][i] = *reinterpret_cast<const u4 *>(at + 1024 * i + v_place());
       vs[b] = c.v_scale(block);
@@ -380,20 +486,16 @@ struct Codes {
 
 // ------------------------------------------------------------- the kernel
 
-// kKeyWaves waves share a row tile's tokens and combine in LDS; the
-// kWaves / kKeyWaves groups of them each have rows of their own.
+// A tile of up to 16 * kTiles rows; the waves share its tokens and combine in LDS.
 // Bytes of the list of requests at the head of a workgroup's LDS.
 __host__ __device__ constexpr int list_bytes(int n) { return (12 * n + 8 + 15) & ~15; }
-// Tokens that a row tile's waves share at a time.
-__host__ __device__ constexpr int stage_tokens(int dim) { return dim == 256 ? 32 : 64; }
-constexpr int waves_per_simd(int dim, int tiles, int key_waves) {
-  if (key_waves == 1) return dim == 256 ? 1 : 2;
+constexpr int waves_per_simd(int dim, int tiles) {
   const int held = dim * tiles;  // of q, o and codes in registers
   return held <= 64 ? 5 : tiles == 1 && held <= 128 ? 4 : held <= 128 ? 3 : held <= 256 ? 2 : 1;
 }
-template <int kType, int kDim, int kTiles, int kKeyWaves, bool kCap>
-__global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles, kKeyWaves)) void attention_kernel(Attention a) {
-  constexpr int kRows = 16 * kTiles * (kWaves / kKeyWaves);
+template <int kType, int kDim, int kTiles, bool kCap>
+__global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attention_kernel(Attention a) {
+  constexpr int kRows = 16 * kTiles;
   constexpr int kPart = kDim < 128 ? kDim : 128;  // dims that one combination takes
   constexpr int kPitch = kPart + 4;
   typedef typename El<kType>::v8 v8;
@@ -404,70 +506,15 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles, kKeyWaves)) vo
   float *mix = reinterpret_cast<float *>(lds + list_bytes(a.batch.n));
   const int lane = lane_id(), g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(wave_id());
-  const int kv_heads = a.kv.kv_heads;
-
-  // the list of requests with rows of this kernel's kind, and the cost before each
-  int n = 0;
-  long long total = 0;
-  for (int i0 = 0; i0 < a.batch.n; i0 += kBlock) {
-    const int i = i0 + threadIdx.x;
-    unsigned long long v[2] = {0, 0}, all[2];
-    if (i < a.batch.n) {
-      const KvRequest r = kv_request(a.batch, a.row_offsets, a.kv.block_shift, i);
-      if (!r.ok) {
-        kv_report(a.status);
-      } else {
-        const int64_t rows = (int64_t)r.count * a.group;
-        if (rows > a.min_rows && rows <= a.max_rows)
-          v[0] = Segments(r, a.tile_tokens).total() * kv_heads;
-      }
-    }
-    const unsigned long long cost = v[0];
-    v[1] = cost > 0;
-    block_exclusive_scan<2, unsigned long long>(v, all, scan);
-    if (cost) {
-      before[n + v[1]] = total + v[0];
-      ids[n + v[1]] = i;
-    }
-    n += (int)all[1];
-    total += all[0];
-  }
-  if (threadIdx.x == 0) before[n] = total;
-  __syncthreads();
-
-  // this workgroup's range: neighbours in cost on one XCD (workgroups go to
-  // the 8 XCDs in turn), where heads and row tiles of a request share its L2
-  const int cap = (int)min((long long)gridDim.x, total / a.range_keys);
-  const int groups = cap >= 8 ? cap & ~7 : max(cap, 1);
-  const int block = blockIdx.x;
-  if (block >= groups || n == 0) {
-    if (threadIdx.x == 0) a.splits[block] = Split{-1, 0, 0, 0};
-    return;
-  }
-  const int w = groups >= 8 ? (block & 7) * (groups >> 3) + (block >> 3) : block;
-  // lanes 0, 1, 2: this range's begin, its end, the one before's begin
-  const int which = lane == 1 ? w + 1 : lane == 2 ? max(w - 1, 0) : w;
-  const Place found = locate(a, before, ids, n, total * which / groups);
-  Place at = uniform(found, 0);
-  const Place end = uniform(found, 1), prev = uniform(found, 2);
-
-  if (threadIdx.x == 0) {
-    Split s = {-1, 0, 0, 0};
-    const bool inside = at.key > 0 && !(prev.key > 0 && prev.item == at.item && prev.head == at.head &&
-                                        prev.tile == at.tile);
-    if (inside) {
-      const int id = ids[at.item];
-      const Segments seg(kv_request(a.batch, a.row_offsets, a.kv.block_shift, id), a.tile_tokens);
-      const long long stop = before[at.item] + at.head * seg.total() + seg.start(at.tile) + seg.length(at.tile);
-      s = {id, at.head, at.tile, (int)((stop * groups + total - 1) / total) - 1};
-    }
-    a.splits[w] = s;
-  }
+  Range range;
+  if (!range.find<kWaves>(a, before, ids, scan)) return;
+  Place at = range.begin;
+  const Place end = uniform(range.end);
+  const int n = __builtin_amdgcn_readfirstlane(range.items), w = __builtin_amdgcn_readfirstlane(range.group), kv_heads = a.kv.kv_heads;
 
   Rowset<kType, kDim, kTiles, kCap> r;
-  const int row0 = kKeyWaves == kWaves ? 0 : wave / kKeyWaves * 16 * kTiles;
-  const int key_wave = wave % kKeyWaves;
   while (at.item < n) {
+    at = uniform(at);  // the compiler does not see that it is
     const int id = __builtin_amdgcn_readfirstlane(ids[at.item]);
     const KvRequest req = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, id);
     const Segments seg(req, a.tile_tokens);
@@ -476,7 +523,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles, kKeyWaves)) vo
     const int stop = last ? end.key : length;
     if (last && stop == at.key) break;
 
-    // rows: lane n of row set t has row row0 + 16 t + n of the tile
+    // rows: lane n of row set t has row 16 t + n of the tile
     const int tile_rows = a.tile_tokens * a.group, shown = req.len - req.count;
     bool valid[kTiles];
     int token[kTiles], head[kTiles];
@@ -484,7 +531,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles, kKeyWaves)) vo
     bool logs = false;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      const int row = row0 + 16 * t + (lane & 15);
+      const int row = 16 * t + (lane & 15);
       token[t] = at.tile * a.tile_tokens + row / a.group;
       head[t] = at.head * a.group + row % a.group;
       valid[t] = row < tile_rows && token[t] < req.count;
@@ -508,135 +555,57 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles, kKeyWaves)) vo
     logs = __any(logs);
     r.clear();
 
-    // the wave's rows begin at token first_token and end at last_token
-    const int first_token = at.tile * a.tile_tokens + row0 / a.group;
-    const int last_token =
-        min(at.tile * a.tile_tokens + (min(row0 + 16 * kTiles, tile_rows) - 1) / a.group, req.count - 1);
-    const int key_end =
-        row0 >= tile_rows || first_token >= req.count ? 0 : min(min(stop, req.len), shown + last_token + 1);
-    const int clear_end = shown + first_token + 1;  // every row sees the tokens before it
+    // every row sees the tokens before clear_end, none those from key_end on
+    const int first_token = at.tile * a.tile_tokens;
+    const int last_token = min(first_token + a.tile_tokens, req.count) - 1;
+    const int clear_end = shown + first_token + 1, key_end = min(min(stop, req.len), shown + last_token + 1);
     const Cache<kDim> cache(a, req, at.head);
-    if (kKeyWaves > 1) {
-      // each wave takes every kKeyWaves-th 32 tokens, straight into registers:
-      // the next K codes leave when these have been taken, V codes likewise,
-      // and the slots are known a step ahead of them
-      constexpr int kStride = 32 * kKeyWaves;
-      int key = at.key + 32 * key_wave;
-      if (key < key_end) {
-        Codes<kDim> c;
-        int slot[2];
-        auto look = [&](int key) {
-          slot[0] = cache.slot(key >> 4);
-          slot[1] = cache.slot((key >> 4) + 1);
-        };
-        look(key);
-        c.fetch_k(cache, slot, key);
-        c.fetch_v(cache, slot, key);
-        look(key + kStride);
-        while (true) {
-          const int next = key + kStride;
-          if (key + 32 > req.len) {
-            const unsigned live[2] = {live_bytes(key + 4 * g, req.len), live_bytes(key + 16 + 4 * g, req.len)};
-#pragma unroll
-            for (int i = 0; i < kDim / 64; ++i)
-#pragma unroll
-              for (int b = 0; b < 2; ++b) c.v[b][i] &= live[b];
-          }
-          r.template step<2>(
-              a,
-              [&](int b, int d) {
-                const u4 w = c.k[b][d >> 1];
-                return widen8<kType>(w[2 * (d & 1)], w[2 * (d & 1) + 1], c.ks[b], c.ks[b]);
-              },
-              [&](int, int d) {
-                return widen8<kType>(c.v[0][d >> 2][d & 3], c.v[1][d >> 2][d & 3], c.vs[0], c.vs[1]);
-              },
-              [&] { if (next < key_end) c.fetch_k(cache, slot, next); }, key, req.len, key + 32 > clear_end,
-              logs, log_row);
-          if (next >= key_end) break;
-          c.fetch_v(cache, slot, next);
-          look(next + kStride);
-          key = next;
-        }
-      }
-    } else {
-      // the waves share the tokens through LDS, kStage of them at a time,
-      // widened once and in operand order; the next stage's codes cross in
-      // registers meanwhile.  Pieces of 1 KiB of codes: sub-block, K or V, 64
-      // dims; a wave carries kOwn, all of one sub-block and side or both.
-      constexpr int kSubs = stage_tokens(kDim) / 16, kStage = 16 * kSubs;
-      constexpr int kSlices = kDim / 64, kOwn = kSubs * 2 * kSlices / kWaves;
-      constexpr int kBytes = kStage * kDim * 4;  // of a stage: K's operands, then V's
-      char *stage = lds + list_bytes(a.batch.n);
-      const int block_end = min(stop, min(req.len, shown + min((at.tile + 1) * a.tile_tokens, req.count)));
-      const int sub = wave * kOwn / (2 * kSlices);
-      u4 own[kOwn];
-      float ks, vs;
-      int live_key;
-      auto fetch = [&](int key) {
-        const char *block = cache.block(cache.slot((key >> 4) + sub));
-        const char *from = cache.codes(block, (key >> 4) + sub);
-        ks = cache.k_scale(block);
-        vs = cache.v_scale(block);
-        live_key = key + 16 * sub;
-#pragma unroll
-        for (int i = 0; i < kOwn; ++i) {
-          const int p = (wave * kOwn + i) % (2 * kSlices), side = p / kSlices;
-          own[i] = *reinterpret_cast<const u4 *>(from + side * cache.kv_stride + p % kSlices * 1024 +
-                                                 (side ? v_place() : k_place()));
-        }
+    // each wave takes every fourth 32 tokens, straight into registers:
+    // the next K codes leave when these have been taken, V codes likewise,
+    // and the slots are known a step ahead of them
+    constexpr int kStride = 32 * kWaves;
+    int key = __builtin_amdgcn_readfirstlane(at.key + 32 * wave);
+    if (key < key_end) {
+      Codes<kDim> c;
+      int slot[2];
+      auto look = [&](int key) {
+        slot[0] = cache.slot(key >> 4);
+        slot[1] = cache.slot((key >> 4) + 1);
       };
-      // K: operand [sub-block][dims step][lane]; V: [pair of sub-blocks][16 dims][lane],
-      // the pair's halves side by side
-      auto put = [&](char *to) {
-        const unsigned live = live_bytes(live_key + 4 * g, req.len);
+      look(key);
+      c.fetch_k(cache, slot, key);
+      c.fetch_v(cache, slot, key);
+      look(key + kStride);
+      while (true) {
+        const int next = key + kStride;
+        if (key + 32 > req.len) {
+          const unsigned live[2] = {live_bytes(key + 4 * g, req.len), live_bytes(key + 16 + 4 * g, req.len)};
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) {
-          const int p = (wave * kOwn + i) % (2 * kSlices), side = p / kSlices, c = p % kSlices;
-          if (side == 0) {
-            char *at = to + ((sub * kSlices + c) * 2 * 64 + lane) * 16;
+          for (int i = 0; i < kDim / 64; ++i)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-              *reinterpret_cast<v8 *>(at + h * 1024) = widen8<kType>(own[i][2 * h], own[i][2 * h + 1], ks, ks);
-          } else {
-            char *at = to + kBytes / 2 + (((sub >> 1) * 4 * kSlices + 4 * c) * 64 + lane) * 16 + (sub & 1) * 8;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const unsigned w = own[i][j] & live;
-              *reinterpret_cast<u2 *>(at + j * 1024) = u2{El<kType>::widen_lo(w, vs), El<kType>::widen_hi(w, vs)};
-            }
-          }
+            for (int b = 0; b < 2; ++b) c.v[b][i] &= live[b];
         }
-      };
-      auto compute = [&](const char *from, int key) {
-        if (key >= key_end) return;
-        r.template step<kSubs>(
-            a,
+        f4 x[kTiles][2];
+        r.template scores<2>(
             [&](int b, int d) {
-              return *reinterpret_cast<const v8 *>(from + ((b * 2 * kSlices + d) * 64 + lane) * 16);
+              const u4 w = c.k[b][d >> 1];
+              return widen8<kType>(w[2 * (d & 1)], w[2 * (d & 1) + 1], c.ks[b], c.ks[b]);
             },
-            [&](int b, int d) {
-              return *reinterpret_cast<const v8 *>(from + kBytes / 2 + ((b * 4 * kSlices + d) * 64 + lane) * 16);
+            x);
+        if (next < key_end) c.fetch_k(cache, slot, next);
+        v8 p[kTiles][1];
+        r.template weights<2>(a, x, p, key, req.len, key + 32 > clear_end, logs, log_row);
+        r.add(
+            [&](int d) {
+              return widen8<kType>(c.v[0][d >> 2][d & 3], c.v[1][d >> 2][d & 3], c.vs[0], c.vs[1]);
             },
-            [] {}, key, req.len, key + kStage > clear_end, logs, log_row);
-      };
-      if (at.key < block_end) {
-        fetch(at.key);
-        put(stage);
-        __syncthreads();
-        int buffer = 0;
-        for (int key = at.key;;) {
-          const int next = key + kStage;
-          if (next < block_end) fetch(next);
-          compute(stage + buffer * kBytes, key);
-          if (next >= block_end) break;
-          key = next;
-          buffer ^= 1;
-          put(stage + buffer * kBytes);
-          __syncthreads();
-        }
+            p);
+        if (next >= key_end) break;
+        c.fetch_v(cache, slot, next);
+        look(next + kStride);
+        key = next;
       }
-      __syncthreads();
+      if (c.bad) kv_report(a.status);
     }
 
 #pragma unroll
@@ -646,80 +615,53 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles, kKeyWaves)) vo
     }
     const bool whole = at.key == 0 && stop == length;
     const int64_t part = ((int64_t)w * 2 + (at.key > 0 ? 0 : 1)) * kRows;
-    if (kKeyWaves == 1) {
+    // the waves' m, sum and O of one row set at a time
+    float *ms = mix, *os = mix + 2 * kWaves * 16;
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t) {
-        const int row = row0 + 16 * t + (lane & 15);
-        if (!valid[t]) continue;
-        if (whole) {
-          const float f = r.sum[t] > 0.f ? 1.f / r.sum[t] : r.sum[t] == 0.f ? 0.f : r.sum[t];
-          char *out = a.out.data + (int64_t)(req.first + token[t]) * a.out.token_stride +
-                      head[t] * a.out.head_stride;
-#pragma unroll
-          for (int d = 0; d < kDim / 16; ++d) {
-            const u2 x = {narrow2<kType>(r.o[t][d][0] * f, r.o[t][d][1] * f),
-                          narrow2<kType>(r.o[t][d][2] * f, r.o[t][d][3] * f)};
-            *reinterpret_cast<u2 *>(out + 2 * (16 * d + 4 * g)) = x;
-          }
-          if (a.lse && g == 0)
-            a.lse[(int64_t)(req.first + token[t]) * a.q_heads + head[t]] =
-                (r.m[t] + __builtin_amdgcn_logf(r.sum[t])) * kLn2;
-        } else {
-          float *o = a.parts + (part + row) * kDim + 4 * g;
-#pragma unroll
-          for (int d = 0; d < kDim / 16; ++d) *reinterpret_cast<f4 *>(o + 16 * d) = r.o[t][d];
-          if (g == 0) *reinterpret_cast<f2 *>(a.part_sums + 2 * (part + row)) = f2{r.m[t], r.sum[t]};
-        }
+    for (int t = 0; t < kTiles; ++t) {
+      if (g == 0) {
+        ms[(wave * 16 + lane) * 2] = r.m[t];
+        ms[(wave * 16 + lane) * 2 + 1] = r.sum[t];
       }
-    } else {
-      // the waves' m, sum and O of one row set at a time
-      float *ms = mix, *os = mix + 2 * kWaves * 16;
+      __syncthreads();
+      float top = kLowest;
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t) {
-        if (g == 0) {
-          ms[(wave * 16 + lane) * 2] = r.m[t];
-          ms[(wave * 16 + lane) * 2 + 1] = r.sum[t];
+      for (int k = 0; k < kWaves; ++k) top = fmaxf(top, ms[(k * 16 + (lane & 15)) * 2]);
+      const float f = __builtin_amdgcn_exp2f(r.m[t] - top);
+#pragma unroll
+      for (int d0 = 0; d0 < kDim; d0 += kPart) {
+#pragma unroll
+        for (int d = d0 / 16; d < (d0 + kPart) / 16; ++d)
+          *reinterpret_cast<f4 *>(os + (wave * 16 + (lane & 15)) * kPitch + 16 * d - d0 + 4 * g) = r.o[t][d] * f;
+        __syncthreads();
+        for (int j = threadIdx.x; j < 16 * kPart / 4; j += kBlock) {
+          const int n16 = j / (kPart / 4), d = j % (kPart / 4) * 4;
+          f4 o = {0.f, 0.f, 0.f, 0.f};
+          float m = kLowest, sum = 0.f;
+#pragma unroll
+          for (int k = 0; k < kWaves; ++k) {
+            o += *reinterpret_cast<const f4 *>(os + (k * 16 + n16) * kPitch + d);
+            m = fmaxf(m, ms[(k * 16 + n16) * 2]);
+          }
+#pragma unroll
+          for (int k = 0; k < kWaves; ++k)
+            sum += ms[(k * 16 + n16) * 2 + 1] * __builtin_amdgcn_exp2f(ms[(k * 16 + n16) * 2] - m);
+          const int row = 16 * t + n16, tok = at.tile * a.tile_tokens + row / a.group;
+          if (row >= tile_rows || tok >= req.count) continue;
+          if (whole) {
+            const int h = at.head * a.group + row % a.group;
+            const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
+            const u2 x = {narrow2<kType>(o[0] * inv, o[1] * inv), narrow2<kType>(o[2] * inv, o[3] * inv)};
+            *reinterpret_cast<u2 *>(a.out.data + (int64_t)(req.first + tok) * a.out.token_stride +
+                                    h * a.out.head_stride + 2 * (d0 + d)) = x;
+            if (a.lse && d0 + d == 0)
+              a.lse[(int64_t)(req.first + tok) * a.q_heads + h] = (m + __builtin_amdgcn_logf(sum)) * kLn2;
+          } else {
+            *reinterpret_cast<f4 *>(a.parts + (part + row) * kDim + d0 + d) = o;
+            if (d0 + d == 0) *reinterpret_cast<f2 *>(a.part_sums + 2 * (part + row)) = f2{m, sum};
+          }
         }
         __syncthreads();
-        float top = kLowest;
-#pragma unroll
-        for (int k = 0; k < kWaves; ++k) top = fmaxf(top, ms[(k * 16 + (lane & 15)) * 2]);
-        const float f = __builtin_amdgcn_exp2f(r.m[t] - top);
-#pragma unroll
-        for (int d0 = 0; d0 < kDim; d0 += kPart) {
-#pragma unroll
-          for (int d = d0 / 16; d < (d0 + kPart) / 16; ++d)
-            *reinterpret_cast<f4 *>(os + (wave * 16 + (lane & 15)) * kPitch + 16 * d - d0 + 4 * g) = r.o[t][d] * f;
-          __syncthreads();
-          for (int j = threadIdx.x; j < 16 * kPart / 4; j += kBlock) {
-            const int n16 = j / (kPart / 4), d = j % (kPart / 4) * 4;
-            f4 o = {0.f, 0.f, 0.f, 0.f};
-            float m = kLowest, sum = 0.f;
-#pragma unroll
-            for (int k = 0; k < kWaves; ++k) {
-              o += *reinterpret_cast<const f4 *>(os + (k * 16 + n16) * kPitch + d);
-              m = fmaxf(m, ms[(k * 16 + n16) * 2]);
-            }
-#pragma unroll
-            for (int k = 0; k < kWaves; ++k)
-              sum += ms[(k * 16 + n16) * 2 + 1] * __builtin_amdgcn_exp2f(ms[(k * 16 + n16) * 2] - m);
-            const int row = 16 * t + n16, tok = at.tile * a.tile_tokens + row / a.group;
-            if (row >= tile_rows || tok >= req.count) continue;
-            if (whole) {
-              const int h = at.head * a.group + row % a.group;
-              const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
-              const u2 x = {narrow2<kType>(o[0] * inv, o[1] * inv), narrow2<kType>(o[2] * inv, o[3] * inv)};
-              *reinterpret_cast<u2 *>(a.out.data + (int64_t)(req.first + tok) * a.out.token_stride +
-                                      h * a.out.head_stride + 2 * (d0 + d)) = x;
-              if (a.lse && d0 + d == 0)
-                a.lse[(int64_t)(req.first + tok) * a.q_heads + h] = (m + __builtin_amdgcn_logf(sum)) * kLn2;
-            } else {
-              *reinterpret_cast<f4 *>(a.parts + (part + row) * kDim + d0 + d) = o;
-              if (d0 + d == 0) *reinterpret_cast<f2 *>(a.part_sums + 2 * (part + row)) = f2{m, sum};
-            }
-          }
-          __syncthreads();
-        }
       }
     }
 
@@ -728,6 +670,282 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles, kKeyWaves)) vo
     if (++at.tile == seg.tiles()) {
       at.tile = 0;
       if (++at.head == kv_heads) {
+        at.head = 0;
+        ++at.item;
+      }
+    }
+  }
+}
+
+// A tile of many rows: 32 to a wave, and all of a workgroup's waves share the
+// tokens.  A stage of them (64; 32 for the longest heads) is widened once, a
+// sub-block's K or V by each wave, into LDS in operand order, two stages in turn.
+// The products are taken as 32x32x16: one such instruction leaves room for 6
+// vector instructions in its 32 cycles, two 16x16x32 for 2 each, and the softmax
+// has about as many cycles as the products.  8 waves on a stage: with 4 each wave
+// widens twice as much (2.13 ms instead of 2.04 for 16 chunks of 512 tokens, 64
+// heads, contexts of 7 k).  At 32 rows a wave, operands cross from LDS at 128 bytes
+// in a product's cycles, all that LDS gives: products, LDS and softmax
+// take about 1.0, 0.9 and 0.9 ms of those 2.04 and overlap in part.
+constexpr int stage_tokens(int dim) { return dim == 256 ? 32 : 64; }
+constexpr int tile_waves(int dim) { return 2 * stage_tokens(dim) / 16; }
+constexpr int tile_rows(int dim) { return 32 * tile_waves(dim); }
+template <int kType, int kDim, bool kCap>
+__global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void tile_kernel(Attention a) {
+  typedef El<kType> E;
+  typedef typename E::v8 v8;
+  constexpr int kSlices = kDim / 64, kOut = kDim / 32, kTW = tile_waves(kDim);
+  constexpr int kStage = stage_tokens(kDim), kSubs = kStage / 16, kHalves = kStage / 32;
+  constexpr int kSide = kStage * kDim * 2;  // bytes of a stage's K or V operands
+  extern __shared__ __align__(16) char lds[];
+  __shared__ unsigned long long scan[2 * kTW];
+  long long *before = reinterpret_cast<long long *>(lds);
+  int *ids = reinterpret_cast<int *>(before + a.batch.n + 1);
+  char *const stages = lds + list_bytes(a.batch.n);
+  const int lane = lane_id(), n32 = lane & 31, hg = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(wave_id());
+  Range range;
+  if (!range.find<kTW>(a, before, ids, scan)) return;
+  Place at = range.begin;
+  const Place end = uniform(range.end);
+  const int items = __builtin_amdgcn_readfirstlane(range.items), w = __builtin_amdgcn_readfirstlane(range.group);
+
+  while (at.item < items) {
+    at = uniform(at);  // the compiler does not see that it is
+    const int id = __builtin_amdgcn_readfirstlane(ids[at.item]);
+    const KvRequest req = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, id);
+    const Segments seg(req, a.tile_tokens);
+    const int length = (int)seg.length(at.tile);
+    const bool last = end.item == at.item && end.head == at.head && end.tile == at.tile;
+    const int stop = last ? end.key : length;
+    if (last && stop == at.key) break;
+
+    // the lane's row: 32 wave + lane % 32 of the tile
+    const int row = 32 * wave + n32, shown = req.len - req.count;
+    const int token = at.tile * a.tile_tokens + row / a.group, head = at.head * a.group + row % a.group;
+    const bool valid = row < a.tile_tokens * a.group && token < req.count;
+    const int limit = valid ? shown + token : -1;  // last cached token that it sees
+    v8 q[kDim / 16];
+    const char *from_q = a.q.data + (int64_t)(req.first + (valid ? token : 0)) * a.q.token_stride +
+                         (valid ? head : 0) * a.q.head_stride + 16 * hg;
+#pragma unroll
+    for (int d = 0; d < kDim / 16; ++d) {
+      u4 x = *reinterpret_cast<const u4 *>(from_q + 32 * d);
+      if (!valid) x = u4{0, 0, 0, 0};
+      q[d] = __builtin_bit_cast(v8, (x & a.keep) ^ a.flip);
+    }
+    const int64_t log_row = (int64_t)a.window * a.q_heads;
+    float *log_at = nullptr;  // the row's place in the log sums of sub-block 0
+    const int back = req.count - 1 - token;
+    if (a.logs && valid && back < a.window)
+      log_at = a.logs + ((int64_t)req.row << (a.kv.block_shift - 4)) * log_row + (int64_t)back * a.q_heads + head;
+    const bool logs = __any(log_at != nullptr);
+    // every row of the wave sees the tokens before clear_end, no row of the tile those from block_end on
+    const int clear_end = __builtin_amdgcn_readfirstlane(shown + at.tile * a.tile_tokens + 32 * wave / a.group + 1);
+    const int block_end = __builtin_amdgcn_readfirstlane(
+        min(stop, min(req.len, shown + min((at.tile + 1) * a.tile_tokens, req.count))));
+    const int first_key = __builtin_amdgcn_readfirstlane(at.key), len = __builtin_amdgcn_readfirstlane(req.len);
+
+    f16v o[kOut];
+#pragma unroll
+    for (int d = 0; d < kOut; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+    float m = kLowest, sum = 0.f;
+    if (first_key < block_end) {
+      // a wave carries one sub-block's K or V, a stage ahead.  Slots and scales by vector
+      // loads, whose waits count in order (a wait for scalar loads waits for all
+      // and for LDS), and no load hangs on a condition (a value that arrives on
+      // one way only is waited for where the ways meet): past the end the
+      // last sub-block is read again.
+      const Cache<kDim> cache(a, req, at.head);
+      u4 own[kSlices];
+      float own_scale;
+      int own_key = 0, slot;
+      bool bad = false;
+      const int sub = wave % kSubs, side = wave / kSubs;
+      const char *const lane_codes = cache.base + side * cache.kv_stride + (side ? v_place() : k_place());
+      const char *const lane_scale = cache.base + side * cache.kv_stride + cache.scales;
+      auto look = [&](int key) { slot = vector_load(cache.slots + cache.entry((key >> 4) + sub)); };
+      auto fetch = [&](int key) {
+        const int64_t from = cache.offset(slot, bad), codes = from + cache.place((key >> 4) + sub);
+        own_key = key + 16 * sub;
+#pragma unroll
+        for (int c = 0; c < kSlices; ++c) own[c] = *reinterpret_cast<const u4 *>(lane_codes + codes + 1024 * c);
+        own_scale = *reinterpret_cast<const float *>(lane_scale + from);
+        look(key + kStage);
+      };
+      // of 32 tokens (a half): K operand [16 dims][lane], lane = token + 32 * (which 8
+      // of them); V operand [16 tokens][32 dims][lane], lane = dim + 32 * hg, of tokens
+      // 4 hg + 0..3 and 8 + 4 hg + 0..3
+      constexpr int kHalf = 32 * kDim * 2;
+      const int own_place = (sub >> 1) * kHalf + (side ? kSide + ((sub & 1) * kOut * 64 + 32 * (lane >> 4 & 1) + (lane & 15)) * 16 + 8 * (lane >> 5)
+                                                      : ((lane >> 4) * 64 + 16 * (sub & 1) + (lane & 15)) * 16);
+      auto put = [&](char *to) {
+        to += own_place;
+        if (side == 0) {
+#pragma unroll
+          for (int c = 0; c < kSlices; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              *reinterpret_cast<v8 *>(to + (4 * c * 64 + 32 * h) * 16) =
+                  widen8<kType>(own[c][2 * h], own[c][2 * h + 1], own_scale, own_scale);
+        } else {
+          if (own_key + 16 > len) {  // codes past the end may be anything
+            const unsigned live = live_bytes(own_key + 4 * (lane >> 4), len);
+#pragma unroll
+            for (int c = 0; c < kSlices; ++c) own[c] &= live;
+          }
+#pragma unroll
+          for (int c = 0; c < kSlices; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              *reinterpret_cast<u2 *>(to + ((2 * c + (j >> 1)) * 64 + 16 * (j & 1)) * 16) =
+                  u2{E::widen_lo(own[c][j], own_scale), E::widen_hi(own[c][j], own_scale)};
+        }
+      };
+      v8 kop[kDim / 16], vop[2][kOut];
+      auto load_k = [&](const char *from, int h) {
+#pragma unroll
+        for (int d = 0; d < kDim / 16; ++d)
+          kop[d] = *reinterpret_cast<const v8 *>(from + h * kHalf + (d * 64 + lane) * 16);
+      };
+      auto load_v = [&](const char *from, int h) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int d = 0; d < kOut; ++d)
+            vop[u][d] = *reinterpret_cast<const v8 *>(from + kSide + h * kHalf + ((u * kOut + d) * 64 + lane) * 16);
+      };
+      auto scores = [&](f16v &x) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = 0.f;
+#pragma unroll
+        for (int d = 0; d < kDim / 16; ++d) x = E::mfma(kop[d], q[d], x);
+      };
+      // score i of a lane is token key + 8 * (i / 4) + 4 * hg + i % 4
+      auto limits = [&](f16v &x, int key) {
+        if (kCap) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)  // tanh(x) = 1 - 2 / (exp(2 x) + 1)
+            x[i] = 1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x[i] * a.cap_in) + 1.f);
+        }
+        if (key + 32 > clear_end) {
+          const int seen = limit - key - 4 * hg;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[i] = 8 * (i >> 2) + (i & 3) <= seen ? x[i] : -__builtin_inff();
+        }
+      };
+      auto raise = [&](const f16v (&x)[kHalves]) {
+        float part[4];
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) part[i & 3] = h + i < 4 && h == 0 ? x[h][i] : fmaxf(part[i & 3], x[h][i]);
+        float top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) * a.scale;
+        if (__any(top > m + kSlack)) {
+          top = fmaxf(top, __shfl_xor(top, 32));
+          const float now = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - now);
+          m = now;
+          sum *= f;
+#pragma unroll
+          for (int d = 0; d < kOut; ++d) o[d] *= f;
+        }
+      };
+      auto weigh = [&](f16v &x, v8 (&p)[2], int key) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale, -m));
+        float part[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          part[u] = ((x[8 * u] + x[8 * u + 1]) + (x[8 * u + 2] + x[8 * u + 3])) +
+                    ((x[8 * u + 4] + x[8 * u + 5]) + (x[8 * u + 6] + x[8 * u + 7]));
+          const u4 b = {narrow2<kType>(x[8 * u], x[8 * u + 1]), narrow2<kType>(x[8 * u + 2], x[8 * u + 3]),
+                        narrow2<kType>(x[8 * u + 4], x[8 * u + 5]), narrow2<kType>(x[8 * u + 6], x[8 * u + 7])};
+          p[u] = __builtin_bit_cast(v8, b);
+        }
+        sum += part[0] + part[1];
+        if (logs) {
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const float all = part[u] + __shfl_xor(part[u], 32);
+            if (hg == 0 && log_at && key + 16 * u < len)
+              log_at[(int64_t)((key >> 4) + u) * log_row] = __builtin_amdgcn_logf(all) + m;
+          }
+        }
+      };
+      auto add = [&](const v8 (&p)[2]) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int d = 0; d < kOut; ++d) o[d] = E::mfma(vop[u][d], p[u], o[d]);
+      };
+      char *from = stages, *to = stages + 2 * kSide;
+      look(first_key);
+      fetch(first_key);
+      put(from);
+      fetch(first_key + kStage);
+      __syncthreads();
+      for (int key = first_key; key < block_end; key += kStage) {
+        f16v x[kHalves];
+        v8 p[kHalves][2];
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) {
+          load_k(from, h);
+          scores(x[h]);
+        }
+        load_v(from, 0);
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) limits(x[h], key + 32 * h);
+        raise(x);
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) weigh(x[h], p[h], key + 32 * h);
+        put(to);
+        fetch(key + 2 * kStage);
+        add(p[0]);
+        if (kHalves > 1) {
+          load_v(from, kHalves - 1);
+          add(p[kHalves - 1]);
+        }
+        __syncthreads();
+        char *const was = from;
+        from = to;
+        to = was;
+      }
+      if (__any(bad)) kv_report(a.status);
+      __syncthreads();
+    }
+
+    sum += __shfl_xor(sum, 32);
+    if (valid && at.key == 0 && stop == length) {
+      const float f = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
+      char *out = a.out.data + (int64_t)(req.first + token) * a.out.token_stride + head * a.out.head_stride + 8 * hg;
+#pragma unroll
+      for (int d = 0; d < kOut; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          *reinterpret_cast<u2 *>(out + 64 * d + 16 * j) =
+              u2{narrow2<kType>(o[d][4 * j] * f, o[d][4 * j + 1] * f),
+                 narrow2<kType>(o[d][4 * j + 2] * f, o[d][4 * j + 3] * f)};
+      if (a.lse && hg == 0)
+        a.lse[(int64_t)(req.first + token) * a.q_heads + head] = (m + __builtin_amdgcn_logf(sum)) * kLn2;
+    } else if (valid) {
+      const int64_t part = ((int64_t)w * 2 + (at.key > 0 ? 0 : 1)) * tile_rows(kDim) + row;
+      float *to = a.parts + part * kDim + 4 * hg;
+#pragma unroll
+      for (int d = 0; d < kOut; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          *reinterpret_cast<f4 *>(to + 32 * d + 8 * j) =
+              f4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
+      if (hg == 0) *reinterpret_cast<f2 *>(a.part_sums + 2 * part) = f2{m, sum};
+    }
+
+    if (last) break;
+    at.key = 0;
+    if (++at.tile == seg.tiles()) {
+      at.tile = 0;
+      if (++at.head == a.kv.kv_heads) {
         at.head = 0;
         ++at.item;
       }
@@ -816,8 +1034,7 @@ __global__ __launch_bounds__(kBlock) void weight_kernel(Attention a, float *bloc
 // ------------------------------------------------------------------- host
 
 constexpr int kGroups = 1024;      // workgroups of the kernel that splits tokens over waves
-constexpr int kTileGroups = 512;   // of the kernel that splits rows over waves
-constexpr int kTileRows = 128;     // its row tile
+constexpr int kTileGroups = 256;   // of the kernel that splits rows over waves: one to a CU
 constexpr int most_rows(int dim) { return dim == 256 ? 32 : 64; }  // of a request in the former
 
 struct Workspace {
@@ -837,9 +1054,9 @@ Workspace layout(const cascade_kv_format_t *f, const cascade_kv_batch_t *b, int 
   w.splits = take(sizeof(Split) * kGroups);
   w.tile_splits = take(sizeof(Split) * kTileGroups);
   w.parts = take(sizeof(float) * kGroups * 2 * most_rows(f->head_dim) * f->head_dim);
-  w.tile_parts = take(sizeof(float) * kTileGroups * 2 * kTileRows * f->head_dim);
+  w.tile_parts = take(sizeof(float) * kTileGroups * 2 * tile_rows(f->head_dim) * f->head_dim);
   w.sums = take(sizeof(float) * kGroups * 2 * most_rows(f->head_dim) * 2);
-  w.tile_sums = take(sizeof(float) * kTileGroups * 2 * kTileRows * 2);
+  w.tile_sums = take(sizeof(float) * kTileGroups * 2 * tile_rows(f->head_dim) * 2);
   w.lse = take(window ? sizeof(float) * b->n_tokens * q_heads : 0);
   w.logs = take(window ? sizeof(float) * b->n_entries * (f->block_tokens / 16) * window * q_heads : 0);
   w.total = at;
@@ -850,14 +1067,18 @@ bool heads_ok(const cascade_kv_format_t *f, int q_heads) {
   return q_heads >= 1 && q_heads % f->kv_heads == 0 && q_heads / f->kv_heads <= 128;
 }
 
-template <int kType, int kDim, int kTiles, int kKeyWaves>
+template <int kType, int kDim, int kTiles>
 void start(const Attention &a, int grid, bool cap, hipStream_t stream) {
-  // combination of the waves, or two stages of operands
-  const size_t mix = kKeyWaves > 1 ? sizeof(float) * kWaves * 16 * (2 + (kDim < 128 ? kDim : 128) + 4)
-                                   : 2 * stage_tokens(kDim) * 4 * kDim;
-  auto kernel = cap ? attention_kernel<kType, kDim, kTiles, kKeyWaves, true>
-                    : attention_kernel<kType, kDim, kTiles, kKeyWaves, false>;
+  const size_t mix = sizeof(float) * kWaves * 16 * (2 + (kDim < 128 ? kDim : 128) + 4);
+  auto kernel = cap ? attention_kernel<kType, kDim, kTiles, true> : attention_kernel<kType, kDim, kTiles, false>;
   hipLaunchKernelGGL(kernel, dim3(grid), dim3(kBlock), list_bytes(a.batch.n) + mix, stream, a);
+}
+
+template <int kType, int kDim>
+void start_tiles(const Attention &a, bool cap, hipStream_t stream) {
+  auto kernel = cap ? tile_kernel<kType, kDim, true> : tile_kernel<kType, kDim, false>;
+  hipLaunchKernelGGL(kernel, dim3(kTileGroups), dim3(64 * tile_waves(kDim)),
+                     list_bytes(a.batch.n) + 2 * stage_tokens(kDim) * kDim * 4, stream, a);
 }
 
 template <int kType, int kDim>
@@ -880,26 +1101,26 @@ int run(Attention a, char *ws, const Workspace &w, bool cap, float *block_weight
   int64_t grid = keys / a.range_keys;
   grid = grid < 8 ? 8 : grid > kGroups ? kGroups : grid;
   if (small == 16)
-    start<kType, kDim, 1, 4>(a, (int)grid, cap, s);
+    start<kType, kDim, 1>(a, (int)grid, cap, s);
   else if (small == 32)
-    start<kType, kDim, 2, 4>(a, (int)grid, cap, s);
+    start<kType, kDim, 2>(a, (int)grid, cap, s);
   else if constexpr (kDim < 256)
-    start<kType, kDim, 4, 4>(a, (int)grid, cap, s);
+    start<kType, kDim, 4>(a, (int)grid, cap, s);
   hipLaunchKernelGGL((join_kernel<kType, kDim>), dim3((int)grid, small / kWaves), dim3(kBlock), 0, s, a,
                      small);
   if (tiled) {
     a.min_rows = small;
     a.max_rows = INT64_MAX;
-    a.tile_tokens = kTileRows / a.group;
+    a.tile_tokens = tile_rows(kDim) / a.group;
     a.atomic_keys = 2048;
     a.cut_keys = stage_tokens(kDim);
     a.range_keys = 256;
     a.splits = reinterpret_cast<Split *>(ws + w.tile_splits);
     a.parts = reinterpret_cast<float *>(ws + w.tile_parts);
     a.part_sums = reinterpret_cast<float *>(ws + w.tile_sums);
-    start<kType, kDim, 2, 1>(a, kTileGroups, cap, s);
-    hipLaunchKernelGGL((join_kernel<kType, kDim>), dim3(kTileGroups, kTileRows / kWaves), dim3(kBlock), 0,
-                       s, a, kTileRows);
+    start_tiles<kType, kDim>(a, cap, s);
+    hipLaunchKernelGGL((join_kernel<kType, kDim>), dim3(kTileGroups, tile_rows(kDim) / kWaves), dim3(kBlock), 0,
+                       s, a, tile_rows(kDim));
   }
   if (block_weight)
     hipLaunchKernelGGL(weight_kernel, dim3((a.batch.n_entries + kEntries - 1) / kEntries), dim3(kBlock), 0,

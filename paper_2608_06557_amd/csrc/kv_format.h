@@ -75,6 +75,15 @@ __device__ __forceinline__ T uniform_load(const T *p) {
   return *(const __attribute__((address_space(4))) T *)(p);
 }
 
+// The same through the vector unit: a register the compiler knows nothing of
+// makes the address look different in every lane.
+template <typename T>
+__device__ __forceinline__ T vector_load(const T *p) {
+  int none;
+  asm("v_mov_b32 %0, 0" : "=v"(none));
+  return p[none];
+}
+
 // A request of a batch, checked against the arrays it points into.
 struct KvRequest {
   int first, count;  // new tokens: rows first .. first + count
