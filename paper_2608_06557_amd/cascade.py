@@ -378,6 +378,21 @@ def _ref(s):
     return None if s is None else C.byref(s)
 
 
+def kv_call(name: str, *args):
+    """A call of the 8-bit KV cache with its arguments converted once:
+    the returned function takes the stream and gives the return code.
+    Structures go by reference, so later changes of theirs are seen."""
+    f = getattr(_kv(), name)
+
+    def fixed(value, kind):
+        if isinstance(value, C.Structure):
+            return C.byref(value)
+        return None if value is None else kind(value)
+
+    given = tuple(fixed(value, kind) for value, kind in zip(args, f.argtypes))
+    return lambda stream: f(*given, stream)
+
+
 def cascade_kv_chunk_bytes(fmt: KvFormat) -> int:
     return int(_kv().cascade_kv_chunk_bytes(C.byref(fmt)))
 

@@ -25,6 +25,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "cascade.h"
@@ -420,12 +421,13 @@ struct Cache {
   int64_t kv_stride, slot_stride, scales;  // `scales`: from the codes to the head's scale
   const int32_t *slots;
   int num_slots, shift, last;  // log2 of sub-blocks a block, last sub-block
-  __device__ __forceinline__ Cache(const Attention &a, const KvRequest &r, int head)
+  // of the tokens before `end`, a request's length at most
+  __device__ __forceinline__ Cache(const Attention &a, const KvRequest &r, int head, int end)
       : base(a.kv.base + ((int64_t)head << a.kv.block_shift) * kDim), kv_stride(a.kv.kv_stride),
         slot_stride(a.kv.slot_stride),
         scales(((int64_t)(a.kv.kv_heads - head) << a.kv.block_shift) * kDim + 4 * head),
         slots(a.slots + r.row), num_slots(a.kv.num_slots), shift(a.kv.block_shift - 4),
-        last((r.len - 1) >> 4) {}
+        last((end - 1) >> 4) {}
   // table entry and slot of sub-block `sub`, or of the last one
   __device__ __forceinline__ int entry(int sub) const { return min(sub, last) >> shift; }
   __device__ __forceinline__ int slot(int sub) const { return uniform_load(slots + entry(sub)); }
@@ -558,11 +560,15 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
     // every row sees the tokens before clear_end, none those from key_end on
     const int first_token = at.tile * a.tile_tokens;
     const int last_token = min(first_token + a.tile_tokens, req.count) - 1;
-    const int clear_end = shown + first_token + 1, key_end = min(min(stop, req.len), shown + last_token + 1);
-    const Cache<kDim> cache(a, req, at.head);
-    // each wave takes every fourth 32 tokens, straight into registers:
-    // the next K codes leave when these have been taken, V codes likewise,
-    // and the slots are known a step ahead of them
+    const int clear_end = __builtin_amdgcn_readfirstlane(shown + first_token + 1);
+    const int key_end = __builtin_amdgcn_readfirstlane(min(min(stop, req.len), shown + last_token + 1));
+    const int len = __builtin_amdgcn_readfirstlane(req.len);
+    const Cache<kDim> cache(a, req, at.head, key_end);
+    // each wave takes every fourth 32 tokens, straight into registers: the next K
+    // codes are requested when these have been taken, V codes likewise, and the
+    // slots are known a step ahead of them.  No load hangs on a condition (a wait
+    // after the ways meet again would wait for too much): past the end the last
+    // sub-block is read again, from a cache.
     constexpr int kStride = 32 * kWaves;
     int key = __builtin_amdgcn_readfirstlane(at.key + 32 * wave);
     if (key < key_end) {
@@ -574,12 +580,13 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
       };
       look(key);
       c.fetch_k(cache, slot, key);
+      // K before V, as in the loop: waits count the loads that follow
+      __builtin_amdgcn_sched_barrier(0);
       c.fetch_v(cache, slot, key);
       look(key + kStride);
       while (true) {
-        const int next = key + kStride;
-        if (key + 32 > req.len) {
-          const unsigned live[2] = {live_bytes(key + 4 * g, req.len), live_bytes(key + 16 + 4 * g, req.len)};
+        if (key + 32 > len) {
+          const unsigned live[2] = {live_bytes(key + 4 * g, len), live_bytes(key + 16 + 4 * g, len)};
 #pragma unroll
           for (int i = 0; i < kDim / 64; ++i)
 #pragma unroll
@@ -592,18 +599,18 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
               return widen8<kType>(w[2 * (d & 1)], w[2 * (d & 1) + 1], c.ks[b], c.ks[b]);
             },
             x);
-        if (next < key_end) c.fetch_k(cache, slot, next);
+        c.fetch_k(cache, slot, key + kStride);
         v8 p[kTiles][1];
-        r.template weights<2>(a, x, p, key, req.len, key + 32 > clear_end, logs, log_row);
+        r.template weights<2>(a, x, p, key, len, key + 32 > clear_end, logs, log_row);
         r.add(
             [&](int d) {
               return widen8<kType>(c.v[0][d >> 2][d & 3], c.v[1][d >> 2][d & 3], c.vs[0], c.vs[1]);
             },
             p);
-        if (next >= key_end) break;
-        c.fetch_v(cache, slot, next);
-        look(next + kStride);
-        key = next;
+        c.fetch_v(cache, slot, key + kStride);
+        look(key + 2 * kStride);
+        key += kStride;
+        if (key >= key_end) break;
       }
       if (c.bad) kv_report(a.status);
     }
@@ -758,7 +765,7 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
       // and for LDS), and no load hangs on a condition (a value that arrives on
       // one way only is waited for where the ways meet): past the end the
       // last sub-block is read again.
-      const Cache<kDim> cache(a, req, at.head);
+      const Cache<kDim> cache(a, req, at.head, block_end);
       u4 own[kSlices];
       float own_scale;
       int own_key = 0, slot;
@@ -953,88 +960,97 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
   }
 }
 
-// Joins the parts of cut segments: one wave per row.
+// Joins the parts of cut segments: a wave takes `each` rows, one after another.
 template <int kType, int kDim>
-__global__ __launch_bounds__(kBlock) void join_kernel(Attention a, int rows) {
+__global__ __launch_bounds__(kBlock) void join_kernel(Attention a, int rows, int each) {
   constexpr int kLanes = kDim / 4, kParts = 64 / kLanes;
   const Split s = a.splits[blockIdx.x];
   if (s.request < 0) return;
-  const int row = __builtin_amdgcn_readfirstlane((int)blockIdx.y * kWaves + wave_id()), lane = lane_id();
+  const int lane = lane_id();
+  const int row0 = __builtin_amdgcn_readfirstlane(((int)blockIdx.y * kWaves + wave_id()) * each);
   const KvRequest req = kv_request(a.batch, a.row_offsets, a.kv.block_shift, s.request);
-  const int token = s.tile * a.tile_tokens + row / a.group;
-  if (row >= a.tile_tokens * a.group || token >= req.count) return;
-  const int head = s.head * a.group + row % a.group;
   // part 0 ends the range of the workgroup before the cut, the others begin theirs
   const int w = blockIdx.x, parts = s.last - w + 2;
-  auto place = [&](int p) { return ((int64_t)(w - 1 + p) * 2 + (p == 0)) * rows + row; };
-  float top = kLowest;
-  for (int p = lane; p < parts; p += 64) top = fmaxf(top, a.part_sums[2 * place(p)]);
+  for (int row = row0; row < row0 + each; ++row) {
+    const int token = s.tile * a.tile_tokens + row / a.group;
+    if (row >= a.tile_tokens * a.group || token >= req.count) return;
+    const int head = s.head * a.group + row % a.group;
+    auto place = [&](int p) { return ((int64_t)(w - 1 + p) * 2 + (p == 0)) * rows + row; };
+    float top = kLowest;
+    for (int p = lane; p < parts; p += 64) top = fmaxf(top, a.part_sums[2 * place(p)]);
 #pragma unroll
-  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  float sum = 0.f;
-  for (int p = lane; p < parts; p += 64) {
-    const f2 ms = *reinterpret_cast<const f2 *>(a.part_sums + 2 * place(p));
-    sum += ms[1] * __builtin_amdgcn_exp2f(ms[0] - top);
-  }
+    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    float sum = 0.f;
+    for (int p = lane; p < parts; p += 64) {
+      const f2 ms = *reinterpret_cast<const f2 *>(a.part_sums + 2 * place(p));
+      sum += ms[1] * __builtin_amdgcn_exp2f(ms[0] - top);
+    }
 #pragma unroll
-  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-  f4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+    f4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-  for (int p = lane / kLanes; p < parts; p += kParts) {
-    const float f = __builtin_amdgcn_exp2f(a.part_sums[2 * place(p)] - top);
-    o += *reinterpret_cast<const f4 *>(a.parts + place(p) * kDim + 4 * (lane % kLanes)) * f;
-  }
+    for (int p = lane / kLanes; p < parts; p += kParts) {
+      const float f = __builtin_amdgcn_exp2f(a.part_sums[2 * place(p)] - top);
+      o += *reinterpret_cast<const f4 *>(a.parts + place(p) * kDim + 4 * (lane % kLanes)) * f;
+    }
 #pragma unroll
-  for (int d = 32; d >= kLanes; d >>= 1)
+    for (int d = 32; d >= kLanes; d >>= 1)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], d);
-  if (lane < kLanes) {
-    const float f = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
-    const u2 x = {narrow2<kType>(o[0] * f, o[1] * f), narrow2<kType>(o[2] * f, o[3] * f)};
-    *reinterpret_cast<u2 *>(a.out.data + (int64_t)(req.first + token) * a.out.token_stride +
-                            head * a.out.head_stride + 8 * lane) = x;
+      for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], d);
+    if (lane < kLanes) {
+      const float f = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
+      const u2 x = {narrow2<kType>(o[0] * f, o[1] * f), narrow2<kType>(o[2] * f, o[3] * f)};
+      *reinterpret_cast<u2 *>(a.out.data + (int64_t)(req.first + token) * a.out.token_stride +
+                              head * a.out.head_stride + 8 * lane) = x;
+    }
+    if (a.lse && lane == 0)
+      a.lse[(int64_t)(req.first + token) * a.q_heads + head] = (top + __builtin_amdgcn_logf(sum)) * kLn2;
   }
-  if (a.lse && lane == 0)
-    a.lse[(int64_t)(req.first + token) * a.q_heads + head] = (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 // Adds to each table entry the weight that its request's last tokens gave it:
 // one wave per entry, its sub-blocks' log sums against the rows' totals.
-constexpr int kEntries = 4 * kWaves;  // entries of one workgroup
 __global__ __launch_bounds__(kBlock) void weight_kernel(Attention a, float *block_weight) {
   __shared__ unsigned sums[kWaves];
-  const int e0 = blockIdx.x * kEntries, lane = lane_id(), subs = a.kv.block_shift - 4;
+  const int e0 = blockIdx.x * kWaves, lane = lane_id(), subs = a.kv.block_shift - 4;
   unsigned ended[1] = {0};
   for (int i = threadIdx.x; i < a.batch.n; i += kBlock) ended[0] += a.row_offsets[i + 1] <= e0;
   block_sum<1, unsigned>(ended, sums);
   int i = __builtin_amdgcn_readfirstlane((int)ended[0]);
-  for (int e = e0 + wave_id(); e < min(e0 + kEntries, a.batch.n_entries); e += kWaves) {
-    while (i < a.batch.n && a.row_offsets[i + 1] <= e) ++i;
-    if (i >= a.batch.n) return;
-    const KvRequest r = kv_request(a.batch, a.row_offsets, a.kv.block_shift, i);
-    if (!r.ok || e < r.row || (int64_t)(e - r.row) << (subs + 4) >= r.len || r.count == 0) continue;
-    const int rows = min(a.window, r.count) * a.q_heads;
-    float sum = 0.f;
-    for (int s = 0; s < 1 << subs; ++s) {
-      const int first = (((e - r.row) << subs) + s) << 4;  // the sub-block's first token
-      const float *log = a.logs + (((int64_t)e << subs) + s) * a.window * a.q_heads;
-      for (int j = lane; j < rows; j += 64) {
-        const int back = j / a.q_heads;
-        if (first > r.len - 1 - back) continue;  // not seen
-        const float lse = a.lse[(int64_t)(r.first + r.count - 1 - back) * a.q_heads + j % a.q_heads];
-        sum += __builtin_amdgcn_exp2f(log[j] - lse * kLog2e);
-      }
+  const int e = __builtin_amdgcn_readfirstlane(e0 + wave_id());
+  while (i < a.batch.n && uniform_load(a.row_offsets + i + 1) <= e) ++i;
+  if (i >= a.batch.n || e >= a.batch.n_entries) return;
+  const KvRequest r = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, i);
+  if (!r.ok || e < r.row || (int64_t)(e - r.row) << (subs + 4) >= r.len || r.count == 0) return;
+  const int rows = min(a.window, r.count) * a.q_heads;
+  // row j: query head j % q_heads of the token j / q_heads before the last
+  const float *lse = a.lse + (int64_t)(r.first + r.count - 1) * a.q_heads;
+  const float old = block_weight[e];
+  float sum = 0.f;
+  for (int s = 0; s < 1 << subs; ++s) {
+    const int first = (((e - r.row) << subs) + s) << 4;  // the sub-block's first token
+    // tokens more than `behind` back do not see it, and left no log sum
+    const int behind = r.len - 1 - first;
+    if (behind < 0) break;
+    const int seen = (int)min((int64_t)rows, (int64_t)(behind + 1) * a.q_heads);
+    const float *log = a.logs + (((int64_t)e << subs) + s) * a.window * a.q_heads;
+    int back = lane / a.q_heads, head = lane - back * a.q_heads;
+#pragma unroll 4
+    for (int j = lane; j < seen; j += 64) {
+      sum += __builtin_amdgcn_exp2f(log[j] - lse[head - back * a.q_heads] * kLog2e);
+      for (head += 64; head >= a.q_heads; head -= a.q_heads) ++back;
     }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-    if (lane == 0) block_weight[e] += sum;
   }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+  if (lane == 0) block_weight[e] = old + sum;
 }
 
 // ------------------------------------------------------------------- host
 
-constexpr int kGroups = 1024;      // workgroups of the kernel that splits tokens over waves
-constexpr int kTileGroups = 256;   // of the kernel that splits rows over waves: one to a CU
+constexpr int kCUs = 256;
+constexpr int kGroups = 4 * kCUs;      // workgroups of the kernel that splits tokens over waves
+constexpr int kTileGroups = kCUs;   // of the kernel that splits rows over waves: one to a CU
 constexpr int most_rows(int dim) { return dim == 256 ? 32 : 64; }  // of a request in the former
 
 struct Workspace {
@@ -1085,31 +1101,35 @@ template <int kType, int kDim>
 int run(Attention a, char *ws, const Workspace &w, bool cap, float *block_weight, hipStream_t s) {
   const int64_t most = (int64_t)a.batch.max_new * a.group;  // rows of a request and KV head
   const int64_t keys = ((int64_t)a.batch.n_entries << a.kv.block_shift) * a.kv.kv_heads;
-  // few rows: 4 waves share a tile's tokens.  More: row tiles of 128,
-  // and requests of up to 32 rows beside them in the first kernel
+  // few rows: 4 waves share a tile's tokens.  More: row tiles, and requests of
+  // up to 32 rows beside them in the first kernel.
   const bool tiled = most > most_rows(kDim);
   const int small = most <= 16 ? 16 : most <= 32 || tiled ? 32 : 64;
-  a.min_rows = 0;
-  a.max_rows = small;
-  a.tile_tokens = small / a.group > 0 ? small / a.group : 1;
-  a.atomic_keys = 0;
-  a.cut_keys = 32;
-  a.range_keys = 256;
-  a.splits = reinterpret_cast<Split *>(ws + w.splits);
-  a.parts = reinterpret_cast<float *>(ws + w.parts);
-  a.part_sums = reinterpret_cast<float *>(ws + w.sums);
-  int64_t grid = keys / a.range_keys;
-  grid = grid < 8 ? 8 : grid > kGroups ? kGroups : grid;
-  if (small == 16)
-    start<kType, kDim, 1>(a, (int)grid, cap, s);
-  else if (small == 32)
-    start<kType, kDim, 2>(a, (int)grid, cap, s);
-  else if constexpr (kDim < 256)
-    start<kType, kDim, 4>(a, (int)grid, cap, s);
-  hipLaunchKernelGGL((join_kernel<kType, kDim>), dim3((int)grid, small / kWaves), dim3(kBlock), 0, s, a,
-                     small);
+  if (!tiled || a.batch.n > 1) {
+    a.min_rows = 0;
+    a.max_rows = small;
+    a.tile_tokens = small / a.group > 0 ? small / a.group : 1;
+    // up to 512 tokens a cut costs more than it evens out (128 requests of 582
+    // tokens on average, 64 heads: 57 us, with every cut made 64)
+    a.atomic_keys = 512;
+    a.cut_keys = 32;
+    a.range_keys = 256;
+    a.splits = reinterpret_cast<Split *>(ws + w.splits);
+    a.parts = reinterpret_cast<float *>(ws + w.parts);
+    a.part_sums = reinterpret_cast<float *>(ws + w.sums);
+    // as many workgroups as fit the GPU at once
+    const int64_t room = kCUs * waves_per_simd(kDim, small / 16);
+    const int grid = (int)std::min(std::min<int64_t>(kGroups, room), std::max<int64_t>(8, keys / a.range_keys));
+    if (small == 16)
+      start<kType, kDim, 1>(a, grid, cap, s);
+    else if (small == 32)
+      start<kType, kDim, 2>(a, grid, cap, s);
+    else if constexpr (kDim < 256)
+      start<kType, kDim, 4>(a, grid, cap, s);
+    hipLaunchKernelGGL((join_kernel<kType, kDim>), dim3(grid, small / kWaves), dim3(kBlock), 0, s, a, small, 1);
+  }
   if (tiled) {
-    a.min_rows = small;
+    a.min_rows = a.batch.n > 1 ? small : 0;
     a.max_rows = INT64_MAX;
     a.tile_tokens = tile_rows(kDim) / a.group;
     a.atomic_keys = 2048;
@@ -1119,11 +1139,11 @@ int run(Attention a, char *ws, const Workspace &w, bool cap, float *block_weight
     a.parts = reinterpret_cast<float *>(ws + w.tile_parts);
     a.part_sums = reinterpret_cast<float *>(ws + w.tile_sums);
     start_tiles<kType, kDim>(a, cap, s);
-    hipLaunchKernelGGL((join_kernel<kType, kDim>), dim3(kTileGroups, tile_rows(kDim) / kWaves), dim3(kBlock), 0,
-                       s, a, tile_rows(kDim));
+    hipLaunchKernelGGL((join_kernel<kType, kDim>), dim3(kTileGroups, tile_rows(kDim) / (2 * kWaves)), dim3(kBlock),
+                       0, s, a, tile_rows(kDim), 2);
   }
   if (block_weight)
-    hipLaunchKernelGGL(weight_kernel, dim3((a.batch.n_entries + kEntries - 1) / kEntries), dim3(kBlock), 0,
+    hipLaunchKernelGGL(weight_kernel, dim3((a.batch.n_entries + kWaves - 1) / kWaves), dim3(kBlock), 0,
                        s, a, block_weight);
   return hipGetLastError() == hipSuccess ? CASCADE_OK : CASCADE_EHIP;
 }

@@ -7,8 +7,9 @@
 // hand-over.  Which ones: the count-th least weight by a radix selection, 8
 // bits of the weights' ordered form a pass (histogram in LDS), then one pass
 // in index order that drops what lies below it and the first of the equal
-// ones.  The weights are a few bytes per 16 cached tokens and stay in the L2
-// between the passes; the call is bound by latency.
+// ones.  A thread keeps its weights (one, or 8 neighbours of a request of more than
+// 1024 blocks) in registers between the passes; the call is bound by latency (8192 blocks of each of 64 requests:
+// FIGURE).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -50,6 +51,110 @@ __device__ __forceinline__ unsigned ordered(float w) {
   return b >> 31 ? ~b : b | 0x80000000u;
 }
 
+// One request's blocks, kPer neighbours to a thread.
+template <int kPer>
+__device__ __forceinline__ void evict_blocks(const cascade_evict_t &a, const Counts &c, const float *weight,
+                                             const int32_t *slot, const unsigned long long (&before)[2],
+                                             unsigned *hist, unsigned *scan, unsigned *picked) {
+  const int tid = threadIdx.x;
+  // a thread's weights: kPer neighbours of the first kThreads * kPer blocks stay
+  // in registers, those of longer requests are read again in every pass
+  auto load = [&](int b0, float (&w)[kPer]) {
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) w[j] = b0 + j < c.blocks ? weight[b0 + j] : 0.f;
+  };
+  float first[kPer];
+  load(tid * kPer, first);
+
+  // the gone-th least: `key` once all digits are known, of which `equal` go
+  unsigned key = 0, equal = 0;
+  if (c.gone > 0) {
+    unsigned rank = c.gone - 1;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      if (tid < 256) hist[tid] = 0;
+      __syncthreads();
+      const unsigned high = shift == 24 ? 0u : ~0u << (shift + 8);
+      auto count = [&](int b0, const float (&w)[kPer]) {
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+          const unsigned k = ordered(w[j]);
+          if (b0 + j >= c.begin && b0 + j < c.end && ((k ^ key) & high) == 0)
+            atomicAdd(&hist[(k >> shift) & 255u], 1u);
+        }
+      };
+      count(tid * kPer, first);
+      for (int b0 = (kThreads + tid) * kPer; b0 < c.end; b0 += kThreads * kPer) {
+        float w[kPer];
+        load(b0, w);
+        count(b0, w);
+      }
+      __syncthreads();
+      if (tid < 64) {
+        unsigned h[4], sum = 0;
+        for (int d = 0; d < 4; ++d) sum += h[d] = hist[4 * tid + d];
+        unsigned at = wave_inclusive_sum(sum) - sum;
+        for (int d = 0; d < 4; ++d) {
+          if (rank >= at && rank < at + h[d]) {
+            picked[0] = key | (unsigned)(4 * tid + d) << shift;
+            picked[1] = rank - at;
+          }
+          at += h[d];
+        }
+      }
+      __syncthreads();
+      key = picked[0];
+      rank = picked[1];
+      __syncthreads();
+    }
+    equal = rank + 1;
+  }
+
+  unsigned base[2] = {0, 0};  // below the key, equal to it: among the blocks so far
+  for (int c0 = 0; c0 < c.blocks; c0 += kThreads * kPer) {
+    const int b0 = c0 + tid * kPer;
+    float w[kPer];
+    int32_t held[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      w[j] = first[j];
+      held[j] = b0 + j < c.blocks ? slot[b0 + j] : 0;
+    }
+    if (c0) load(b0, w);
+    unsigned v[2] = {0, 0}, total[2];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const bool can = c.gone > 0 && b0 + j >= c.begin && b0 + j < c.end;
+      v[0] += can && ordered(w[j]) < key;
+      v[1] += can && ordered(w[j]) == key;
+    }
+    block_exclusive_scan<2, unsigned, kEvictWaves>(v, total, scan);
+    unsigned less = base[0] + v[0], same = base[1] + v[1];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int b = b0 + j;
+      const bool can = c.gone > 0 && b >= c.begin && b < c.end;
+      const bool below = can && ordered(w[j]) < key, on = can && ordered(w[j]) == key;
+      const unsigned gone_before = less + min(same, equal);
+      if (b < c.blocks) {
+        if (below || (on && same < equal)) {
+          const unsigned long long at = before[1] + gone_before;
+          if (at < (unsigned long long)a.n_entries) a.freed[at] = held[j];
+        } else {
+          const unsigned long long at = before[0] + (b - gone_before);
+          if (at < (unsigned long long)a.n_entries) {
+            a.slots_out[at] = held[j];
+            a.weight_out[at] = w[j];
+          }
+        }
+      }
+      less += below;
+      same += on;
+    }
+    base[0] += total[0];
+    base[1] += total[1];
+  }
+}
+
 __global__ __launch_bounds__(kThreads) void evict_kernel(cascade_evict_t a,
                                                          const int32_t *row_offsets,
                                                          const int32_t *slots, int32_t *status) {
@@ -80,67 +185,10 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(cascade_evict_t a,
   if (!c.ok) return;
   const float *weight = a.block_weight + row_offsets[i];
   const int32_t *slot = slots + row_offsets[i];
-
-  // the gone-th least: `key` once all digits are known, of which `equal` go
-  unsigned key = 0, equal = 0;
-  if (c.gone > 0) {
-    unsigned rank = c.gone - 1;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
-      __syncthreads();
-      const unsigned high = shift == 24 ? 0u : ~0u << (shift + 8);
-      for (int b = c.begin + tid; b < c.end; b += kThreads) {
-        const unsigned k = ordered(weight[b]);
-        if (((k ^ key) & high) == 0) atomicAdd(&hist[(k >> shift) & 255u], 1u);
-      }
-      __syncthreads();
-      if (tid < 64) {
-        unsigned h[4], sum = 0;
-        for (int d = 0; d < 4; ++d) sum += h[d] = hist[4 * tid + d];
-        unsigned at = wave_inclusive_sum(sum) - sum;
-        for (int d = 0; d < 4; ++d) {
-          if (rank >= at && rank < at + h[d]) {
-            picked[0] = key | (unsigned)(4 * tid + d) << shift;
-            picked[1] = rank - at;
-          }
-          at += h[d];
-        }
-      }
-      __syncthreads();
-      key = picked[0];
-      rank = picked[1];
-      __syncthreads();
-    }
-    equal = rank + 1;
-  }
-
-  unsigned base[2] = {0, 0};  // below the key, equal to it: among the blocks so far
-  for (int b0 = 0; b0 < c.blocks; b0 += kThreads) {
-    const int b = b0 + tid;
-    const bool in = b < c.blocks, can = c.gone > 0 && b >= c.begin && b < c.end;
-    const float w = in ? weight[b] : 0.f;
-    const unsigned k = ordered(w);
-    unsigned v[2] = {can && k < key, can && k == key}, total[2];
-    const bool less = v[0], same = v[1];
-    block_exclusive_scan<2, unsigned, kEvictWaves>(v, total, scan);
-    const unsigned eq = base[1] + v[1];
-    const bool gone = less || (same && eq < equal);
-    const unsigned gone_before = base[0] + v[0] + min(eq, equal);
-    if (in) {
-      if (gone) {
-        const unsigned long long at = before[1] + gone_before;
-        if (at < (unsigned long long)a.n_entries) a.freed[at] = slot[b];
-      } else {
-        const unsigned long long at = before[0] + (b - gone_before);
-        if (at < (unsigned long long)a.n_entries) {
-          a.slots_out[at] = slot[b];
-          a.weight_out[at] = w;
-        }
-      }
-    }
-    base[0] += total[0];
-    base[1] += total[1];
-  }
+  if (c.blocks <= kThreads)
+    evict_blocks<1>(a, c, weight, slot, before, hist, scan, picked);
+  else
+    evict_blocks<8>(a, c, weight, slot, before, hist, scan, picked);
 }
 
 __global__ void evict_none_kernel(cascade_evict_t a) {

@@ -482,13 +482,12 @@ class DeviceKvAppend:
             self.c_rope = cx.Rope(2 * freq.numel(), int(interleaved),
                                   _check_array(freq, torch.int64, 0, "freq"), rope_scale)
             self.positions = _check_array(positions, torch.int32, batch.tokens, "positions")
+        self._call = cx.kv_call("cascade_kv_append", kv.c_pool, layer, kv.c_format, batch.c_batch,
+                                batch.c_table, self.dtype, self.q_heads, *self.c_rows,
+                                self.c_rope, self.positions, kv.status.data_ptr())
 
     def run(self, stream=None) -> None:
-        b = self.batch
-        _raise(cx.cascade_kv_append(self.kv.c_pool, self.layer, self.kv.c_format, b.c_batch,
-                                    b.c_table, self.dtype, self.q_heads, *self.c_rows,
-                                    self.c_rope, self.positions, self.kv.status.data_ptr(),
-                                    stream_handle(stream)))
+        _raise(self._call(stream_handle(stream)))
 
 
 class DeviceAttention:
@@ -523,12 +522,12 @@ class DeviceAttention:
         self.workspace = workspace
         self.ws_ptr = (workspace.data_ptr() + 255) & ~255
         self.ws_bytes = workspace.data_ptr() + workspace.numel() - self.ws_ptr
+        self._call = cx.kv_call("cascade_attention", kv.c_pool, layer, kv.c_format, batch.c_batch,
+                                batch.c_table, self.c_args, self.ws_ptr, self.ws_bytes,
+                                kv.status.data_ptr())
 
     def run(self, stream=None) -> None:
-        b = self.batch
-        _raise(cx.cascade_attention(self.kv.c_pool, self.layer, self.kv.c_format, b.c_batch,
-                                    b.c_table, self.c_args, self.ws_ptr, self.ws_bytes,
-                                    self.kv.status.data_ptr(), stream_handle(stream)))
+        _raise(self._call(stream_handle(stream)))
 
 
 class DeviceKvEvict:
@@ -559,7 +558,8 @@ class DeviceKvEvict:
             p(out[0], i32, n, "kv_len_out"), p(out[1], i32, n + 1, "row_offsets_out"),
             p(out[2], i32, entries, "slots_out"), p(out[3], torch.float32, entries, "weight_out"),
             p(out[4], i32, entries, "freed"), p(out[5], i32, 1, "n_freed"))
+        self._call = cx.kv_call("cascade_kv_evict", self.c_table, self.c_args,
+                                self.status.data_ptr())
 
     def run(self, stream=None) -> None:
-        _raise(cx.cascade_kv_evict(self.c_table, self.c_args, self.status.data_ptr(),
-                                   stream_handle(stream)))
+        _raise(self._call(stream_handle(stream)))
