@@ -120,6 +120,7 @@ struct Attention {
   int64_t min_rows, max_rows;  // requests with min_rows < rows <= max_rows are taken
   int tile_tokens;         // tokens of one row tile
   int atomic_keys;         // segments up to this long are not cut
+  int fixed_keys;          // what a segment costs besides its tokens, in tokens
   int cut_keys;            // cuts are at multiples of this power of two, the tokens of a step
   int range_keys;          // least tokens of one workgroup, at least two steps
   Split *splits;           // [gridDim]
@@ -130,47 +131,67 @@ struct Attention {
 
 // ---------------------------------------------------------------- the work
 
-struct Segments {  // of one request and KV head
+// The segments of one request and KV head.  A segment costs its tokens and
+// `fixed` more (its queries, first loads and output).
+struct Segments {
   long long before;  // cached tokens that every row sees
-  int count, per;
-  __device__ __forceinline__ Segments(const KvRequest &r, int tile_tokens)
-      : before(r.len > r.count ? r.len - r.count : 0), count(r.count), per(tile_tokens) {}
+  int count, per, fixed;
+  __device__ __forceinline__ Segments(int len, int count, const Attention &a)
+      : before(len > count ? len - count : 0), count(count), per(a.tile_tokens), fixed(a.fixed_keys) {}
   __device__ __forceinline__ int tiles() const { return (count + per - 1) / per; }
   // tokens that row tile t runs over
   __device__ __forceinline__ long long length(int t) const {
     return before + min((long long)(t + 1) * per, (long long)count);
   }
-  // the same summed over the tiles before t
+  // the costs of the tiles before t
   __device__ __forceinline__ long long start(int t) const {
-    return t * before + (long long)per * ((long long)t * (t + 1) / 2);
+    return t * (before + fixed) + (long long)per * ((long long)t * (t + 1) / 2);
   }
   __device__ __forceinline__ long long total() const {
     const int t = tiles() - 1;
-    return start(t) + length(t);
+    return start(t) + length(t) + fixed;
   }
 };
+
+// floor(a / b) of whole numbers 0 <= a < 2^52, 0 < b: by doubles, whose
+// quotient is off by one at most
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  long long q = (long long)((double)a / (double)b);
+  const long long r = a - q * b;
+  return r < 0 ? q - 1 : r >= b ? q + 1 : q;
+}
 
 struct Place {
   int item, head, tile, key;
 };
 
+// The list of requests with rows of a kernel's kind, in LDS.
+struct List {
+  long long *before;  // cost before each, and of all
+  int *ids, *len, *count;
+  __device__ __forceinline__ List(char *lds, int n)
+      : before(reinterpret_cast<long long *>(lds)), ids(reinterpret_cast<int *>(before + n + 1)), len(ids + n),
+        count(len + n) {}
+};
+__host__ __device__ constexpr int list_bytes(int n) { return (20 * n + 8 + 15) & ~15; }
+
 // Where the range of cost `c` begins: a segment and a token of it.
-__device__ __forceinline__ Place locate(const Attention &a, const long long *before, const int *ids,
-                                        int n, long long c) {
+__device__ __forceinline__ Place locate(const Attention &a, const List &list, int n, long long c) {
   Place p = {n, 0, 0, 0};
-  if (n == 0 || c >= before[n]) return p;
+  if (n == 0 || c >= list.before[n]) return p;
   int lo = 0, hi = n;  // before[lo] <= c < before[hi]
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (before[mid] <= c) lo = mid; else hi = mid;
+    if (list.before[mid] <= c) lo = mid; else hi = mid;
   }
   p.item = lo;
-  const Segments s(kv_request(a.batch, a.row_offsets, a.kv.block_shift, ids[lo]), a.tile_tokens);
-  long long left = c - before[lo];
+  const Segments s(list.len[lo], list.count[lo], a);
   const long long per_head = s.total();
-  p.head = (int)(left / per_head);
+  long long left = c - list.before[lo];
+  p.head = (int)quotient(left, per_head);
   left -= p.head * per_head;
-  int t0 = 0, t1 = s.tiles();  // start(t0) <= left < start(t1)
+  const int tiles = s.tiles();
+  int t0 = 0, t1 = tiles;  // start(t0) <= left < start(t1)
   while (t1 - t0 > 1) {
     const int mid = (t0 + t1) >> 1;
     if (s.start(mid) <= left) t0 = mid; else t1 = mid;
@@ -179,10 +200,10 @@ __device__ __forceinline__ Place locate(const Attention &a, const long long *bef
   left -= s.start(t0);
   const long long length = s.length(t0);
   if (length > a.atomic_keys) {
-    p.key = (int)left & -a.cut_keys;
-  } else if (2 * left >= length) {  // not cut: the nearer end
+    p.key = (int)max(left - s.fixed, 0ll) & -a.cut_keys;
+  } else if (2 * left >= length + s.fixed) {  // not cut: the nearer end
     p.tile = t0 + 1;
-    if (p.tile == s.tiles()) {
+    if (p.tile == tiles) {
       p.tile = 0;
       if (++p.head == a.kv.kv_heads) {
         p.head = 0;
@@ -204,52 +225,59 @@ __device__ __forceinline__ long long first_lane(unsigned long long x) {
   return (long long)((unsigned long long)__builtin_amdgcn_readfirstlane((unsigned)(x >> 32)) << 32 | lo);
 }
 
+// Where range w of `groups` begins: total w / groups, rounded down in two steps
+// whose products stay small.
+__device__ __forceinline__ long long cut(long long total, int w, int groups) {
+  const long long whole = quotient(total, groups);
+  return whole * w + (unsigned)((unsigned)(total - whole * groups) * (unsigned)w) / (unsigned)groups;
+}
+
 // The part of the work that a workgroup takes.
 struct Range {
   Place begin, end;
   int items;  // requests in the list
   int group;  // which range it is
 
-  // Fills the list (`before`: cost before each of its requests, and the total;
-  // `ids`: their numbers; both in LDS) and finds the range; false if there is
-  // none.  Called by all threads.  Records the segment that the range's begin
-  // is the first cut of.
+  // Fills the list and finds the range; false if there is none.  Called by all
+  // threads.  Records the segment that the range's begin is the first cut of.
   template <int kW>
-  __device__ __forceinline__ bool find(const Attention &a, long long *before, int *ids,
-                                       unsigned long long *scan) {
+  __device__ __forceinline__ bool find(const Attention &a, const List &list, unsigned long long *scan) {
     const int lane = lane_id();
-    // the list of requests with rows of this kernel's kind, and the cost before each
     int n = 0;
     long long total = 0;
     for (int i0 = 0; i0 < a.batch.n; i0 += 64 * kW) {
       const int i = i0 + threadIdx.x;
       unsigned long long v[2] = {0, 0}, all[2];
+      KvRequest r = {};
       if (i < a.batch.n) {
-        const KvRequest r = kv_request(a.batch, a.row_offsets, a.kv.block_shift, i);
+        r = kv_request(a.batch, a.row_offsets, a.kv.block_shift, i);
         if (!r.ok) {
           kv_report(a.status);
         } else {
           const int64_t rows = (int64_t)r.count * a.group;
           if (rows > a.min_rows && rows <= a.max_rows)
-            v[0] = Segments(r, a.tile_tokens).total() * a.kv.kv_heads;
+            v[0] = Segments(r.len, r.count, a).total() * a.kv.kv_heads;
         }
       }
       const unsigned long long cost = v[0];
       v[1] = cost > 0;
       block_exclusive_scan<2, unsigned long long, kW>(v, all, scan);
       if (cost) {
-        before[n + v[1]] = total + v[0];
-        ids[n + v[1]] = i;
+        const int at = n + (int)v[1];
+        list.before[at] = total + v[0];
+        list.ids[at] = i;
+        list.len[at] = r.len;
+        list.count[at] = r.count;
       }
       n += __builtin_amdgcn_readfirstlane((int)all[1]);
       total += first_lane(all[0]);
     }
-    if (threadIdx.x == 0) before[n] = total;
+    if (threadIdx.x == 0) list.before[n] = total;
     __syncthreads();
 
     // this workgroup's range: neighbours in cost on one XCD (workgroups go to
     // the 8 XCDs in turn), where heads and row tiles of a request share its L2
-    const int cap = (int)min((long long)gridDim.x, total / a.range_keys);
+    const int cap = (int)min((long long)gridDim.x, quotient(total, a.range_keys));
     const int groups = cap >= 8 ? cap & ~7 : max(cap, 1);
     const int block = blockIdx.x;
     if (block >= groups || n == 0) {
@@ -259,7 +287,7 @@ struct Range {
     const int w = groups >= 8 ? (block & 7) * (groups >> 3) + (block >> 3) : block;
     // lanes 0, 1, 2: this range's begin, its end, the one before's begin
     const int which = lane == 1 ? w + 1 : lane == 2 ? max(w - 1, 0) : w;
-    const Place found = locate(a, before, ids, n, total * which / groups);
+    const Place found = locate(a, list, n, cut(total, which, groups));
     const Place at = uniform(found, 0), prev = uniform(found, 2);
     begin = at;
     end = uniform(found, 1);
@@ -271,10 +299,13 @@ struct Range {
       const bool inside = at.key > 0 && !(prev.key > 0 && prev.item == at.item && prev.head == at.head &&
                                           prev.tile == at.tile);
       if (inside) {
-        const int id = ids[at.item];
-        const Segments seg(kv_request(a.batch, a.row_offsets, a.kv.block_shift, id), a.tile_tokens);
-        const long long stop = before[at.item] + at.head * seg.total() + seg.start(at.tile) + seg.length(at.tile);
-        s = {id, at.head, at.tile, (int)((stop * groups + total - 1) / total) - 1};
+        const Segments seg(list.len[at.item], list.count[at.item], a);
+        const long long stop = list.before[at.item] + at.head * seg.total() + seg.start(at.tile) +
+                               seg.length(at.tile) + seg.fixed;
+        // the last range that begins before `stop`
+        int end = min((int)quotient(stop, max(quotient(total, groups), 1ll)) + 1, groups - 1);
+        while (cut(total, end, groups) >= stop) --end;
+        s = {list.ids[at.item], at.head, at.tile, end};
       }
       a.splits[w] = s;
     }
@@ -489,8 +520,6 @@ struct Codes {
 // ------------------------------------------------------------- the kernel
 
 // A tile of up to 16 * kTiles rows; the waves share its tokens and combine in LDS.
-// Bytes of the list of requests at the head of a workgroup's LDS.
-__host__ __device__ constexpr int list_bytes(int n) { return (12 * n + 8 + 15) & ~15; }
 constexpr int waves_per_simd(int dim, int tiles) {
   const int held = dim * tiles;  // of q, o and codes in registers
   return held <= 64 ? 5 : tiles == 1 && held <= 128 ? 4 : held <= 128 ? 3 : held <= 256 ? 2 : 1;
@@ -503,13 +532,12 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
   typedef typename El<kType>::v8 v8;
   extern __shared__ __align__(16) char lds[];
   __shared__ unsigned long long scan[2 * kWaves];
-  long long *before = reinterpret_cast<long long *>(lds);
-  int *ids = reinterpret_cast<int *>(before + a.batch.n + 1);
+  const List list(lds, a.batch.n);
   float *mix = reinterpret_cast<float *>(lds + list_bytes(a.batch.n));
   const int lane = lane_id(), g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(wave_id());
   Range range;
-  if (!range.find<kWaves>(a, before, ids, scan)) return;
+  if (!range.find<kWaves>(a, list, scan)) return;
   Place at = range.begin;
   const Place end = uniform(range.end);
   const int n = __builtin_amdgcn_readfirstlane(range.items), w = __builtin_amdgcn_readfirstlane(range.group), kv_heads = a.kv.kv_heads;
@@ -517,9 +545,9 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
   Rowset<kType, kDim, kTiles, kCap> r;
   while (at.item < n) {
     at = uniform(at);  // the compiler does not see that it is
-    const int id = __builtin_amdgcn_readfirstlane(ids[at.item]);
+    const int id = __builtin_amdgcn_readfirstlane(list.ids[at.item]);
     const KvRequest req = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, id);
-    const Segments seg(req, a.tile_tokens);
+    const Segments seg(req.len, req.count, a);
     const int length = (int)seg.length(at.tile);
     const bool last = end.item == at.item && end.head == at.head && end.tile == at.tile;
     const int stop = last ? end.key : length;
@@ -706,22 +734,21 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
   constexpr int kSide = kStage * kDim * 2;  // bytes of a stage's K or V operands
   extern __shared__ __align__(16) char lds[];
   __shared__ unsigned long long scan[2 * kTW];
-  long long *before = reinterpret_cast<long long *>(lds);
-  int *ids = reinterpret_cast<int *>(before + a.batch.n + 1);
+  const List list(lds, a.batch.n);
   char *const stages = lds + list_bytes(a.batch.n);
   const int lane = lane_id(), n32 = lane & 31, hg = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(wave_id());
   Range range;
-  if (!range.find<kTW>(a, before, ids, scan)) return;
+  if (!range.find<kTW>(a, list, scan)) return;
   Place at = range.begin;
   const Place end = uniform(range.end);
   const int items = __builtin_amdgcn_readfirstlane(range.items), w = __builtin_amdgcn_readfirstlane(range.group);
 
   while (at.item < items) {
     at = uniform(at);  // the compiler does not see that it is
-    const int id = __builtin_amdgcn_readfirstlane(ids[at.item]);
+    const int id = __builtin_amdgcn_readfirstlane(list.ids[at.item]);
     const KvRequest req = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, id);
-    const Segments seg(req, a.tile_tokens);
+    const Segments seg(req.len, req.count, a);
     const int length = (int)seg.length(at.tile);
     const bool last = end.item == at.item && end.head == at.head && end.tile == at.tile;
     const int stop = last ? end.key : length;
@@ -1112,6 +1139,7 @@ int run(Attention a, char *ws, const Workspace &w, bool cap, float *block_weight
     // up to 512 tokens a cut costs more than it evens out (128 requests of 582
     // tokens on average, 64 heads: 57 us, with every cut made 64)
     a.atomic_keys = 512;
+    a.fixed_keys = 256;
     a.cut_keys = 32;
     a.range_keys = 256;
     a.splits = reinterpret_cast<Split *>(ws + w.splits);
@@ -1133,6 +1161,7 @@ int run(Attention a, char *ws, const Workspace &w, bool cap, float *block_weight
     a.max_rows = INT64_MAX;
     a.tile_tokens = tile_rows(kDim) / a.group;
     a.atomic_keys = 2048;
+    a.fixed_keys = 128;
     a.cut_keys = stage_tokens(kDim);
     a.range_keys = 256;
     a.splits = reinterpret_cast<Split *>(ws + w.tile_splits);
