@@ -120,7 +120,6 @@ struct Attention {
   int64_t min_rows, max_rows;  // requests with min_rows < rows <= max_rows are taken
   int tile_tokens;         // tokens of one row tile
   int atomic_keys;         // segments up to this long are not cut
-  int fixed_keys;          // what a segment costs besides its tokens, in tokens
   int cut_keys;            // cuts are at multiples of this power of two, the tokens of a step
   int range_keys;          // least tokens of one workgroup, at least two steps
   Split *splits;           // [gridDim]
@@ -131,13 +130,18 @@ struct Attention {
 
 // ---------------------------------------------------------------- the work
 
-// The segments of one request and KV head.  A segment costs its tokens and
-// `fixed` more (its queries, first loads and output).
+// What a segment costs besides its tokens (its queries, first loads and
+// output), in tokens.  128 decode rows over caches up to 8192 tokens: 56 us,
+// without it 65; 128 to 512 are alike.  A 32 Ki token prefill in chunks: 1.87
+// ms, without it 1.98.
+constexpr int kFixedKeys = 256;
+
+// The segments of one request and KV head.
 struct Segments {
   long long before;  // cached tokens that every row sees
-  int count, per, fixed;
+  int count, per;
   __device__ __forceinline__ Segments(int len, int count, const Attention &a)
-      : before(len > count ? len - count : 0), count(count), per(a.tile_tokens), fixed(a.fixed_keys) {}
+      : before(len > count ? len - count : 0), count(count), per(a.tile_tokens) {}
   __device__ __forceinline__ int tiles() const { return (count + per - 1) / per; }
   // tokens that row tile t runs over
   __device__ __forceinline__ long long length(int t) const {
@@ -145,11 +149,11 @@ struct Segments {
   }
   // the costs of the tiles before t
   __device__ __forceinline__ long long start(int t) const {
-    return t * (before + fixed) + (long long)per * ((long long)t * (t + 1) / 2);
+    return t * (before + kFixedKeys) + (long long)per * ((long long)t * (t + 1) / 2);
   }
   __device__ __forceinline__ long long total() const {
     const int t = tiles() - 1;
-    return start(t) + length(t) + fixed;
+    return start(t) + length(t) + kFixedKeys;
   }
 };
 
@@ -200,8 +204,8 @@ __device__ __forceinline__ Place locate(const Attention &a, const List &list, in
   left -= s.start(t0);
   const long long length = s.length(t0);
   if (length > a.atomic_keys) {
-    p.key = (int)max(left - s.fixed, 0ll) & -a.cut_keys;
-  } else if (2 * left >= length + s.fixed) {  // not cut: the nearer end
+    p.key = (int)max(left - kFixedKeys, 0ll) & -a.cut_keys;
+  } else if (2 * left >= length + kFixedKeys) {  // not cut: the nearer end
     p.tile = t0 + 1;
     if (p.tile == tiles) {
       p.tile = 0;
@@ -301,7 +305,7 @@ struct Range {
       if (inside) {
         const Segments seg(list.len[at.item], list.count[at.item], a);
         const long long stop = list.before[at.item] + at.head * seg.total() + seg.start(at.tile) +
-                               seg.length(at.tile) + seg.fixed;
+                               seg.length(at.tile) + kFixedKeys;
         // the last range that begins before `stop`
         int end = min((int)quotient(stop, max(quotient(total, groups), 1ll)) + 1, groups - 1);
         while (cut(total, end, groups) >= stop) --end;
@@ -1139,7 +1143,6 @@ int run(Attention a, char *ws, const Workspace &w, bool cap, float *block_weight
     // up to 512 tokens a cut costs more than it evens out (128 requests of 582
     // tokens on average, 64 heads: 57 us, with every cut made 64)
     a.atomic_keys = 512;
-    a.fixed_keys = 256;
     a.cut_keys = 32;
     a.range_keys = 256;
     a.splits = reinterpret_cast<Split *>(ws + w.splits);
@@ -1161,7 +1164,6 @@ int run(Attention a, char *ws, const Workspace &w, bool cap, float *block_weight
     a.max_rows = INT64_MAX;
     a.tile_tokens = tile_rows(kDim) / a.group;
     a.atomic_keys = 2048;
-    a.fixed_keys = 128;
     a.cut_keys = stage_tokens(kDim);
     a.range_keys = 256;
     a.splits = reinterpret_cast<Split *>(ws + w.tile_splits);
