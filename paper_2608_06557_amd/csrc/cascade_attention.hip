@@ -323,7 +323,6 @@ struct Range {
 template <int kType, int kDim, int kTiles, bool kCap>
 struct Rowset {
   typedef typename El<kType>::v8 v8;
-  v8 q[kTiles][kDim / 32];
   f4 o[kTiles][kDim / 16];
   float m[kTiles], sum[kTiles];
   int limit[kTiles];    // last cached token that the lane's row sees
@@ -340,18 +339,23 @@ struct Rowset {
   }
 
   // Scores of kB sub-blocks of 16 tokens; `k(b, d)` gives the operand of
-  // sub-block b and dims step d.
-  template <int kB, typename KOp>
-  __device__ __forceinline__ void scores(KOp k, f4 (&s)[kTiles][kB]) const {
+  // sub-block b and dims step d, `q(t, d)` that of row set t.
+  template <int kB, typename KOp, typename QOp>
+  __device__ __forceinline__ void scores(KOp k, QOp q, f4 (&s)[kTiles][kB]) const {
 #pragma unroll
-    for (int b = 0; b < kB; ++b) {
+    for (int b = 0; b < kB; ++b)
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) s[t][b] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int d = 0; d < kDim / 32; ++d) {
-        const v8 x = k(b, d);
+    for (int d = 0; d < kDim / 32; ++d) {
+      v8 x[kTiles];
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) s[t][b] = El<kType>::mfma(x, q[t][d], s[t][b]);
+      for (int t = 0; t < kTiles; ++t) x[t] = q(t, d);
+#pragma unroll
+      for (int b = 0; b < kB; ++b) {
+        const v8 y = k(b, d);
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) s[t][b] = El<kType>::mfma(y, x[t], s[t][b]);
       }
     }
   }
@@ -524,9 +528,14 @@ struct Codes {
 // ------------------------------------------------------------- the kernel
 
 // A tile of up to 16 * kTiles rows; the waves share its tokens and combine in LDS.
+// As many waves as its registers allow without scratch; 64 rows of 128 dims
+// spill 30 registers at two and are faster so (32 requests of 64 draft rows a
+// head over 9 Ki tokens: 157 us, without scratch at one wave 205), others that
+// could be pressed further are slower (32 rows of 128 dims at three waves: 132
+// us, at two 128; of 256 at two: 243, at one 234).
 constexpr int waves_per_simd(int dim, int tiles) {
-  const int held = dim * tiles;  // of q, o and codes in registers
-  return held <= 64 ? 5 : tiles == 1 && held <= 128 ? 4 : held <= 128 ? 3 : held <= 256 ? 2 : 1;
+  const int held = dim * tiles;  // of o in registers
+  return held <= 64 ? 5 : tiles == 1 && held <= 128 ? 4 : held <= 128 ? 3 : held <= 256 || tiles == 4 ? 2 : 1;
 }
 template <int kType, int kDim, int kTiles, bool kCap>
 __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attention_kernel(Attention a) {
@@ -537,7 +546,10 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
   extern __shared__ __align__(16) char lds[];
   __shared__ unsigned long long scan[2 * kWaves];
   const List list(lds, a.batch.n);
-  float *mix = reinterpret_cast<float *>(lds + list_bytes(a.batch.n));
+  // the waves' m and sum, and their O or before it q
+  float *const ms = reinterpret_cast<float *>(lds + list_bytes(a.batch.n)), *const os = ms + 2 * kWaves * 16;
+  char *const qs = reinterpret_cast<char *>(os);
+  static_assert(kRows * kDim * 2 <= 4 * kWaves * 16 * kPitch, "q fits the place of O");
   const int lane = lane_id(), g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(wave_id());
   Range range;
@@ -570,15 +582,6 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
       head[t] = at.head * a.group + row % a.group;
       valid[t] = row < tile_rows && token[t] < req.count;
       r.limit[t] = valid[t] ? shown + token[t] : -1;
-      const char *q = a.q.data + (int64_t)(req.first + (valid[t] ? token[t] : 0)) * a.q.token_stride +
-                      (valid[t] ? head[t] : 0) * a.q.head_stride + 32 * g;
-#pragma unroll
-      for (int d = 0; d < kDim / 32; ++d) {
-        u4 x = *reinterpret_cast<const u4 *>(q + 128 * (d >> 1) + 16 * (d & 1));
-        if (!valid[t]) x = u4{0, 0, 0, 0};
-        x = (x & a.keep) ^ a.flip;
-        r.q[t][d] = __builtin_bit_cast(typename El<kType>::v8, x);
-      }
       r.log_at[t] = nullptr;
       const int back = req.count - 1 - token[t];
       if (a.logs && valid[t] && back < a.window)
@@ -603,19 +606,39 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
     // sub-block is read again, from a cache.
     constexpr int kStride = 32 * kWaves;
     int key = __builtin_amdgcn_readfirstlane(at.key + 32 * wave);
+    Codes<kDim> c;
+    int slot[2];
+    auto look = [&](int key) {
+      slot[0] = cache.slot(key >> 4);
+      slot[1] = cache.slot((key >> 4) + 1);
+    };
+    look(key);
+    // the waves share the rows' q, which lies in operand order in LDS
+    constexpr int kQs = kTiles * (kDim / 32), kMine = (kQs + kWaves - 1) / kWaves;
+    u4 q[kMine];
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const int e = min(i * kWaves + wave, kQs - 1), d = e % (kDim / 32);
+      const int row = e / (kDim / 32) * 16 + (lane & 15);
+      const int token = at.tile * a.tile_tokens + row / a.group, head = at.head * a.group + row % a.group;
+      const bool valid = row < tile_rows && token < req.count;
+      q[i] = *reinterpret_cast<const u4 *>(a.q.data + (int64_t)(req.first + (valid ? token : 0)) * a.q.token_stride +
+                                           (valid ? head : 0) * a.q.head_stride + 32 * g + 128 * (d >> 1) +
+                                           16 * (d & 1));
+      q[i] = valid ? (q[i] & a.keep) ^ a.flip : u4{0, 0, 0, 0};
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    c.fetch_k(cache, slot, key);
+    // K before V, as in the loop: waits count the loads that follow
+    __builtin_amdgcn_sched_barrier(0);
+    c.fetch_v(cache, slot, key);
+    __builtin_amdgcn_sched_barrier(0);
+    look(key + kStride);
+#pragma unroll
+    for (int i = 0; i < kMine; ++i)
+      *reinterpret_cast<u4 *>(qs + (min(i * kWaves + wave, kQs - 1) * 64 + lane) * 16) = q[i];
+    __syncthreads();
     if (key < key_end) {
-      Codes<kDim> c;
-      int slot[2];
-      auto look = [&](int key) {
-        slot[0] = cache.slot(key >> 4);
-        slot[1] = cache.slot((key >> 4) + 1);
-      };
-      look(key);
-      c.fetch_k(cache, slot, key);
-      // K before V, as in the loop: waits count the loads that follow
-      __builtin_amdgcn_sched_barrier(0);
-      c.fetch_v(cache, slot, key);
-      look(key + kStride);
       while (true) {
         if (key + 32 > len) {
           const unsigned live[2] = {live_bytes(key + 4 * g, len), live_bytes(key + 16 + 4 * g, len)};
@@ -625,10 +648,15 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
             for (int b = 0; b < 2; ++b) c.v[b][i] &= live[b];
         }
         f4 x[kTiles][2];
+        int q_at = lane * 16;
+        asm volatile("" : "+v"(q_at));  // or the loads of q move out of the loop, into registers
         r.template scores<2>(
             [&](int b, int d) {
               const u4 w = c.k[b][d >> 1];
               return widen8<kType>(w[2 * (d & 1)], w[2 * (d & 1) + 1], c.ks[b], c.ks[b]);
+            },
+            [&](int t, int d) {
+              return *reinterpret_cast<const v8 *>(qs + (t * (kDim / 32) + d) * 1024 + q_at);
             },
             x);
         c.fetch_k(cache, slot, key + kStride);
@@ -654,8 +682,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
     }
     const bool whole = at.key == 0 && stop == length;
     const int64_t part = ((int64_t)w * 2 + (at.key > 0 ? 0 : 1)) * kRows;
-    // the waves' m, sum and O of one row set at a time
-    float *ms = mix, *os = mix + 2 * kWaves * 16;
+    // one row set at a time
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
       if (g == 0) {
