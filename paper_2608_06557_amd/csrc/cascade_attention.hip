@@ -115,7 +115,7 @@ struct Attention {
   float cap_in;            // softcap: exp2 argument per q.k
   unsigned keep, flip;     // q's bits: none where the scale was 0, turned signs where it was negative
   float *lse;              // [n_tokens][q_heads] or NULL
-  float *logs;             // [sub-block][window][q_heads]: log2 of a sub-block's weight, or NULL
+  float *logs;             // log2 of sub-blocks' weights, or NULL
   int window;
   int64_t min_rows, max_rows;  // requests with min_rows < rows <= max_rows are taken
   int tile_tokens;         // tokens of one row tile
@@ -129,6 +129,17 @@ struct Attention {
 };
 
 // ---------------------------------------------------------------- the work
+
+// Log sums lie as [sub-block][KV head][window][head of the group], so that a
+// segment's tile writes whole lines.  A row's place in a sub-block's, for the
+// head `of_group` of the token `back` before its request's last:
+__device__ __forceinline__ int log_place(const Attention &a, int kv_head, int back, int of_group) {
+  return (kv_head * a.window + back) * a.group + of_group;
+}
+// and those of a request's first sub-block:
+__device__ __forceinline__ float *first_logs(const Attention &a, int first_entry) {
+  return a.logs + ((int64_t)first_entry << (a.kv.block_shift - 4)) * a.window * a.q_heads;
+}
 
 // What a segment costs besides its tokens (its queries, first loads and
 // output), in tokens.  128 decode rows over caches up to 8192 tokens: 56 us,
@@ -326,7 +337,7 @@ struct Rowset {
   f4 o[kTiles][kDim / 16];
   float m[kTiles], sum[kTiles];
   int limit[kTiles];    // last cached token that the lane's row sees
-  float *log_at[kTiles];  // the row's place in the log sums of sub-block 0, NULL for none
+  int log_at[kTiles];   // the row's place in a sub-block's log sums, -1 for none
 
   __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -364,7 +375,7 @@ struct Rowset {
   // some row does not see all of the tokens.
   template <int kB>
   __device__ __forceinline__ void weights(const Attention &a, f4 (&s)[kTiles][kB], v8 (&p)[kTiles][kB / 2],
-                                          int key, int len, bool masked, bool logs, int64_t log_row) {
+                                          int key, int len, bool masked, float *logs) {
     const int lane = lane_id(), g = lane >> 4;
     if (kCap) {
 #pragma unroll
@@ -434,8 +445,8 @@ struct Rowset {
           float x = part[t][b];
           x += __shfl_xor(x, 16);
           x += __shfl_xor(x, 32);
-          if (g == 0 && log_at[t] && key + 16 * b < len)
-            log_at[t][(int64_t)((key >> 4) + b) * log_row] = __builtin_amdgcn_logf(x) + m[t];
+          if (g == 0 && log_at[t] >= 0 && key + 16 * b < len)
+            (logs + (int64_t)((key >> 4) + b) * a.window * a.q_heads)[log_at[t]] = __builtin_amdgcn_logf(x) + m[t];
         }
     }
   }
@@ -530,7 +541,7 @@ struct Codes {
 // A tile of up to 16 * kTiles rows; the waves share its tokens and combine in LDS.
 // As many waves as its registers allow without scratch; 64 rows of 128 dims
 // spill 30 registers at two and are faster so (32 requests of 64 draft rows a
-// head over 9 Ki tokens: 157 us, without scratch at one wave 205), others that
+// head over 7 Ki tokens: 157 us, without scratch at one wave 205), others that
 // could be pressed further are slower (32 rows of 128 dims at three waves: 132
 // us, at two 128; of 256 at two: 243, at one 234).
 constexpr int waves_per_simd(int dim, int tiles) {
@@ -571,25 +582,17 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
 
     // rows: lane n of row set t has row 16 t + n of the tile
     const int tile_rows = a.tile_tokens * a.group, shown = req.len - req.count;
-    bool valid[kTiles];
-    int token[kTiles], head[kTiles];
-    const int64_t log_row = (int64_t)a.window * a.q_heads;
-    bool logs = false;
+    bool any = false;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      const int row = 16 * t + (lane & 15);
-      token[t] = at.tile * a.tile_tokens + row / a.group;
-      head[t] = at.head * a.group + row % a.group;
-      valid[t] = row < tile_rows && token[t] < req.count;
-      r.limit[t] = valid[t] ? shown + token[t] : -1;
-      r.log_at[t] = nullptr;
-      const int back = req.count - 1 - token[t];
-      if (a.logs && valid[t] && back < a.window)
-        r.log_at[t] = a.logs + ((int64_t)req.row << (a.kv.block_shift - 4)) * log_row +
-                      (int64_t)back * a.q_heads + head[t];
-      logs |= r.log_at[t] != nullptr;
+      const int row = 16 * t + (lane & 15), token = at.tile * a.tile_tokens + row / a.group;
+      const bool valid = row < tile_rows && token < req.count;
+      r.limit[t] = valid ? shown + token : -1;
+      const int back = req.count - 1 - token;
+      r.log_at[t] = a.logs && valid && back < a.window ? log_place(a, at.head, back, row % a.group) : -1;
+      any |= r.log_at[t] >= 0;
     }
-    logs = __any(logs);
+    float *const logs = __any(any) ? first_logs(a, req.row) : nullptr;
     r.clear();
 
     // every row sees the tokens before clear_end, none those from key_end on
@@ -661,7 +664,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
             x);
         c.fetch_k(cache, slot, key + kStride);
         v8 p[kTiles][1];
-        r.template weights<2>(a, x, p, key, len, key + 32 > clear_end, logs, log_row);
+        r.template weights<2>(a, x, p, key, len, key + 32 > clear_end, logs);
         r.add(
             [&](int d) {
               return widen8<kType>(c.v[0][d >> 2][d & 3], c.v[1][d >> 2][d & 3], c.vs[0], c.vs[1]);
@@ -799,12 +802,10 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
       if (!valid) x = u4{0, 0, 0, 0};
       q[d] = __builtin_bit_cast(v8, (x & a.keep) ^ a.flip);
     }
-    const int64_t log_row = (int64_t)a.window * a.q_heads;
-    float *log_at = nullptr;  // the row's place in the log sums of sub-block 0
     const int back = req.count - 1 - token;
-    if (a.logs && valid && back < a.window)
-      log_at = a.logs + ((int64_t)req.row << (a.kv.block_shift - 4)) * log_row + (int64_t)back * a.q_heads + head;
-    const bool logs = __any(log_at != nullptr);
+    const int log_at =
+        a.logs && valid && back < a.window ? log_place(a, at.head, back, head - at.head * a.group) : -1;
+    float *const logs = __any(log_at >= 0) ? first_logs(a, req.row) : nullptr;
     // every row of the wave sees the tokens before clear_end, no row of the tile those from block_end on
     const int clear_end = __builtin_amdgcn_readfirstlane(shown + at.tile * a.tile_tokens + 32 * wave / a.group + 1);
     const int block_end = __builtin_amdgcn_readfirstlane(
@@ -934,8 +935,8 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
             const float all = part[u] + __shfl_xor(part[u], 32);
-            if (hg == 0 && log_at && key + 16 * u < len)
-              log_at[(int64_t)((key >> 4) + u) * log_row] = __builtin_amdgcn_logf(all) + m;
+            if (hg == 0 && log_at >= 0 && key + 16 * u < len)
+              (logs + (int64_t)((key >> 4) + u) * a.window * a.q_heads)[log_at] = __builtin_amdgcn_logf(all) + m;
           }
         }
       };
@@ -1080,23 +1081,32 @@ __global__ __launch_bounds__(kBlock) void weight_kernel(Attention a, float *bloc
   if (i >= a.batch.n || e >= a.batch.n_entries) return;
   const KvRequest r = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, i);
   if (!r.ok || e < r.row || (int64_t)(e - r.row) << (subs + 4) >= r.len || r.count == 0) return;
-  const int rows = min(a.window, r.count) * a.q_heads;
-  // row j: query head j % q_heads of the token j / q_heads before the last
   const float *lse = a.lse + (int64_t)(r.first + r.count - 1) * a.q_heads;
   const float old = block_weight[e];
   float sum = 0.f;
+  // 64 rows on: `step` of KV heads, tokens back and heads of the group
+  int backs = 0, step[3], first[3];
   for (int s = 0; s < 1 << subs; ++s) {
-    const int first = (((e - r.row) << subs) + s) << 4;  // the sub-block's first token
+    const int token = (((e - r.row) << subs) + s) << 4;  // the sub-block's first token
     // tokens more than `behind` back do not see it, and left no log sum
-    const int behind = r.len - 1 - first;
+    const int behind = r.len - 1 - token;
     if (behind < 0) break;
-    const int seen = (int)min((int64_t)rows, (int64_t)(behind + 1) * a.q_heads);
+    const int seen = min(min(a.window, r.count), behind + 1);
+    if (seen != backs) {
+      backs = seen;
+      const int per = backs * a.group;
+      step[0] = 64 / per, step[1] = 64 % per / a.group, step[2] = 64 % per % a.group;
+      first[0] = lane / per, first[1] = lane % per / a.group, first[2] = lane % per % a.group;
+    }
     const float *log = a.logs + (((int64_t)e << subs) + s) * a.window * a.q_heads;
-    int back = lane / a.q_heads, head = lane - back * a.q_heads;
+    int kv_head = first[0], back = first[1], head = first[2];
 #pragma unroll 4
-    for (int j = lane; j < seen; j += 64) {
-      sum += __builtin_amdgcn_exp2f(log[j] - lse[head - back * a.q_heads] * kLog2e);
-      for (head += 64; head >= a.q_heads; head -= a.q_heads) ++back;
+    for (int j = lane; j < backs * a.q_heads; j += 64) {
+      const float x = log[(kv_head * a.window + back) * a.group + head];
+      sum += __builtin_amdgcn_exp2f(x - lse[kv_head * a.group + head - back * a.q_heads] * kLog2e);
+      kv_head += step[0], back += step[1], head += step[2];
+      if (head >= a.group) head -= a.group, ++back;
+      if (back >= backs) back -= backs, ++kv_head;
     }
   }
 #pragma unroll
