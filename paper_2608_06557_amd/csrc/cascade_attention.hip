@@ -1168,7 +1168,8 @@ void start_tiles(const Attention &a, bool cap, hipStream_t stream) {
 template <int kType, int kDim>
 int run(Attention a, char *ws, const Workspace &w, bool cap, float *block_weight, hipStream_t s) {
   const int64_t most = (int64_t)a.batch.max_new * a.group;  // rows of a request and KV head
-  const int64_t keys = ((int64_t)a.batch.n_entries << a.kv.block_shift) * a.kv.kv_heads;
+  const int64_t table = (int64_t)a.batch.n_entries << a.kv.block_shift;  // no request is longer
+  const int64_t keys = table * a.kv.kv_heads;
   // few rows: 4 waves share a tile's tokens.  More: row tiles, and requests of
   // up to 32 rows beside them in the first kernel.
   const bool tiled = most > most_rows(kDim);
@@ -1177,9 +1178,11 @@ int run(Attention a, char *ws, const Workspace &w, bool cap, float *block_weight
     a.min_rows = 0;
     a.max_rows = small;
     a.tile_tokens = small / a.group > 0 ? small / a.group : 1;
-    // up to 512 tokens a cut costs more than it evens out (128 requests of 582
-    // tokens on average, 64 heads: 57 us, with every cut made 64)
-    a.atomic_keys = 512;
+    // Up to 512 tokens a cut costs more than it evens out (128 requests of 582
+    // tokens on average, 64 heads: 57 us, with every cut made 64);
+    // up to 1024 where no request can be longer, which saves the join (one of
+    // 777 tokens: 11.0 us, cut 12.5; 100: 8.0, with a join that finds nothing 11.4)
+    a.atomic_keys = table <= 1024 ? 1024 : 512;
     a.cut_keys = 32;
     a.range_keys = 256;
     a.splits = reinterpret_cast<Split *>(ws + w.splits);
@@ -1194,7 +1197,8 @@ int run(Attention a, char *ws, const Workspace &w, bool cap, float *block_weight
       start<kType, kDim, 2>(a, grid, cap, s);
     else if constexpr (kDim < 256)
       start<kType, kDim, 4>(a, grid, cap, s);
-    hipLaunchKernelGGL((join_kernel<kType, kDim>), dim3(grid, small / kWaves), dim3(kBlock), 0, s, a, small, 1);
+    if (table > a.atomic_keys)  // else none is cut
+      hipLaunchKernelGGL((join_kernel<kType, kDim>), dim3(grid, small / kWaves), dim3(kBlock), 0, s, a, small, 1);
   }
   if (tiled) {
     a.min_rows = a.batch.n > 1 ? small : 0;
@@ -1207,8 +1211,9 @@ int run(Attention a, char *ws, const Workspace &w, bool cap, float *block_weight
     a.parts = reinterpret_cast<float *>(ws + w.tile_parts);
     a.part_sums = reinterpret_cast<float *>(ws + w.tile_sums);
     start_tiles<kType, kDim>(a, cap, s);
-    hipLaunchKernelGGL((join_kernel<kType, kDim>), dim3(kTileGroups, tile_rows(kDim) / (2 * kWaves)), dim3(kBlock),
-                       0, s, a, tile_rows(kDim), 2);
+    if (table > a.atomic_keys)
+      hipLaunchKernelGGL((join_kernel<kType, kDim>), dim3(kTileGroups, tile_rows(kDim) / (2 * kWaves)), dim3(kBlock),
+                         0, s, a, tile_rows(kDim), 2);
   }
   if (block_weight)
     hipLaunchKernelGGL(weight_kernel, dim3((a.batch.n_entries + kWaves - 1) / kWaves), dim3(kBlock), 0,
