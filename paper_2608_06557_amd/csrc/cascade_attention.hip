@@ -59,6 +59,10 @@ template <> struct El<CASCADE_BF16> {
   static __device__ __forceinline__ unsigned widen_hi(unsigned w, float s) {
     return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, true));
   }
+  // c plus both of w
+  static __device__ __forceinline__ float add2(unsigned w, float c) {
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2, w), __builtin_bit_cast(v2, 0x3f803f80u), c, false);
+  }
   static __device__ __forceinline__ f4 mfma(v8 a, v8 b, f4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
   }
@@ -74,6 +78,9 @@ template <> struct El<CASCADE_F16> {
   }
   static __device__ __forceinline__ unsigned widen_hi(unsigned w, float s) {
     return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, s, true));
+  }
+  static __device__ __forceinline__ float add2(unsigned w, float c) {
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(v2, w), __builtin_bit_cast(v2, 0x3c003c00u), c, false);
   }
   static __device__ __forceinline__ f4 mfma(v8 a, v8 b, f4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
@@ -93,6 +100,16 @@ template <int kType>
 __device__ __forceinline__ unsigned narrow2(float a, float b) {
   const f2 f = {a, b};
   return __builtin_bit_cast(unsigned, __builtin_convertvector(f, typename El<kType>::v2));
+}
+
+// What O is multiplied by so that it is an average by the weights as they were
+// rounded, `used` their sum, and not by the weights of `sum`: a row that one
+// token dominates is exact then, where the rounding of its weight would stay.
+// 8 heads over 777 tokens of bfloat16: relative error 1.8e-3 to 2.2e-3 (of
+// which the result's own rounding is 1.4e-3 to 1.7e-3), without it up to
+// 2.7e-3.  It costs the row tiles 3 %, the others nothing.
+__device__ __forceinline__ float evened(float sum, float used) {
+  return used > 0.f && used < __builtin_inff() ? sum / used : 1.f;
 }
 
 struct Rows {
@@ -336,6 +353,7 @@ struct Rowset {
   typedef typename El<kType>::v8 v8;
   f4 o[kTiles][kDim / 16];
   float m[kTiles], sum[kTiles];
+  float used[kTiles];   // sum of the weights as they are rounded for the product
   int limit[kTiles];    // last cached token that the lane's row sees
   int log_at[kTiles];   // the row's place in a sub-block's log sums, -1 for none
 
@@ -343,7 +361,7 @@ struct Rowset {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
       m[t] = kLowest;
-      sum[t] = 0.f;
+      sum[t] = used[t] = 0.f;
 #pragma unroll
       for (int d = 0; d < kDim / 16; ++d) o[t][d] = f4{0.f, 0.f, 0.f, 0.f};
     }
@@ -414,6 +432,7 @@ struct Rowset {
         const float now = fmaxf(m[t], top[t]), f = __builtin_amdgcn_exp2f(m[t] - now);
         m[t] = now;
         sum[t] *= f;
+        used[t] *= f;
 #pragma unroll
         for (int d = 0; d < kDim / 16; ++d) o[t][d] *= f;
       }
@@ -435,6 +454,8 @@ struct Rowset {
                       narrow2<kType>(s[t][b + 1][0], s[t][b + 1][1]),
                       narrow2<kType>(s[t][b + 1][2], s[t][b + 1][3])};
         p[t][b / 2] = __builtin_bit_cast(v8, w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) used[t] = El<kType>::add2(w[i], used[t]);
       }
     }
     if (logs) {
@@ -682,6 +703,8 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
     for (int t = 0; t < kTiles; ++t) {
       r.sum[t] += __shfl_xor(r.sum[t], 16);
       r.sum[t] += __shfl_xor(r.sum[t], 32);
+      r.used[t] += __shfl_xor(r.used[t], 16);
+      r.used[t] += __shfl_xor(r.used[t], 32);
     }
     const bool whole = at.key == 0 && stop == length;
     const int64_t part = ((int64_t)w * 2 + (at.key > 0 ? 0 : 1)) * kRows;
@@ -696,7 +719,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
       float top = kLowest;
 #pragma unroll
       for (int k = 0; k < kWaves; ++k) top = fmaxf(top, ms[(k * 16 + (lane & 15)) * 2]);
-      const float f = __builtin_amdgcn_exp2f(r.m[t] - top);
+      const float f = __builtin_amdgcn_exp2f(r.m[t] - top) * evened(r.sum[t], r.used[t]);
 #pragma unroll
       for (int d0 = 0; d0 < kDim; d0 += kPart) {
 #pragma unroll
@@ -817,7 +840,7 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
     for (int d = 0; d < kOut; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-    float m = kLowest, sum = 0.f;
+    float m = kLowest, sum = 0.f, used = 0.f;
     if (first_key < block_end) {
       // a wave carries one sub-block's K or V, a stage ahead.  Slots and scales by vector
       // loads, whose waits count in order (a wait for scalar loads waits for all
@@ -914,6 +937,7 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
           const float now = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - now);
           m = now;
           sum *= f;
+          used *= f;
 #pragma unroll
           for (int d = 0; d < kOut; ++d) o[d] *= f;
         }
@@ -929,6 +953,8 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
           const u4 b = {narrow2<kType>(x[8 * u], x[8 * u + 1]), narrow2<kType>(x[8 * u + 2], x[8 * u + 3]),
                         narrow2<kType>(x[8 * u + 4], x[8 * u + 5]), narrow2<kType>(x[8 * u + 6], x[8 * u + 7])};
           p[u] = __builtin_bit_cast(v8, b);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) used = E::add2(b[i], used);
         }
         sum += part[0] + part[1];
         if (logs) {
@@ -983,8 +1009,10 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
     }
 
     sum += __shfl_xor(sum, 32);
+    used += __shfl_xor(used, 32);
+    const float even = evened(sum, used);
     if (valid && at.key == 0 && stop == length) {
-      const float f = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
+      const float f = (sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum) * even;
       char *out = a.out.data + (int64_t)(req.first + token) * a.out.token_stride + head * a.out.head_stride + 8 * hg;
 #pragma unroll
       for (int d = 0; d < kOut; ++d)
@@ -1003,7 +1031,7 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           *reinterpret_cast<f4 *>(to + 32 * d + 8 * j) =
-              f4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
+              f4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]} * even;
       if (hg == 0) *reinterpret_cast<f2 *>(a.part_sums + 2 * part) = f2{m, sum};
     }
 
