@@ -22,6 +22,13 @@
 // itself (a scan), so ragged batches need neither a host plan nor another launch.  A
 // segment that one workgroup covers is written at once; parts of a cut one go
 // to the workspace and a second launch joins them.
+//
+// Few rows of a request are bound by reading the cache: 4 requests of 115 Ki
+// tokens, 32 heads over 8 of 128 dims, 947 MB in 177 us (5.3 TB/s; a large
+// read reaches 6.2) and 8 for the join; 128 requests of 582 tokens, 64 heads,
+// 157 MB in 35 us (4.5 TB/s: 4 us are the list, and short segments fill and
+// drain), the join and the weights 10 more.  Many rows are bound by the
+// products and the softmax beside them (tile_kernel).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -588,7 +595,8 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
   if (!range.find<kWaves>(a, list, scan)) return;
   Place at = range.begin;
   const Place end = uniform(range.end);
-  const int n = __builtin_amdgcn_readfirstlane(range.items), w = __builtin_amdgcn_readfirstlane(range.group), kv_heads = a.kv.kv_heads;
+  const int n = __builtin_amdgcn_readfirstlane(range.items), w = __builtin_amdgcn_readfirstlane(range.group);
+  const int kv_heads = a.kv.kv_heads;
 
   Rowset<kType, kDim, kTiles, kCap> r;
   while (at.item < n) {
@@ -775,10 +783,12 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
 // The products are taken as 32x32x16: one such instruction leaves room for 6
 // vector instructions in its 32 cycles, two 16x16x32 for 2 each, and the softmax
 // has about as many cycles as the products.  8 waves on a stage: with 4 each wave
-// widens twice as much (2.13 ms instead of 2.04 for 16 chunks of 512 tokens, 64
-// heads, contexts of 7 k).  At 32 rows a wave, operands cross from LDS at 128 bytes
+// widens twice as much and takes 4 % longer.  16 chunks of 512 tokens, 64 heads over
+// 8 of 128 dims, contexts of 7 k: 1.8 to 1.9 ms, 0.95 PFLOP/s of the 1.24 that a large
+// matrix product reaches.  At 32 rows a wave, operands cross from LDS at 128 bytes
 // in a product's cycles, all that LDS gives: products, LDS and softmax
-// take about 1.0, 0.9 and 0.9 ms of those 2.04 and overlap in part.
+// take about 1.0, 0.9 and 0.9 ms and overlap in part; 64 rows to a wave halve the LDS
+// reads, but leave one wave to a SIMD and take 25 % longer.
 constexpr int stage_tokens(int dim) { return dim == 256 ? 32 : 64; }
 constexpr int tile_waves(int dim) { return 2 * stage_tokens(dim) / 16; }
 constexpr int tile_rows(int dim) { return 32 * tile_waves(dim); }
