@@ -114,7 +114,7 @@ __device__ __forceinline__ unsigned narrow2(float a, float b) {
 // token dominates is exact then, where the rounding of its weight would stay.
 // 8 heads over 777 tokens of bfloat16: relative error 1.8e-3 to 2.2e-3 (of
 // which the result's own rounding is 1.4e-3 to 1.7e-3), without it up to
-// 2.7e-3.  It costs the row tiles 3 %, the others nothing.
+// 2.7e-3.  It costs row tiles 3 % where log sums are wanted too, else nothing.
 __device__ __forceinline__ float evened(float sum, float used) {
   return used > 0.f && used < __builtin_inff() ? sum / used : 1.f;
 }
@@ -851,6 +851,7 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
     float m = kLowest, sum = 0.f, used = 0.f;
+    const bool exact = a.lse != nullptr;  // only log sums need the sum of the weights unrounded
     if (first_key < block_end) {
       // a wave carries one sub-block's K or V, a stage ahead.  Slots and scales by vector
       // loads, whose waits count in order (a wait for scalar loads waits for all
@@ -955,17 +956,20 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
       auto weigh = [&](f16v &x, v8 (&p)[2], int key) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale, -m));
-        float part[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          part[u] = ((x[8 * u] + x[8 * u + 1]) + (x[8 * u + 2] + x[8 * u + 3])) +
-                    ((x[8 * u + 4] + x[8 * u + 5]) + (x[8 * u + 6] + x[8 * u + 7]));
           const u4 b = {narrow2<kType>(x[8 * u], x[8 * u + 1]), narrow2<kType>(x[8 * u + 2], x[8 * u + 3]),
                         narrow2<kType>(x[8 * u + 4], x[8 * u + 5]), narrow2<kType>(x[8 * u + 6], x[8 * u + 7])};
           p[u] = __builtin_bit_cast(v8, b);
 #pragma unroll
           for (int i = 0; i < 4; ++i) used = E::add2(b[i], used);
         }
+        if (!exact) return;
+        float part[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          part[u] = ((x[8 * u] + x[8 * u + 1]) + (x[8 * u + 2] + x[8 * u + 3])) +
+                    ((x[8 * u + 4] + x[8 * u + 5]) + (x[8 * u + 6] + x[8 * u + 7]));
         sum += part[0] + part[1];
         if (logs) {
 #pragma unroll
@@ -1020,6 +1024,7 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
 
     sum += __shfl_xor(sum, 32);
     used += __shfl_xor(used, 32);
+    if (!exact) sum = used;
     const float even = evened(sum, used);
     if (valid && at.key == 0 && stop == length) {
       const float f = (sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum) * even;
