@@ -139,7 +139,8 @@ struct Attention {
   float cap_in;            // softcap: exp2 argument per q.k
   unsigned keep, flip;     // q's bits: none where the scale was 0, turned signs where it was negative
   float *lse;              // [n_tokens][q_heads] or NULL
-  float *logs;             // log2 of sub-blocks' weights, or NULL
+  float *logs;             // log2 of weights over runs of tokens, or NULL
+  int log_shift;           // log2 of such a run
   int window;
   int64_t min_rows, max_rows;  // requests with min_rows < rows <= max_rows are taken
   int tile_tokens;         // tokens of one row tile
@@ -154,15 +155,17 @@ struct Attention {
 
 // ---------------------------------------------------------------- the work
 
-// Log sums lie as [sub-block][KV head][window][head of the group], so that a
-// segment's tile writes whole lines.  A row's place in a sub-block's, for the
-// head `of_group` of the token `back` before its request's last:
+// Log sums are kept of each 32 tokens, or 16 in blocks of no more (32 requests
+// with draft rows and weights of 8 tokens: 118 us, by 16 123).  They lie as
+// [run][KV head][window][head of the group], so that a segment's tile writes
+// whole lines.  A row's place in a run's, for the head `of_group` of the token
+// `back` before its request's last:
 __device__ __forceinline__ int log_place(const Attention &a, int kv_head, int back, int of_group) {
   return (kv_head * a.window + back) * a.group + of_group;
 }
-// and those of a request's first sub-block:
+// and those of a request's first run:
 __device__ __forceinline__ float *first_logs(const Attention &a, int first_entry) {
-  return a.logs + ((int64_t)first_entry << (a.kv.block_shift - 4)) * a.window * a.q_heads;
+  return a.logs + ((int64_t)first_entry << (a.kv.block_shift - a.log_shift)) * a.window * a.q_heads;
 }
 
 // What a segment costs besides its tokens (its queries, first loads and
@@ -362,7 +365,7 @@ struct Rowset {
   float m[kTiles], sum[kTiles];
   float used[kTiles];   // sum of the weights as they are rounded for the product
   int limit[kTiles];    // last cached token that the lane's row sees
-  int log_at[kTiles];   // the row's place in a sub-block's log sums, -1 for none
+  int log_at[kTiles];   // the row's place in a run's log sums, -1 for none
 
   __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -466,16 +469,23 @@ struct Rowset {
       }
     }
     if (logs) {
+      static_assert(kB == 2, "one run of 32 tokens, or two of 16");
+      const int64_t run = (int64_t)a.window * a.q_heads;
+      float *const to = logs + (key >> a.log_shift) * run;
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-        for (int b = 0; b < kB; ++b) {
-          float x = part[t][b];
+      for (int t = 0; t < kTiles; ++t) {
+        auto keep = [&](float x, float *to) {
           x += __shfl_xor(x, 16);
           x += __shfl_xor(x, 32);
-          if (g == 0 && log_at[t] >= 0 && key + 16 * b < len)
-            (logs + (int64_t)((key >> 4) + b) * a.window * a.q_heads)[log_at[t]] = __builtin_amdgcn_logf(x) + m[t];
+          if (g == 0 && log_at[t] >= 0) to[log_at[t]] = __builtin_amdgcn_logf(x) + m[t];
+        };
+        if (a.log_shift == 5) {
+          keep(part[t][0] + part[t][1], to);
+        } else {
+          keep(part[t][0], to);
+          if (key + 16 < len) keep(part[t][1], to + run);
         }
+      }
     }
   }
 
@@ -972,11 +982,17 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
                     ((x[8 * u + 4] + x[8 * u + 5]) + (x[8 * u + 6] + x[8 * u + 7]));
         sum += part[0] + part[1];
         if (logs) {
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const float all = part[u] + __shfl_xor(part[u], 32);
-            if (hg == 0 && log_at >= 0 && key + 16 * u < len)
-              (logs + (int64_t)((key >> 4) + u) * a.window * a.q_heads)[log_at] = __builtin_amdgcn_logf(all) + m;
+          const int64_t run = (int64_t)a.window * a.q_heads;
+          float *const to = logs + (key >> a.log_shift) * run;
+          auto keep = [&](float x, float *to) {
+            x += __shfl_xor(x, 32);
+            if (hg == 0 && log_at >= 0) to[log_at] = __builtin_amdgcn_logf(x) + m;
+          };
+          if (a.log_shift == 5) {
+            if (key < len) keep(part[0] + part[1], to);
+          } else {
+            if (key < len) keep(part[0], to);
+            if (key + 16 < len) keep(part[1], to + run);
           }
         }
       };
@@ -1111,10 +1127,10 @@ __global__ __launch_bounds__(kBlock) void join_kernel(Attention a, int rows, int
 }
 
 // Adds to each table entry the weight that its request's last tokens gave it:
-// one wave per entry, its sub-blocks' log sums against the rows' totals.
+// one wave per entry, its runs' log sums against the rows' totals.
 __global__ __launch_bounds__(kBlock) void weight_kernel(Attention a, float *block_weight) {
   __shared__ unsigned sums[kWaves];
-  const int e0 = blockIdx.x * kWaves, lane = lane_id(), subs = a.kv.block_shift - 4;
+  const int e0 = blockIdx.x * kWaves, lane = lane_id(), subs = a.kv.block_shift - a.log_shift;
   unsigned ended[1] = {0};
   for (int i = threadIdx.x; i < a.batch.n; i += kBlock) ended[0] += a.row_offsets[i + 1] <= e0;
   block_sum<1, unsigned>(ended, sums);
@@ -1123,14 +1139,14 @@ __global__ __launch_bounds__(kBlock) void weight_kernel(Attention a, float *bloc
   while (i < a.batch.n && uniform_load(a.row_offsets + i + 1) <= e) ++i;
   if (i >= a.batch.n || e >= a.batch.n_entries) return;
   const KvRequest r = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, i);
-  if (!r.ok || e < r.row || (int64_t)(e - r.row) << (subs + 4) >= r.len || r.count == 0) return;
+  if (!r.ok || e < r.row || (int64_t)(e - r.row) << a.kv.block_shift >= r.len || r.count == 0) return;
   const float *lse = a.lse + (int64_t)(r.first + r.count - 1) * a.q_heads;
   const float old = block_weight[e];
   float sum = 0.f;
   // 64 rows on: `step` of KV heads, tokens back and heads of the group
   int backs = 0, step[3], first[3];
   for (int s = 0; s < 1 << subs; ++s) {
-    const int token = (((e - r.row) << subs) + s) << 4;  // the sub-block's first token
+    const int token = (((e - r.row) << subs) + s) << a.log_shift;  // the run's first
     // tokens more than `behind` back do not see it, and left no log sum
     const int behind = r.len - 1 - token;
     if (behind < 0) break;
@@ -1168,6 +1184,8 @@ struct Workspace {
   size_t splits, tile_splits, parts, tile_parts, sums, tile_sums, lse, logs, total;
 };
 
+int log_shift(const cascade_kv_format_t *f) { return f->block_tokens >= 32 ? 5 : 4; }
+
 size_t aligned(size_t n) { return (n + 255) & ~(size_t)255; }
 
 Workspace layout(const cascade_kv_format_t *f, const cascade_kv_batch_t *b, int q_heads, int window) {
@@ -1185,7 +1203,7 @@ Workspace layout(const cascade_kv_format_t *f, const cascade_kv_batch_t *b, int 
   w.sums = take(sizeof(float) * kGroups * 2 * most_rows(f->head_dim) * 2);
   w.tile_sums = take(sizeof(float) * kTileGroups * 2 * tile_rows(f->head_dim) * 2);
   w.lse = take(window ? sizeof(float) * b->n_tokens * q_heads : 0);
-  w.logs = take(window ? sizeof(float) * b->n_entries * (f->block_tokens / 16) * window * q_heads : 0);
+  w.logs = take(window ? sizeof(float) * ((size_t)b->n_entries * f->block_tokens >> log_shift(f)) * window * q_heads : 0);
   w.total = at;
   return w;
 }
@@ -1323,6 +1341,7 @@ extern "C" int cascade_attention(const cascade_kv_pool_t *pool, int32_t layer,
   char *ws = static_cast<char *>(workspace);
   a.window = args->weight_window;
   a.lse = args->lse ? args->lse : a.window ? reinterpret_cast<float *>(ws + w.lse) : nullptr;
+  a.log_shift = log_shift(format);
   a.logs = a.window && batch->n_entries ? reinterpret_cast<float *>(ws + w.logs) : nullptr;
   a.status = status_dev;
   const auto s = static_cast<hipStream_t>(stream);
