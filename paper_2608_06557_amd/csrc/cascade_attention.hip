@@ -576,7 +576,7 @@ struct Codes {
 
 // ------------------------------------------------------------- the kernel
 
-// A tile of up to 16 * kTiles rows; the waves share its tokens and combine in LDS.
+// A tile of up to 16 * kTiles rows; kWaves waves share its tokens and combine in LDS.
 // As many waves as its registers allow without scratch; 64 rows of 128 dims
 // spill 30 registers at two and are faster so (32 requests of 64 draft rows a
 // head over 7 Ki tokens: 157 us, without scratch at one wave 205), others that
@@ -586,8 +586,9 @@ constexpr int waves_per_simd(int dim, int tiles) {
   const int held = dim * tiles;  // of o in registers
   return held <= 64 ? 5 : tiles == 1 && held <= 128 ? 4 : held <= 128 ? 3 : held <= 256 || tiles == 4 ? 2 : 1;
 }
-template <int kType, int kDim, int kTiles, bool kCap>
-__global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attention_kernel(Attention a) {
+template <int kType, int kDim, int kTiles, bool kCap, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, waves_per_simd(kDim, kTiles)) void attention_kernel(Attention a) {
+  constexpr int kBlock = 64 * kWaves;
   constexpr int kRows = 16 * kTiles;
   constexpr int kPart = kDim < 128 ? kDim : 128;  // dims that one combination takes
   constexpr int kPitch = kPart + 4;
@@ -1176,6 +1177,12 @@ __global__ __launch_bounds__(kBlock) void weight_kernel(Attention a, float *bloc
 // ------------------------------------------------------------------- host
 
 constexpr int kCUs = 256;
+// Up to this many tokens in the whole table nothing is cut, which saves the join
+// (one request of 777 tokens: 11.4 us, cut 12.5; of 100: 7.8, with a join that
+// finds nothing 11.4).  A single tile of few rows has 8 waves then, where its
+// tokens are enough for them (777: 10.4 us, 600: 9.5 against 10.2; 100: 8.2
+// against 7.8, so not there; 16 waves 15.9).
+constexpr int kUncut = 1024, kWide = 8;
 constexpr int kGroups = 4 * kCUs;      // workgroups of the kernel that splits tokens over waves
 constexpr int kTileGroups = kCUs;   // of the kernel that splits rows over waves: one to a CU
 constexpr int most_rows(int dim) { return dim == 256 ? 32 : 64; }  // of a request in the former
@@ -1212,11 +1219,12 @@ bool heads_ok(const cascade_kv_format_t *f, int q_heads) {
   return q_heads >= 1 && q_heads % f->kv_heads == 0 && q_heads / f->kv_heads <= 128;
 }
 
-template <int kType, int kDim, int kTiles>
+template <int kType, int kDim, int kTiles, int kW = kWaves>
 void start(const Attention &a, int grid, bool cap, hipStream_t stream) {
-  const size_t mix = sizeof(float) * kWaves * 16 * (2 + (kDim < 128 ? kDim : 128) + 4);
-  auto kernel = cap ? attention_kernel<kType, kDim, kTiles, true> : attention_kernel<kType, kDim, kTiles, false>;
-  hipLaunchKernelGGL(kernel, dim3(grid), dim3(kBlock), list_bytes(a.batch.n) + mix, stream, a);
+  const size_t mix = sizeof(float) * kW * 16 * (2 + (kDim < 128 ? kDim : 128) + 4);
+  auto kernel =
+      cap ? attention_kernel<kType, kDim, kTiles, true, kW> : attention_kernel<kType, kDim, kTiles, false, kW>;
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * kW), list_bytes(a.batch.n) + mix, stream, a);
 }
 
 template <int kType, int kDim>
@@ -1240,19 +1248,21 @@ int run(Attention a, char *ws, const Workspace &w, bool cap, float *block_weight
     a.max_rows = small;
     a.tile_tokens = small / a.group > 0 ? small / a.group : 1;
     // Up to 512 tokens a cut costs more than it evens out (128 requests of 582
-    // tokens on average, 64 heads: 57 us, with every cut made 64);
-    // up to 1024 where no request can be longer, which saves the join (one of
-    // 777 tokens: 11.0 us, cut 12.5; 100: 8.0, with a join that finds nothing 11.4)
-    a.atomic_keys = table <= 1024 ? 1024 : 512;
+    // tokens on average, 64 heads: 57 us, with every cut made 64).
+    a.atomic_keys = table <= kUncut ? kUncut : 512;
     a.cut_keys = 32;
     a.range_keys = 256;
     a.splits = reinterpret_cast<Split *>(ws + w.splits);
     a.parts = reinterpret_cast<float *>(ws + w.parts);
     a.part_sums = reinterpret_cast<float *>(ws + w.sums);
-    // as many workgroups as fit the GPU at once
+    // as many workgroups as there is work for (a segment's fixed cost counts: 8
+    // requests of 100 tokens 8.0 us, without it 15.1) and as fit the GPU at once
     const int64_t room = kCUs * waves_per_simd(kDim, small / 16);
-    const int grid = (int)std::min(std::min<int64_t>(kGroups, room), std::max<int64_t>(8, keys / a.range_keys));
-    if (small == 16)
+    const int64_t work = (keys + (int64_t)a.batch.n * a.kv.kv_heads * kFixedKeys) / a.range_keys;
+    const int grid = (int)std::min(std::min<int64_t>(kGroups, room), std::max<int64_t>(8, work));
+    if (small == 16 && table <= kUncut && table > 512ll * a.batch.n)
+      start<kType, kDim, 1, kWide>(a, grid, cap, s);
+    else if (small == 16)
       start<kType, kDim, 1>(a, grid, cap, s);
     else if (small == 32)
       start<kType, kDim, 2>(a, grid, cap, s);
