@@ -144,7 +144,8 @@ struct Attention {
   int window;
   int64_t min_rows, max_rows;  // requests with min_rows < rows <= max_rows are taken
   int tile_tokens;         // tokens of one row tile
-  int atomic_keys;         // segments up to this long are not cut
+  // segments up to twice a workgroup's share are not cut, within these bounds
+  int least_keys, atomic_keys;
   int cut_keys;            // cuts are at multiples of this power of two, the tokens of a step
   int range_keys;          // least tokens of one workgroup, at least two steps
   Split *splits;           // [gridDim]
@@ -218,7 +219,7 @@ struct List {
 __host__ __device__ constexpr int list_bytes(int n) { return (20 * n + 8 + 15) & ~15; }
 
 // Where the range of cost `c` begins: a segment and a token of it.
-__device__ __forceinline__ Place locate(const Attention &a, const List &list, int n, long long c) {
+__device__ __forceinline__ Place locate(const Attention &a, const List &list, int n, int atomic_keys, long long c) {
   Place p = {n, 0, 0, 0};
   if (n == 0 || c >= list.before[n]) return p;
   int lo = 0, hi = n;  // before[lo] <= c < before[hi]
@@ -241,7 +242,7 @@ __device__ __forceinline__ Place locate(const Attention &a, const List &list, in
   p.tile = t0;
   left -= s.start(t0);
   const long long length = s.length(t0);
-  if (length > a.atomic_keys) {
+  if (length > atomic_keys) {
     p.key = (int)max(left - kFixedKeys, 0ll) & -a.cut_keys;
   } else if (2 * left >= length + kFixedKeys) {  // not cut: the nearer end
     p.tile = t0 + 1;
@@ -329,7 +330,9 @@ struct Range {
     const int w = groups >= 8 ? (block & 7) * (groups >> 3) + (block >> 3) : block;
     // lanes 0, 1, 2: this range's begin, its end, the one before's begin
     const int which = lane == 1 ? w + 1 : lane == 2 ? max(w - 1, 0) : w;
-    const Place found = locate(a, list, n, cut(total, which, groups));
+    const long long share = min(quotient(total, groups), (long long)a.atomic_keys);
+    const int atomic_keys = min(max(2 * (int)share, a.least_keys), a.atomic_keys);
+    const Place found = locate(a, list, n, atomic_keys, cut(total, which, groups));
     const Place at = uniform(found, 0), prev = uniform(found, 2);
     begin = at;
     end = uniform(found, 1);
@@ -1249,7 +1252,7 @@ int run(Attention a, char *ws, const Workspace &w, bool cap, float *block_weight
     a.tile_tokens = small / a.group > 0 ? small / a.group : 1;
     // Up to 512 tokens a cut costs more than it evens out (128 requests of 582
     // tokens on average, 64 heads: 57 us, with every cut made 64).
-    a.atomic_keys = table <= kUncut ? kUncut : 512;
+    a.least_keys = a.atomic_keys = table <= kUncut ? kUncut : 512;
     a.cut_keys = 32;
     a.range_keys = 256;
     a.splits = reinterpret_cast<Split *>(ws + w.splits);
@@ -1275,6 +1278,10 @@ int run(Attention a, char *ws, const Workspace &w, bool cap, float *block_weight
     a.min_rows = a.batch.n > 1 ? small : 0;
     a.max_rows = INT64_MAX;
     a.tile_tokens = tile_rows(kDim) / a.group;
+    // shorter ones are cut where there are few (64 rows of each of 8 KV heads, 2000
+    // tokens: 37 us, uncut 61), but not those of up to 16 stages (512 rows of 600
+    // tokens: 29 us, cut 35)
+    a.least_keys = 16 * stage_tokens(kDim);
     a.atomic_keys = 2048;
     a.cut_keys = stage_tokens(kDim);
     a.range_keys = 256;
@@ -1282,7 +1289,7 @@ int run(Attention a, char *ws, const Workspace &w, bool cap, float *block_weight
     a.parts = reinterpret_cast<float *>(ws + w.tile_parts);
     a.part_sums = reinterpret_cast<float *>(ws + w.tile_sums);
     start_tiles<kType, kDim>(a, cap, s);
-    if (table > a.atomic_keys)
+    if (table > a.least_keys)
       hipLaunchKernelGGL((join_kernel<kType, kDim>), dim3(kTileGroups, tile_rows(kDim) / (2 * kWaves)), dim3(kBlock),
                          0, s, a, tile_rows(kDim), 2);
   }
