@@ -71,3 +71,10 @@ def test_evict_most_requests(dev):
     assert op.kv_len_out.tolist() == e[0] and op.row_offsets_out.tolist() == e[1]
     assert op.slots_out[:len(e[2])].tolist() == e[2] and op.freed[:len(e[4])].tolist() == e[4]
     assert int(op.n_freed) == len(e[4])
+
+
+def test_few_row_tiles_are_cut(dev):
+    """Row tiles too few to fill the GPU, of lengths that many would leave whole."""
+    attend(dev, 7, 8, 4, 128, [70], [2000], window=3)
+    attend(dev, 8, 4, 2, 256, [138, 100], [753, 641])
+    attend(dev, 9, 4, 2, 64, [90, 1, 120], [1500, 1500, 1100], window=2, name="f16")
