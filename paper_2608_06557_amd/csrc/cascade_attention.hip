@@ -17,7 +17,7 @@
 // 2^8 times a row's length.
 //
 // Work is the list of (request, head, row tile) segments, each as long as
-// its last row sees tokens, cut into equal ranges of tokens, one per
+// its last row sees tokens, cut into ranges of equal cost, one per
 // workgroup.  Every workgroup derives the list from the batch's lengths by
 // itself (a scan), so ragged batches need neither a host plan nor another launch.  A
 // segment that one workgroup covers is written at once; parts of a cut one go
