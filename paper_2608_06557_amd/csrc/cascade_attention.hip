@@ -35,6 +35,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "attention_work.h"
 #include "cascade.h"
 #include "device_util.h"
 #include "kv_format.h"
@@ -124,12 +125,7 @@ struct Rows {
   int64_t token_stride, head_stride;  // bytes
 };
 
-// A cut segment: request, KV head, row tile, last workgroup with a part of it.
-struct Split {
-  int request, head, tile, last;
-};
-
-struct Attention {
+struct Attention : Cuts {
   KvView kv;
   cascade_kv_batch_t batch;
   const int32_t *row_offsets, *slots;
@@ -143,11 +139,6 @@ struct Attention {
   int log_shift;           // log2 of such a run
   int window;
   int64_t min_rows, max_rows;  // requests with min_rows < rows <= max_rows are taken
-  int tile_tokens;         // tokens of one row tile
-  // segments up to twice a workgroup's share are not cut, within these bounds
-  int least_keys, atomic_keys;
-  int cut_keys;            // cuts are at multiples of this power of two, the tokens of a step
-  int range_keys;          // least tokens of one workgroup, at least two steps
   Split *splits;           // [gridDim]
   float *parts;            // [gridDim][2][rows][kDim]
   float *part_sums;        // [gridDim][2][rows][2]: m and sum
@@ -169,94 +160,6 @@ __device__ __forceinline__ float *first_logs(const Attention &a, int first_entry
   return a.logs + ((int64_t)first_entry << (a.kv.block_shift - a.log_shift)) * a.window * a.q_heads;
 }
 
-// What a segment costs besides its tokens (its queries, first loads and
-// output), in tokens.  128 decode rows over caches up to 8192 tokens: 56 us,
-// without it 65; 128 to 512 are alike.  A 32 Ki token prefill in chunks: 1.87
-// ms, without it 1.98.
-constexpr int kFixedKeys = 256;
-
-// The segments of one request and KV head.
-struct Segments {
-  long long before;  // cached tokens that every row sees
-  int count, per;
-  __device__ __forceinline__ Segments(int len, int count, const Attention &a)
-      : before(len > count ? len - count : 0), count(count), per(a.tile_tokens) {}
-  __device__ __forceinline__ int tiles() const { return (count + per - 1) / per; }
-  // tokens that row tile t runs over
-  __device__ __forceinline__ long long length(int t) const {
-    return before + min((long long)(t + 1) * per, (long long)count);
-  }
-  // the costs of the tiles before t
-  __device__ __forceinline__ long long start(int t) const {
-    return t * (before + kFixedKeys) + (long long)per * ((long long)t * (t + 1) / 2);
-  }
-  __device__ __forceinline__ long long total() const {
-    const int t = tiles() - 1;
-    return start(t) + length(t) + kFixedKeys;
-  }
-};
-
-// floor(a / b) of whole numbers 0 <= a < 2^52, 0 < b: by doubles, whose
-// quotient is off by one at most
-__device__ __forceinline__ long long quotient(long long a, long long b) {
-  long long q = (long long)((double)a / (double)b);
-  const long long r = a - q * b;
-  return r < 0 ? q - 1 : r >= b ? q + 1 : q;
-}
-
-struct Place {
-  int item, head, tile, key;
-};
-
-// The list of requests with rows of a kernel's kind, in LDS.
-struct List {
-  long long *before;  // cost before each, and of all
-  int *ids, *len, *count;
-  __device__ __forceinline__ List(char *lds, int n)
-      : before(reinterpret_cast<long long *>(lds)), ids(reinterpret_cast<int *>(before + n + 1)), len(ids + n),
-        count(len + n) {}
-};
-__host__ __device__ constexpr int list_bytes(int n) { return (20 * n + 8 + 15) & ~15; }
-
-// Where the range of cost `c` begins: a segment and a token of it.
-__device__ __forceinline__ Place locate(const Attention &a, const List &list, int n, int atomic_keys, long long c) {
-  Place p = {n, 0, 0, 0};
-  if (n == 0 || c >= list.before[n]) return p;
-  int lo = 0, hi = n;  // before[lo] <= c < before[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (list.before[mid] <= c) lo = mid; else hi = mid;
-  }
-  p.item = lo;
-  const Segments s(list.len[lo], list.count[lo], a);
-  const long long per_head = s.total();
-  long long left = c - list.before[lo];
-  p.head = (int)quotient(left, per_head);
-  left -= p.head * per_head;
-  const int tiles = s.tiles();
-  int t0 = 0, t1 = tiles;  // start(t0) <= left < start(t1)
-  while (t1 - t0 > 1) {
-    const int mid = (t0 + t1) >> 1;
-    if (s.start(mid) <= left) t0 = mid; else t1 = mid;
-  }
-  p.tile = t0;
-  left -= s.start(t0);
-  const long long length = s.length(t0);
-  if (length > atomic_keys) {
-    p.key = (int)max(left - kFixedKeys, 0ll) & -a.cut_keys;
-  } else if (2 * left >= length + kFixedKeys) {  // not cut: the nearer end
-    p.tile = t0 + 1;
-    if (p.tile == tiles) {
-      p.tile = 0;
-      if (++p.head == a.kv.kv_heads) {
-        p.head = 0;
-        ++p.item;
-      }
-    }
-  }
-  return p;
-}
-
 // A lane's place, as wave-uniform numbers.
 __device__ __forceinline__ Place uniform(const Place &p, int lane = 0) {
   return {__builtin_amdgcn_readlane(p.item, lane), __builtin_amdgcn_readlane(p.head, lane),
@@ -266,13 +169,6 @@ __device__ __forceinline__ Place uniform(const Place &p, int lane = 0) {
 __device__ __forceinline__ long long first_lane(unsigned long long x) {
   const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)x);
   return (long long)((unsigned long long)__builtin_amdgcn_readfirstlane((unsigned)(x >> 32)) << 32 | lo);
-}
-
-// Where range w of `groups` begins: total w / groups, rounded down in two steps
-// whose products stay small.
-__device__ __forceinline__ long long cut(long long total, int w, int groups) {
-  const long long whole = quotient(total, groups);
-  return whole * w + (unsigned)((unsigned)(total - whole * groups) * (unsigned)w) / (unsigned)groups;
 }
 
 // The part of the work that a workgroup takes.
@@ -299,7 +195,7 @@ struct Range {
         } else {
           const int64_t rows = (int64_t)r.count * a.group;
           if (rows > a.min_rows && rows <= a.max_rows)
-            v[0] = Segments(r.len, r.count, a).total() * a.kv.kv_heads;
+            v[0] = Segments(r.len, r.count, a.tile_tokens).total() * a.kv.kv_heads;
         }
       }
       const unsigned long long cost = v[0];
@@ -320,8 +216,7 @@ struct Range {
 
     // this workgroup's range: neighbours in cost on one XCD (workgroups go to
     // the 8 XCDs in turn), where heads and row tiles of a request share its L2
-    const int cap = (int)min((long long)gridDim.x, quotient(total, a.range_keys));
-    const int groups = cap >= 8 ? cap & ~7 : max(cap, 1);
+    const int groups = ranges(a, total, gridDim.x);
     const int block = blockIdx.x;
     if (block >= groups || n == 0) {
       if (threadIdx.x == 0) a.splits[block] = Split{-1, 0, 0, 0};
@@ -330,30 +225,15 @@ struct Range {
     const int w = groups >= 8 ? (block & 7) * (groups >> 3) + (block >> 3) : block;
     // lanes 0, 1, 2: this range's begin, its end, the one before's begin
     const int which = lane == 1 ? w + 1 : lane == 2 ? max(w - 1, 0) : w;
-    const long long share = min(quotient(total, groups), (long long)a.atomic_keys);
-    const int atomic_keys = min(max(2 * (int)share, a.least_keys), a.atomic_keys);
-    const Place found = locate(a, list, n, atomic_keys, cut(total, which, groups));
+    const Place found =
+        locate(a, a.kv.kv_heads, list, n, uncut_keys(a, total, groups), cut(total, which, groups));
     const Place at = uniform(found, 0), prev = uniform(found, 2);
     begin = at;
     end = uniform(found, 1);
     items = n;
     group = w;
 
-    if (threadIdx.x == 0) {
-      Split s = {-1, 0, 0, 0};
-      const bool inside = at.key > 0 && !(prev.key > 0 && prev.item == at.item && prev.head == at.head &&
-                                          prev.tile == at.tile);
-      if (inside) {
-        const Segments seg(list.len[at.item], list.count[at.item], a);
-        const long long stop = list.before[at.item] + at.head * seg.total() + seg.start(at.tile) +
-                               seg.length(at.tile) + kFixedKeys;
-        // the last range that begins before `stop`
-        int end = min((int)quotient(stop, max(quotient(total, groups), 1ll)) + 1, groups - 1);
-        while (cut(total, end, groups) >= stop) --end;
-        s = {list.ids[at.item], at.head, at.tile, end};
-      }
-      a.splits[w] = s;
-    }
+    if (threadIdx.x == 0) a.splits[w] = first_cut(a, list, at, prev, total, groups);
     return true;
   }
 };
@@ -617,7 +497,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(kDim, kTiles)) void att
     at = uniform(at);  // the compiler does not see that it is
     const int id = __builtin_amdgcn_readfirstlane(list.ids[at.item]);
     const KvRequest req = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, id);
-    const Segments seg(req.len, req.count, a);
+    const Segments seg(req.len, req.count, a.tile_tokens);
     const int length = (int)seg.length(at.tile);
     const bool last = end.item == at.item && end.head == at.head && end.tile == at.tile;
     const int stop = last ? end.key : length;
@@ -829,7 +709,7 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
     at = uniform(at);  // the compiler does not see that it is
     const int id = __builtin_amdgcn_readfirstlane(list.ids[at.item]);
     const KvRequest req = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, id);
-    const Segments seg(req.len, req.count, a);
+    const Segments seg(req.len, req.count, a.tile_tokens);
     const int length = (int)seg.length(at.tile);
     const bool last = end.item == at.item && end.head == at.head && end.tile == at.tile;
     const int stop = last ? end.key : length;
