@@ -161,4 +161,14 @@ CASCADE_WORK_FN Split first_cut(const Cuts &a, const List &list, const Place &at
   return Split{list.ids[at.item], at.head, at.tile, end};
 }
 
+// The sub-blocks (16 tokens) of a request's tokens before `end`, which is above
+// 0: a segment that sees nothing has none, and its request may have no blocks.
+struct SubBlocks {
+  int shift, last;  // log2 of sub-blocks a block, last sub-block
+  CASCADE_WORK_FN SubBlocks(int block_shift, int end) : shift(block_shift - 4), last((end - 1) >> 4) {}
+  // table entry of sub-block `sub`, or of the last one, and its place in the block
+  CASCADE_WORK_FN int entry(int sub) const { return least(sub, last) >> shift; }
+  CASCADE_WORK_FN int within(int sub) const { return least(sub, last) & ((1 << shift) - 1); }
+};
+
 }  // namespace cascade

@@ -387,20 +387,18 @@ struct Rowset {
 
 // Where a request's head lies in the cache.
 template <int kDim>
-struct Cache {
+struct Cache : SubBlocks {
   const char *base;    // the head's codes in slot 0
   int64_t kv_stride, slot_stride, scales;  // `scales`: from the codes to the head's scale
   const int32_t *slots;
-  int num_slots, shift, last;  // log2 of sub-blocks a block, last sub-block
-  // of the tokens before `end`, a request's length at most
+  int num_slots;
+  // of the tokens before `end`, a request's length at most, and above 0
   __device__ __forceinline__ Cache(const Attention &a, const KvRequest &r, int head, int end)
-      : base(a.kv.base + ((int64_t)head << a.kv.block_shift) * kDim), kv_stride(a.kv.kv_stride),
-        slot_stride(a.kv.slot_stride),
+      : SubBlocks(a.kv.block_shift, end), base(a.kv.base + ((int64_t)head << a.kv.block_shift) * kDim),
+        kv_stride(a.kv.kv_stride), slot_stride(a.kv.slot_stride),
         scales(((int64_t)(a.kv.kv_heads - head) << a.kv.block_shift) * kDim + 4 * head),
-        slots(a.slots + r.row), num_slots(a.kv.num_slots), shift(a.kv.block_shift - 4),
-        last((end - 1) >> 4) {}
-  // table entry and slot of sub-block `sub`, or of the last one
-  __device__ __forceinline__ int entry(int sub) const { return min(sub, last) >> shift; }
+        slots(a.slots + r.row), num_slots(a.kv.num_slots) {}
+  // slot of sub-block `sub`, or of the last one
   __device__ __forceinline__ int slot(int sub) const { return uniform_load(slots + entry(sub)); }
   // from slot 0 to a slot
   __device__ __forceinline__ int64_t offset(int slot, bool &bad) const {
@@ -411,7 +409,7 @@ struct Cache {
   // the head's codes in a slot; one outside the pool counts as slot 0 and sets `bad`
   __device__ __forceinline__ const char *block(int slot, bool &bad) const { return base + offset(slot, bad); }
   // a sub-block within its block's codes
-  __device__ __forceinline__ int place(int sub) const { return (min(sub, last) & ((1 << shift) - 1)) * 16 * kDim; }
+  __device__ __forceinline__ int place(int sub) const { return within(sub) * 16 * kDim; }
   __device__ __forceinline__ const char *codes(const char *block, int sub) const { return block + place(sub); }
   __device__ __forceinline__ float k_scale(const char *block) const {
     return uniform_load(reinterpret_cast<const float *>(block + scales));
@@ -524,81 +522,84 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(kDim, kTiles)) void att
     const int clear_end = __builtin_amdgcn_readfirstlane(shown + first_token + 1);
     const int key_end = __builtin_amdgcn_readfirstlane(min(min(stop, req.len), shown + last_token + 1));
     const int len = __builtin_amdgcn_readfirstlane(req.len);
-    const Cache<kDim> cache(a, req, at.head, key_end);
-    // each wave takes every fourth 32 tokens, straight into registers: the next K
-    // codes are requested when these have been taken, V codes likewise, and the
-    // slots are known a step ahead of them.  No load hangs on a condition (a wait
-    // after the ways meet again would wait for too much): past the end the last
-    // sub-block is read again, from a cache.
-    constexpr int kStride = 32 * kWaves;
-    int key = __builtin_amdgcn_readfirstlane(at.key + 32 * wave);
-    Codes<kDim> c;
-    int slot[2];
-    auto look = [&](int key) {
-      slot[0] = cache.slot(key >> 4);
-      slot[1] = cache.slot((key >> 4) + 1);
-    };
-    look(key);
-    // the waves share the rows' q, which lies in operand order in LDS
-    constexpr int kQs = kTiles * (kDim / 32), kMine = (kQs + kWaves - 1) / kWaves;
-    u4 q[kMine];
+    // the same in all waves; a request may have no blocks where nothing is seen
+    if (at.key < key_end) {
+      const Cache<kDim> cache(a, req, at.head, key_end);
+      // each wave takes every fourth 32 tokens, straight into registers: the next K
+      // codes are requested when these have been taken, V codes likewise, and the
+      // slots are known a step ahead of them.  No load hangs on a condition (a wait
+      // after the ways meet again would wait for too much): past the end the last
+      // sub-block is read again, from a cache.
+      constexpr int kStride = 32 * kWaves;
+      int key = __builtin_amdgcn_readfirstlane(at.key + 32 * wave);
+      Codes<kDim> c;
+      int slot[2];
+      auto look = [&](int key) {
+        slot[0] = cache.slot(key >> 4);
+        slot[1] = cache.slot((key >> 4) + 1);
+      };
+      look(key);
+      // the waves share the rows' q, which lies in operand order in LDS
+      constexpr int kQs = kTiles * (kDim / 32), kMine = (kQs + kWaves - 1) / kWaves;
+      u4 q[kMine];
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-      const int e = min(i * kWaves + wave, kQs - 1), d = e % (kDim / 32);
-      const int row = e / (kDim / 32) * 16 + (lane & 15);
-      const int token = at.tile * a.tile_tokens + row / a.group, head = at.head * a.group + row % a.group;
-      const bool valid = row < tile_rows && token < req.count;
-      q[i] = *reinterpret_cast<const u4 *>(a.q.data + (int64_t)(req.first + (valid ? token : 0)) * a.q.token_stride +
-                                           (valid ? head : 0) * a.q.head_stride + 32 * g + 128 * (d >> 1) +
-                                           16 * (d & 1));
-      q[i] = valid ? (q[i] & a.keep) ^ a.flip : u4{0, 0, 0, 0};
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    c.fetch_k(cache, slot, key);
-    // K before V, as in the loop: waits count the loads that follow
-    __builtin_amdgcn_sched_barrier(0);
-    c.fetch_v(cache, slot, key);
-    __builtin_amdgcn_sched_barrier(0);
-    look(key + kStride);
-#pragma unroll
-    for (int i = 0; i < kMine; ++i)
-      *reinterpret_cast<u4 *>(qs + (min(i * kWaves + wave, kQs - 1) * 64 + lane) * 16) = q[i];
-    __syncthreads();
-    if (key < key_end) {
-      while (true) {
-        if (key + 32 > len) {
-          const unsigned live[2] = {live_bytes(key + 4 * g, len), live_bytes(key + 16 + 4 * g, len)};
-#pragma unroll
-          for (int i = 0; i < kDim / 64; ++i)
-#pragma unroll
-            for (int b = 0; b < 2; ++b) c.v[b][i] &= live[b];
-        }
-        f4 x[kTiles][2];
-        int q_at = lane * 16;
-        asm volatile("" : "+v"(q_at));  // or the loads of q move out of the loop, into registers
-        r.template scores<2>(
-            [&](int b, int d) {
-              const u4 w = c.k[b][d >> 1];
-              return widen8<kType>(w[2 * (d & 1)], w[2 * (d & 1) + 1], c.ks[b], c.ks[b]);
-            },
-            [&](int t, int d) {
-              return *reinterpret_cast<const v8 *>(qs + (t * (kDim / 32) + d) * 1024 + q_at);
-            },
-            x);
-        c.fetch_k(cache, slot, key + kStride);
-        v8 p[kTiles][1];
-        r.template weights<2>(a, x, p, key, len, key + 32 > clear_end, logs);
-        r.add(
-            [&](int d) {
-              return widen8<kType>(c.v[0][d >> 2][d & 3], c.v[1][d >> 2][d & 3], c.vs[0], c.vs[1]);
-            },
-            p);
-        c.fetch_v(cache, slot, key + kStride);
-        look(key + 2 * kStride);
-        key += kStride;
-        if (key >= key_end) break;
+      for (int i = 0; i < kMine; ++i) {
+        const int e = min(i * kWaves + wave, kQs - 1), d = e % (kDim / 32);
+        const int row = e / (kDim / 32) * 16 + (lane & 15);
+        const int token = at.tile * a.tile_tokens + row / a.group, head = at.head * a.group + row % a.group;
+        const bool valid = row < tile_rows && token < req.count;
+        q[i] = *reinterpret_cast<const u4 *>(a.q.data + (int64_t)(req.first + (valid ? token : 0)) * a.q.token_stride +
+                                             (valid ? head : 0) * a.q.head_stride + 32 * g + 128 * (d >> 1) +
+                                             16 * (d & 1));
+        q[i] = valid ? (q[i] & a.keep) ^ a.flip : u4{0, 0, 0, 0};
       }
-      if (c.bad) kv_report(a.status);
+      __builtin_amdgcn_sched_barrier(0);
+      c.fetch_k(cache, slot, key);
+      // K before V, as in the loop: waits count the loads that follow
+      __builtin_amdgcn_sched_barrier(0);
+      c.fetch_v(cache, slot, key);
+      __builtin_amdgcn_sched_barrier(0);
+      look(key + kStride);
+#pragma unroll
+      for (int i = 0; i < kMine; ++i)
+        *reinterpret_cast<u4 *>(qs + (min(i * kWaves + wave, kQs - 1) * 64 + lane) * 16) = q[i];
+      __syncthreads();
+      if (key < key_end) {
+        while (true) {
+          if (key + 32 > len) {
+            const unsigned live[2] = {live_bytes(key + 4 * g, len), live_bytes(key + 16 + 4 * g, len)};
+#pragma unroll
+            for (int i = 0; i < kDim / 64; ++i)
+#pragma unroll
+              for (int b = 0; b < 2; ++b) c.v[b][i] &= live[b];
+          }
+          f4 x[kTiles][2];
+          int q_at = lane * 16;
+          asm volatile("" : "+v"(q_at));  // or the loads of q move out of the loop, into registers
+          r.template scores<2>(
+              [&](int b, int d) {
+                const u4 w = c.k[b][d >> 1];
+                return widen8<kType>(w[2 * (d & 1)], w[2 * (d & 1) + 1], c.ks[b], c.ks[b]);
+              },
+              [&](int t, int d) {
+                return *reinterpret_cast<const v8 *>(qs + (t * (kDim / 32) + d) * 1024 + q_at);
+              },
+              x);
+          c.fetch_k(cache, slot, key + kStride);
+          v8 p[kTiles][1];
+          r.template weights<2>(a, x, p, key, len, key + 32 > clear_end, logs);
+          r.add(
+              [&](int d) {
+                return widen8<kType>(c.v[0][d >> 2][d & 3], c.v[1][d >> 2][d & 3], c.vs[0], c.vs[1]);
+              },
+              p);
+          c.fetch_v(cache, slot, key + kStride);
+          look(key + 2 * kStride);
+          key += kStride;
+          if (key >= key_end) break;
+        }
+        if (c.bad) kv_report(a.status);
+      }
     }
 
 #pragma unroll

@@ -67,6 +67,19 @@ int main(int argc, char **argv) {
       if (last && stop == at.key) break;
       CHECK(at.key <= stop && stop <= length);
       const Key key(list.ids[at.item], at.head, at.tile);
+      // the look-ups of few rows (8 waves, 32 tokens each, two steps ahead) and of
+      // row tiles (a sub-block to a wave, two stages ahead), made where there are tokens
+      const int blocks = (list.len[at.item] + block - 1) / block;
+      if (at.key < stop) {
+        const SubBlocks subs(__builtin_ctz(block), stop);
+        for (int k = at.key; k <= stop + 3 * 256; k += 16) {
+          CHECK(subs.entry(k >> 4) >= 0 && subs.entry(k >> 4) < blocks);
+          CHECK(subs.within(k >> 4) >= 0 && subs.within(k >> 4) < block / 16);
+        }
+        CHECK(subs.entry((stop - 1) >> 4) == (stop - 1) / block);
+      } else {
+        CHECK(stop == 0 && SubBlocks(__builtin_ctz(block), stop).entry(0) < 0);  // not to be looked up
+      }
       if (at.key == 0 && stop == length) ++whole[key];
       else parts[key].push_back(Part{w, at.key, stop});
       if (last) break;
@@ -149,4 +162,15 @@ def test_more_new_tokens_than_cached_ones(walk, rule):
         for heads in (1, 8):
             for group in (1, 4):
                 walk(rule, [count], [length], heads, group)
-                walk(rule, [3, count, 1], [0, length, 40], heads, group)
+                walk(rule, [3, count, 1], [0, length, 40], heads, group, 32)
+
+
+@pytest.mark.parametrize("rule", list(RULES))
+def test_nothing_is_looked_up_where_nothing_is_seen(walk, rule):
+    """Batches of requests without cached tokens, the first one among them,
+    with and without a table."""
+    for block in (16, 128):
+        walk(rule, [1], [0], 8, 8, block)
+        walk(rule, [64], [0], 2, 1, block)
+        walk(rule, [5, 1, 2], [0, 0, 0], 2, 4, block)
+        walk(rule, [5, 1, 70], [0, 17, 30], 2, 4, block)
