@@ -609,8 +609,9 @@ int cascade_rope_frequencies(const cascade_rope_spec_t *spec, uint64_t *freq, fl
    A pool slot may be written for one request only: blocks that requests
    share hold no new tokens.  Requests outside the domain above, slots
    outside [0, num_slots) and negative positions set *status_dev =
-   CASCADE_EINVAL and are not written; a NaN or infinite key or value sets it too and
-   is stored as 0 (status_dev may be NULL).  Returns CASCADE_EINVAL for NULL
+   CASCADE_EINVAL and are not written (of a negative position neither the
+   query nor the new keys and values of its block); a NaN or infinite key or
+   value sets it too and is stored as 0 (status_dev may be NULL).  Returns CASCADE_EINVAL for NULL
    pointers, formats, sizes, strides or alignments outside the domain, CASCADE_EHIP on a
    failed launch. */
 int cascade_kv_append(const cascade_kv_pool_t *pool, int32_t layer,

@@ -168,16 +168,16 @@ __device__ __forceinline__ void rotate_queries(const Append &a) {
   const int64_t row = id / kUnits;
   const int t = (int)(row / a.q_heads), h = (int)(row % a.q_heads);
   if (t >= a.batch.n_tokens) return;
-  int p = 0;
-  if (a.rope.dim) {
-    p = a.rope.positions[t];
-    if (p < 0) kv_report(a.status);
-  }
+  const int p = a.rope.dim ? a.rope.positions[t] : 0;
   int da, db;
   unit_dims(a.rope, u, da, db);
   float x[8], y[8];
   widen<kType>(load_row(a.q, t, h, da), x);
   widen<kType>(load_row(a.q, t, h, db), y);
+  if (p < 0) {
+    kv_report(a.status);
+    return;
+  }
   rotate_unit(a.rope, u, p, x, y);
   char *out = a.q_out.data + t * a.q_out.token_stride + h * a.q_out.head_stride;
   *reinterpret_cast<u4 *>(out + 2 * da) = narrow<kType>(x);
@@ -334,7 +334,7 @@ __global__ __launch_bounds__(kBlock) void append_kernel(Append a) {
       if (t == r.first || o == 0) {  // otherwise the run began in an earlier group
         const int slot = a.slots[r.row + (at >> a.kv.block_shift)];
         bool fine = slot >= 0 && slot < a.kv.num_slots;
-        if (a.rope.dim && side == 0)
+        if (a.rope.dim)
           for (int j = lane_id(); j < m; j += 64) fine &= a.rope.positions[t + j] >= 0;
         if (__all(fine))
           write_run<kType, kDim>(a, t, m, o, slot, head, side, tiles[wave_id()]);
