@@ -301,10 +301,18 @@ __device__ __forceinline__ void write_run(const Append &a, int t, int m, int o, 
   if (lane == 0 && (o == 0 || grew)) *scale_at = scale;
 }
 
+__device__ __forceinline__ bool writable(const KvRequest &r) { return r.ok && r.len >= r.count; }
+
 template <int kType, int kDim>
 __global__ __launch_bounds__(kBlock) void append_kernel(Append a) {
   if ((int)blockIdx.x < a.q_blocks) {
     rotate_queries<kType, kDim>(a);
+    return;
+  }
+  if (blockIdx.x == gridDim.x - 1) {
+    // the others meet only requests with new tokens
+    for (int i = threadIdx.x; i < a.batch.n; i += kBlock)
+      if (!writable(kv_request(a.batch, a.row_offsets, a.kv.block_shift, i))) kv_report(a.status);
     return;
   }
   __shared__ __align__(16) char tiles[kWaves][16 * kDim];
@@ -322,10 +330,7 @@ __global__ __launch_bounds__(kBlock) void append_kernel(Append a) {
   const int bt = 1 << a.kv.block_shift;
   for (int i = (int)ended[0], t = t0; t < t1 && i < a.batch.n; ++i) {
     const KvRequest r = kv_request(a.batch, a.row_offsets, a.kv.block_shift, i);
-    if (!r.ok || r.len < r.count) {
-      kv_report(a.status);
-      continue;
-    }
+    if (!writable(r)) continue;
     t = max(t, r.first);
     while (t < t1 && t < r.first + r.count) {
       const int at = r.len - r.count + (t - r.first);  // cache index
@@ -407,13 +412,14 @@ extern "C" int cascade_kv_append(const cascade_kv_pool_t *pool, int32_t layer,
   const int64_t q_blocks = (units + kBlock - 1) / kBlock;
   const int64_t kv_blocks = (int64_t)((batch->n_tokens + a.group - 1) / a.group) *
                             ((2 * format->kv_heads + kWaves - 1) / kWaves);
-  if (q_blocks + kv_blocks > INT32_MAX / kBlock) return CASCADE_EINVAL;
+  const int64_t blocks = q_blocks + kv_blocks + 1;  // the last one checks the batch
+  if (blocks > INT32_MAX / kBlock) return CASCADE_EINVAL;
   a.q_blocks = (int)q_blocks;
   const auto s = static_cast<hipStream_t>(stream);
   if (dtype == CASCADE_BF16)
-    launch<CASCADE_BF16>(a, (int)(q_blocks + kv_blocks), format->head_dim, s);
+    launch<CASCADE_BF16>(a, (int)blocks, format->head_dim, s);
   else
-    launch<CASCADE_F16>(a, (int)(q_blocks + kv_blocks), format->head_dim, s);
+    launch<CASCADE_F16>(a, (int)blocks, format->head_dim, s);
   return hipGetLastError() == hipSuccess ? CASCADE_OK : CASCADE_EHIP;
 }
 

@@ -1,5 +1,5 @@
-"""cascade_kv_append where positions are negative: what is reported, and what is
-left as it was."""
+"""cascade_kv_append where positions are negative or requests without new
+tokens are outside the domain: what is reported, and what is left as it was."""
 import numpy as np
 import pytest
 import torch
@@ -52,3 +52,35 @@ def test_negative_positions_are_not_written(dev, inter):
     for slot in range(b["pool"]):
         want = pool[0, :, slot].cuda() if slot in bad_slots else got[0][1][:, slot]
         assert torch.equal(got[1][1][:, slot], want), slot
+
+
+@pytest.mark.parametrize("fault", ["length", "long", "row", "row end", "offsets"])
+@pytest.mark.parametrize("at", [0, 1, 3])
+def test_bad_requests_without_new_tokens_are_reported(dev, fault, at):
+    rng = np.random.default_rng(2)
+    h, d, bt = 2, 64, 16
+    counts = [1, 1, 2, 1]
+    counts[at] = 0
+    b = ref.batch(rng, counts, [20, 21, 22, 30], bt)
+    pool = ref.random_pool(rng, 1, b["pool"], h, d, bt)
+    k = rows(rng, b["tokens"], h, d, torch.bfloat16).cuda()
+    g = on_gpu(b)
+    if fault == "length":
+        g["len"][at] = -1
+    elif fault == "long":
+        g["len"][at] = 33
+    elif fault == "row":
+        g["rows"][at] = -1
+    elif fault == "row end":
+        g["rows"][at + 1] = 1 << 30
+    else:
+        g["off"][at + 1] -= 1
+    kv = dev.DeviceKvPool(pool.cuda(), h, d, bt)
+    dev.DeviceKvAppend(kv, make_batch(dev, g), None, k, k).run()
+    with pytest.raises(RuntimeError):
+        kv.check()
+    if fault in ("length", "long"):  # otherwise a neighbour is bad too
+        clean = dev.DeviceKvPool(pool.cuda(), h, d, bt)
+        dev.DeviceKvAppend(clean, make_batch(dev, on_gpu(b)), None, k, k).run()
+        clean.check()
+        assert torch.equal(kv.pool, clean.pool)
