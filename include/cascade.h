@@ -519,7 +519,9 @@ int cascade_tier_reclaim_chain(const cascade_tier_chain_t *chain, void *index,
      K  ((d / 64) * 16 + t) * 64 + d % 64
      V  (((d / 64) * 4 + t / 4) * 16 + d % 16) * 16 + (d % 64) / 16 * 4 + t % 4
    A power of two makes a code's value exact in bfloat16 and lets a block's
-   scale grow by exact steps.  The pool's chunk_bytes is at least
+   scale grow by exact steps; what float16 rows cannot hold of it is applied in
+   32 bits, so that rows of either type read any cache (values over 2^90 may
+   overflow the sums).  The pool's chunk_bytes is at least
    cascade_kv_chunk_bytes(format).  Places past a request's last token may
    hold anything, NaN codes included; codes before it must be finite, as
    cascade_kv_append leaves them. */

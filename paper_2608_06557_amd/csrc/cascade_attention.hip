@@ -10,7 +10,8 @@
 // where the second wants its weights, so P never moves between lanes, and m is
 // a scalar per lane.  K and V codes come straight from the cache in operand
 // order, 16 bytes a lane, and are widened by the scaled FP8 conversion, which
-// applies the block's power-of-two scale exactly.
+// applies the block's power-of-two scale exactly (in float16 as much of it as
+// the type holds, the rest in 32 bits: Units).
 //
 // m follows the row's maximum only when a score exceeds it by 2^8: most tiles
 // then rescale nothing and need no exchange between lanes; sums stay below
@@ -59,6 +60,7 @@ constexpr float kSlack = 8.f;  // a row's m lags its maximum by at most this (lo
 
 template <int kType> struct El;
 template <> struct El<CASCADE_BF16> {
+  static constexpr bool kBounded = false;  // holds a code times any scale
   typedef bf2 v2;
   typedef bf8 v8;
   static __device__ __forceinline__ unsigned widen_lo(unsigned w, float s) {
@@ -79,6 +81,7 @@ template <> struct El<CASCADE_BF16> {
   }
 };
 template <> struct El<CASCADE_F16> {
+  static constexpr bool kBounded = true;
   typedef h2 v2;
   typedef h8 v8;
   static __device__ __forceinline__ unsigned widen_lo(unsigned w, float s) {
@@ -119,6 +122,43 @@ __device__ __forceinline__ unsigned narrow2(float a, float b) {
 __device__ __forceinline__ float evened(float sum, float used) {
   return used > 0.f && used < __builtin_inff() ? sum / used : 1.f;
 }
+
+// A block's scale as the part that the conversion applies and the rest, for
+// 32 bits.  float16 holds every code times 2^-15 (the least is 2^-24) to 2^7 (the
+// largest is 57344); beyond, keys' scores are multiplied by the rest, and O is
+// kept in units of it while a block's values are added.  Asking whether there is
+// a rest costs float16 rows, of bfloat16's times: 32 requests with draft rows
+// 117.9 us against 117.1, 4 of 115 Ki tokens 185 against 182, row tiles 1 to 2 %
+// (of 256 dims 22 %: the compiler moves more of O between its register files).
+__device__ __forceinline__ float applied(float scale, float &rest) {
+  const int bits = __builtin_bit_cast(int, scale), held = min(max(bits, (127 - 15) << 23), (127 + 7) << 23);
+  rest = __builtin_bit_cast(float, bits - held + (127 << 23));
+  return __builtin_bit_cast(float, held);
+}
+// Of values a rest under 2^-24 counts as that: they are under 2^-30, and a
+// result's last place is 2^-24.  So O over a rest stays finite unless the result
+// is over the type's largest anyway.
+__device__ __forceinline__ float unit_of(float rest) { return fmaxf(rest, 0x1p-24f); }
+__device__ __forceinline__ float inverse_unit(float unit) {  // of a power of two
+  return __builtin_bit_cast(float, (254 << 23) - __builtin_bit_cast(int, unit));
+}
+// The scales of the two sub-blocks of a step.
+template <int kType>
+struct Units {
+  float scale[2], rest[2];
+  bool odd = false;  // a rest is not 1
+  __device__ __forceinline__ Units(const float (&s)[2]) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      scale[b] = s[b];
+      if (El<kType>::kBounded) {
+        const float held = applied(s[b], rest[b]);  // the same in all lanes
+        scale[b] = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, held)));
+        odd |= __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, rest[b])) != 127 << 23;
+      }
+    }
+  }
+};
 
 struct Rows {
   char *data;
@@ -383,6 +423,13 @@ struct Rowset {
       for (int t = 0; t < kTiles; ++t) o[t][d] = El<kType>::mfma(x, p[t][0], o[t][d]);
     }
   }
+
+  __device__ __forceinline__ void scale_o(float f) {
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int d = 0; d < kDim / 16; ++d) o[t][d] *= f;
+  }
 };
 
 // Where a request's head lies in the cache.
@@ -576,23 +623,50 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(kDim, kTiles)) void att
           f4 x[kTiles][2];
           int q_at = lane * 16;
           asm volatile("" : "+v"(q_at));  // or the loads of q move out of the loop, into registers
+          const Units<kType> ku(c.ks);
           r.template scores<2>(
               [&](int b, int d) {
                 const u4 w = c.k[b][d >> 1];
-                return widen8<kType>(w[2 * (d & 1)], w[2 * (d & 1) + 1], c.ks[b], c.ks[b]);
+                return widen8<kType>(w[2 * (d & 1)], w[2 * (d & 1) + 1], ku.scale[b], ku.scale[b]);
               },
               [&](int t, int d) {
                 return *reinterpret_cast<const v8 *>(qs + (t * (kDim / 32) + d) * 1024 + q_at);
               },
               x);
+          if (__builtin_expect(ku.odd, false)) {
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+              for (int b = 0; b < 2; ++b) x[t][b] *= ku.rest[b];
+          }
           c.fetch_k(cache, slot, key + kStride);
           v8 p[kTiles][1];
           r.template weights<2>(a, x, p, key, len, key + 32 > clear_end, logs);
-          r.add(
-              [&](int d) {
-                return widen8<kType>(c.v[0][d >> 2][d & 3], c.v[1][d >> 2][d & 3], c.vs[0], c.vs[1]);
-              },
-              p);
+          const Units<kType> vu(c.vs);
+          // at once, or sub-block by sub-block where their values have rests
+          v8 part[kTiles][1];
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) part[t][0] = p[t][0];
+          for (int b = 0;; ++b) {
+            if (__builtin_expect(vu.odd, false)) {
+              r.scale_o(inverse_unit(unit_of(vu.rest[b])));
+#pragma unroll
+              for (int t = 0; t < kTiles; ++t) {
+                u4 w = __builtin_bit_cast(u4, p[t][0]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = i / 2 == b ? w[i] : 0;
+                part[t][0] = __builtin_bit_cast(v8, w);
+              }
+            }
+            float s0 = vu.scale[0], s1 = vu.scale[1];
+            if (El<kType>::kBounded) asm volatile("" : "+s"(s0), "+s"(s1));  // or all of V is widened before the loop
+            r.add(
+                [&](int d) { return widen8<kType>(c.v[0][d >> 2][d & 3], c.v[1][d >> 2][d & 3], s0, s1); },
+                part);
+            if (__builtin_expect(!vu.odd, true)) break;
+            r.scale_o(unit_of(vu.rest[b]));
+            if (b) break;
+          }
           c.fetch_v(cache, slot, key + kStride);
           look(key + 2 * kStride);
           key += kStride;
@@ -687,6 +761,10 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(kDim, kTiles)) void att
 constexpr int stage_tokens(int dim) { return dim == 256 ? 32 : 64; }
 constexpr int tile_waves(int dim) { return 2 * stage_tokens(dim) / 16; }
 constexpr int tile_rows(int dim) { return 32 * tile_waves(dim); }
+// of LDS: K, V, and what of their scales the type does not hold
+constexpr int stage_bytes(int type, int dim) {
+  return stage_tokens(dim) * dim * 4 + (type == CASCADE_F16 ? stage_tokens(dim) / 16 * 8 : 0);
+}
 template <int kType, int kDim, bool kCap>
 __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void tile_kernel(Attention a) {
   typedef El<kType> E;
@@ -694,6 +772,7 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
   constexpr int kSlices = kDim / 64, kOut = kDim / 32, kTW = tile_waves(kDim);
   constexpr int kStage = stage_tokens(kDim), kSubs = kStage / 16, kHalves = kStage / 32;
   constexpr int kSide = kStage * kDim * 2;  // bytes of a stage's K or V operands
+  constexpr bool kBounded = E::kBounded;
   extern __shared__ __align__(16) char lds[];
   __shared__ unsigned long long scan[2 * kTW];
   const List list(lds, a.batch.n);
@@ -777,6 +856,12 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
       const int own_place = (sub >> 1) * kHalf + (side ? kSide + ((sub & 1) * kOut * 64 + 32 * (lane >> 4 & 1) + (lane & 15)) * 16 + 8 * (lane >> 5)
                                                       : ((lane >> 4) * 64 + 16 * (sub & 1) + (lane & 15)) * 16);
       auto put = [&](char *to) {
+        float scale = own_scale;
+        if (kBounded) {
+          float rest;
+          scale = applied(own_scale, rest);
+          if (lane == 0) reinterpret_cast<float *>(to + 2 * kSide)[side * kSubs + sub] = rest;
+        }
         to += own_place;
         if (side == 0) {
 #pragma unroll
@@ -784,7 +869,7 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
 #pragma unroll
             for (int h = 0; h < 2; ++h)
               *reinterpret_cast<v8 *>(to + (4 * c * 64 + 32 * h) * 16) =
-                  widen8<kType>(own[c][2 * h], own[c][2 * h + 1], own_scale, own_scale);
+                  widen8<kType>(own[c][2 * h], own[c][2 * h + 1], scale, scale);
         } else {
           if (own_key + 16 > len) {  // codes past the end may be anything
             const unsigned live = live_bytes(own_key + 4 * (lane >> 4), len);
@@ -796,7 +881,7 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
 #pragma unroll
             for (int j = 0; j < 4; ++j)
               *reinterpret_cast<u2 *>(to + ((2 * c + (j >> 1)) * 64 + 16 * (j & 1)) * 16) =
-                  u2{E::widen_lo(own[c][j], own_scale), E::widen_hi(own[c][j], own_scale)};
+                  u2{E::widen_lo(own[c][j], scale), E::widen_hi(own[c][j], scale)};
         }
       };
       v8 kop[kDim / 16], vop[2][kOut];
@@ -881,13 +966,24 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
           }
         }
       };
-      auto add = [&](const v8 (&p)[2]) {
+      // what a stage's scales leave to 32 bits
+      auto rest = [&](const char *from, int side, int sub) {
+        return reinterpret_cast<const float *>(from + 2 * kSide)[side * kSubs + sub];
+      };
+      auto scale_o = [&](float f) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int d = 0; d < kOut; ++d) o[d] *= f;
+      };
+      auto add = [&](const v8 (&p)[2], const char *from, int h, bool apart) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          if (__builtin_expect(apart, false)) scale_o(inverse_unit(unit_of(rest(from, 1, 2 * h + u))));
 #pragma unroll
           for (int d = 0; d < kOut; ++d) o[d] = E::mfma(vop[u][d], p[u], o[d]);
+          if (__builtin_expect(apart, false)) scale_o(unit_of(rest(from, 1, 2 * h + u)));
+        }
       };
-      char *from = stages, *to = stages + 2 * kSide;
+      char *from = stages, *to = stages + stage_bytes(kType, kDim);
       look(first_key);
       fetch(first_key);
       put(from);
@@ -896,10 +992,19 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
       for (int key = first_key; key < block_end; key += kStage) {
         f16v x[kHalves];
         v8 p[kHalves][2];
+        // a lane for each of the stage's, K's and V's
+        const float any_rest = kBounded ? rest(from, 0, lane % (2 * kSubs)) : 1.f;
 #pragma unroll
         for (int h = 0; h < kHalves; ++h) {
           load_k(from, h);
           scores(x[h]);
+        }
+        const unsigned odd = kBounded ? (unsigned)__ballot(any_rest != 1.f) : 0;
+        if (__builtin_expect(odd & ((1u << kSubs) - 1), 0)) {
+#pragma unroll
+          for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[h][i] *= rest(from, 0, 2 * h + (i >> 3));
         }
         load_v(from, 0);
 #pragma unroll
@@ -909,10 +1014,11 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
         for (int h = 0; h < kHalves; ++h) weigh(x[h], p[h], key + 32 * h);
         put(to);
         fetch(key + 2 * kStage);
-        add(p[0]);
+        const bool apart = odd >> kSubs & ((1u << kSubs) - 1);
+        add(p[0], from, 0, apart);
         if (kHalves > 1) {
           load_v(from, kHalves - 1);
-          add(p[kHalves - 1]);
+          add(p[kHalves - 1], from, kHalves - 1, apart);
         }
         __syncthreads();
         char *const was = from;
@@ -1115,7 +1221,7 @@ template <int kType, int kDim>
 void start_tiles(const Attention &a, bool cap, hipStream_t stream) {
   auto kernel = cap ? tile_kernel<kType, kDim, true> : tile_kernel<kType, kDim, false>;
   hipLaunchKernelGGL(kernel, dim3(kTileGroups), dim3(64 * tile_waves(kDim)),
-                     list_bytes(a.batch.n) + 2 * stage_tokens(kDim) * kDim * 4, stream, a);
+                     list_bytes(a.batch.n) + 2 * stage_bytes(kType, kDim), stream, a);
 }
 
 template <int kType, int kDim>
