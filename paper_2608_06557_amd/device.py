@@ -507,12 +507,12 @@ class DeviceAttention:
         self.kv, self.batch, self.layer = kv, batch, layer
         self.tensors = (q, out, lse, block_weight)
         heads, f32 = q.shape[1], torch.float32
+        weighs = block_weight is not None and batch.c_batch.n_entries > 0  # or nothing to add to
         self.c_args = cx.Attention(
             _dtype(q), heads, scale, softcap, kv_rows(q), kv_rows(out),
             None if lse is None else _check_array(lse, f32, batch.tokens * heads, "lse"),
-            None if block_weight is None else
-            _check_array(block_weight, f32, batch.c_batch.n_entries, "block_weight"),
-            weight_window if block_weight is not None else 0)
+            _check_array(block_weight, f32, batch.c_batch.n_entries, "block_weight") if weighs else None,
+            weight_window if weighs else 0)
         self.ws_bytes = cx.cascade_attention_workspace_bytes(kv.c_format, batch.c_batch, heads,
                                                              self.c_args.weight_window)
         if self.ws_bytes == 0:

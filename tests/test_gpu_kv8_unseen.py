@@ -63,3 +63,8 @@ def test_nothing_in_front_of_the_table_counts(dev):
     e = ref.attend(pool[0], q, b, h, d, bt, 0.1)
     got = run_attention(dev, pool.cuda(), q.cuda(), dict(g, slots=held[8:]), h, d, bt, 0.1)
     check_attention(got, e, "bf16", d, 0)
+
+
+def test_weights_of_an_empty_table(dev):
+    """Block weights asked for where no request has a block."""
+    attend(dev, 5, 4, 2, 64, [3, 1], [0, 0], window=2)
