@@ -403,6 +403,14 @@ def _check_array(t, dtype, size: int, name: str) -> int:
     return t.data_ptr()
 
 
+def _check_device(device, *tensors) -> None:
+    """Addresses of another device's memory, or the host's, would be read as
+    this one's."""
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"a tensor lies on {t.device}, not {device}")
+
+
 class DeviceKvPool:
     """A pool of the 8-bit cache over a byte tensor [layers, 2 (K, V), slots,
     bytes]; the last dimension holds at least a chunk and may be padded."""
@@ -442,6 +450,7 @@ class KvBatch:
         i32 = _torch().int32
         n = int(kv_len.numel())
         self.tensors = (token_offsets, kv_len, row_offsets, slots)
+        _check_device(kv_len.device, *self.tensors)
         self.n, self.tokens = n, int(tokens)
         self.c_batch = cx.KvBatch(n, tokens, most_new, slots.numel(),
                                   _check_array(token_offsets, i32, n + 1, "token_offsets"),
@@ -475,6 +484,7 @@ class DeviceKvAppend:
                 raise ValueError("rows do not fit the batch, the heads or each other")
         self.kv, self.batch, self.layer = kv, batch, layer
         self.tensors = (q, k, v, q_out, positions, freq)
+        _check_device(kv.pool.device, *self.tensors, *batch.tensors)
         self.dtype, self.q_heads = _dtype(k), 0 if q is None else q.shape[1]
         self.c_rows = [None if t is None else kv_rows(t) for t in (q, q_out, k, v)]
         self.c_rope, self.positions = None, None
@@ -506,6 +516,7 @@ class DeviceAttention:
             raise ValueError("q and out do not fit the batch, the pool or each other")
         self.kv, self.batch, self.layer = kv, batch, layer
         self.tensors = (q, out, lse, block_weight)
+        _check_device(kv.pool.device, *self.tensors, *batch.tensors, workspace)
         heads, f32 = q.shape[1], torch.float32
         weighs = block_weight is not None and batch.c_batch.n_entries > 0  # or nothing to add to
         self.c_args = cx.Attention(
@@ -545,6 +556,7 @@ class DeviceKvEvict:
             out = (new(n), new(n + 1), new(entries), new(entries, torch.float32), new(entries),
                    new(1))
         self.tensors = (kv_len, row_offsets, slots, block_weight, keep_blocks)
+        _check_device(kv_len.device, *self.tensors, *out)
         self.kv_len_out, self.row_offsets_out, self.slots_out = out[:3]
         self.weight_out, self.freed, self.n_freed = out[3:]
         p = _check_array
