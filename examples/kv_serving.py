@@ -124,8 +124,7 @@ class Server:
         op = dev.DeviceKvEvict(self.block, self.length, self.entries, self.slots, self.weight,
                                self.i32([self.budget] * len(live)), sink=1, recent=2)
         op.run()
-        if int(op.status):
-            raise RuntimeError(cx.cascade_strerror(int(op.status)))
+        op.check()
         at, kept = op.row_offsets_out.tolist(), op.slots_out.tolist()
         gone = op.freed[:int(op.n_freed)].tolist()
         for i, (r, length) in enumerate(zip(live, op.kv_len_out.tolist())):

@@ -575,3 +575,7 @@ class DeviceKvEvict:
 
     def run(self, stream=None) -> None:
         _raise(self._call(stream_handle(stream)))
+
+    def check(self) -> None:
+        """Synchronise and raise if a call found bad device data."""
+        _raise(int(self.status.item()))

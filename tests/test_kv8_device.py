@@ -66,3 +66,12 @@ def test_tensors_of_another_device_are_refused():
     for i in range(5):
         with pytest.raises(ValueError):
             device.DeviceKvEvict(16, *[t.to(elsewhere) if j == i else t for j, t in enumerate(args)])
+
+
+def test_an_eviction_is_checked_as_the_pool_is():
+    op = device.DeviceKvEvict(16, i32(2), i32(0, 1), i32(1), torch.zeros(1), i32(1))
+    op.check()
+    for code in (cx.EINVAL, cx.ENOSPC):
+        op.status.fill_(code)
+        with pytest.raises(RuntimeError, match=cx.cascade_strerror(code)):
+            op.check()
