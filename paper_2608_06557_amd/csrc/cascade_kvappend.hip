@@ -407,8 +407,16 @@ extern "C" int cascade_kv_append(const cascade_kv_pool_t *pool, int32_t layer,
   a.q_heads = q_heads;
   a.status = status_dev;
   const int64_t units = q ? (int64_t)batch->n_tokens * q_heads * (format->head_dim / 16) : 0;
-  // few tokens: a workgroup for each, so that every run has a wave of its own
-  a.group = batch->n_tokens <= 512 ? 1 : 16;
+  // A wave takes the runs that begin in a group's tokens one after another, and a
+  // workgroup looks at its group's request first.  So groups are small where runs
+  // are short, or few in all.  Groups of 1, 4 and 16 tokens take, in us, for
+  //   single tokens, 64 query heads: 128 of them 7.0, 15.5, 50.6; 512 18, 22, 58;
+  //     640 23, 26, 63; 1024 36, 31, 77; 2048 70, 58, 91
+  //   chunks of 512 tokens: one 13.4, 7.6, 7.2; 16 130, 59, 44
+  //   of 16: 4 of them 6.1, 5.9, 8.5; 32 13.5, 10.6, 10.0; 100 35, 23, 16
+  //   of 12: 16 of them 7.1, 9.0, 12.1; 128 30, 18, 19
+  const bool few = batch->n_tokens <= 512, runs = batch->n_tokens >= 16ll * batch->n;
+  a.group = few ? (runs ? 4 : 1) : (runs ? 16 : 4);
   const int64_t q_blocks = (units + kBlock - 1) / kBlock;
   const int64_t kv_blocks = (int64_t)((batch->n_tokens + a.group - 1) / a.group) *
                             ((2 * format->kv_heads + kWaves - 1) / kWaves);
