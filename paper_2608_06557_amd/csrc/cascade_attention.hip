@@ -538,9 +538,8 @@ constexpr int waves_per_simd(int dim, int tiles) {
   const int held = dim * tiles;  // of o in registers
   return held <= 64 ? 5 : tiles == 1 && held <= 128 ? 4 : held <= 128 ? 3 : held <= 256 || tiles == 4 ? 2 : 1;
 }
-template <int kType, int kDim, int kTiles, Cap kCap, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, waves_per_simd(kDim, kTiles)) void attention_kernel(Attention a) {
-  constexpr int kBlock = 64 * kWaves;
+template <int kType, int kDim, int kTiles, Cap kCap>
+__global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attention_kernel(Attention a) {
   constexpr int kRows = 16 * kTiles;
   constexpr int kPart = kDim < 128 ? kDim : 128;  // dims that one combination takes
   constexpr int kPitch = kPart + 4;
@@ -1191,11 +1190,11 @@ __global__ __launch_bounds__(kBlock) void weight_kernel(Attention a, float *bloc
 
 constexpr int kCUs = 256;
 // Up to this many tokens in the whole table nothing is cut, which saves the join
-// (one request of 777 tokens: 11.4 us, cut 12.5; of 100: 7.8, with a join that
-// finds nothing 11.4).  A single tile of few rows has 8 waves then, where its
-// tokens are enough for them (777: 10.4 us, 600: 9.5 against 10.2; 100: 8.2
-// against 7.8, so not there; 16 waves 15.9).
-constexpr int kUncut = 1024, kWide = 8;
+// (one request of 777 tokens: 11.8 us, cut 12.5; of 100: 8.0, with a join that
+// finds nothing 11.4).  8 waves on a tile instead of 4 take 11.5 us for 777 tokens
+// and 12.1 against 12.3 for 1024, but 10.4 against 9.9 for 512, 10.4 against 9.8
+// for 777 of 64 dims, and no less for 2 to 4 requests.
+constexpr int kUncut = 1024;
 constexpr int kGroups = 4 * kCUs;      // workgroups of the kernel that splits tokens over waves
 constexpr int kTileGroups = kCUs;   // of the kernel that splits rows over waves: one to a CU
 constexpr int most_rows(int dim) { return dim == 256 ? 32 : 64; }  // of a request in the former
@@ -1232,14 +1231,14 @@ bool heads_ok(const cascade_kv_format_t *f, int q_heads) {
   return q_heads >= 1 && q_heads % f->kv_heads == 0 && q_heads / f->kv_heads <= 128;
 }
 
-template <int kType, int kDim, int kTiles, int kW = kWaves>
+template <int kType, int kDim, int kTiles>
 void start(const Attention &a, int grid, Cap cap, hipStream_t stream) {
-  const size_t mix = sizeof(float) * kW * 16 * (2 + (kDim < 128 ? kDim : 128) + 4);
+  const size_t mix = sizeof(float) * kWaves * 16 * (2 + (kDim < 128 ? kDim : 128) + 4);
   auto kernel =
-      cap == Cap::kWide     ? attention_kernel<kType, kDim, kTiles, Cap::kWide, kW>
-      : cap == Cap::kNarrow ? attention_kernel<kType, kDim, kTiles, Cap::kNarrow, kW>
-                            : attention_kernel<kType, kDim, kTiles, Cap::kNone, kW>;
-  hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * kW), list_bytes(a.batch.n) + mix, stream, a);
+      cap == Cap::kWide     ? attention_kernel<kType, kDim, kTiles, Cap::kWide>
+      : cap == Cap::kNarrow ? attention_kernel<kType, kDim, kTiles, Cap::kNarrow>
+                            : attention_kernel<kType, kDim, kTiles, Cap::kNone>;
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * kWaves), list_bytes(a.batch.n) + mix, stream, a);
 }
 
 template <int kType, int kDim>
@@ -1277,9 +1276,7 @@ int run(Attention a, char *ws, const Workspace &w, Cap cap, float *block_weight,
     const int64_t room = kCUs * waves_per_simd(kDim, small / 16);
     const int64_t work = (keys + (int64_t)a.batch.n * a.kv.kv_heads * kFixedKeys) / a.range_keys;
     const int grid = (int)std::min(std::min<int64_t>(kGroups, room), std::max<int64_t>(8, work));
-    if (small == 16 && table <= kUncut && table > 512ll * a.batch.n)
-      start<kType, kDim, 1, kWide>(a, grid, cap, s);
-    else if (small == 16)
+    if (small == 16)
       start<kType, kDim, 1>(a, grid, cap, s);
     else if (small == 32)
       start<kType, kDim, 2>(a, grid, cap, s);
