@@ -43,10 +43,8 @@ CASCADE_WORK_FN T most(T a, T b) { return a < b ? b : a; }
 struct Segments {
   long long shown;  // cached tokens that every row sees; below 0 the first -shown rows see none
   int count, per;
-  int blind;        // leading tiles that see nothing
   CASCADE_WORK_FN Segments(int len, int count, int tile_tokens)
-      : shown((long long)len - count), count(count), per(tile_tokens),
-        blind(count > len ? (count - len) / tile_tokens : 0) {}
+      : shown((long long)len - count), count(count), per(tile_tokens) {}
   CASCADE_WORK_FN int tiles() const { return (count + per - 1) / per; }
   // tokens that row tile t runs over
   CASCADE_WORK_FN long long length(int t) const {
@@ -54,12 +52,18 @@ struct Segments {
   }
   // the costs of the tiles before t
   CASCADE_WORK_FN long long start(int t) const {
-    const long long z = least(blind, t);
-    return (long long)t * kFixedKeys + (t - z) * shown + per * (((long long)t * (t + 1) - z * (z + 1)) / 2);
+    return t * (shown + kFixedKeys) + (long long)per * ((long long)t * (t + 1) / 2) + (shown < 0 ? unseen(t) : 0);
   }
   CASCADE_WORK_FN long long total() const {
     const int t = tiles() - 1;
     return start(t) + length(t) + kFixedKeys;
+  }
+
+ private:
+  // by how much the tiles before t that see nothing bring the sum of shown + (t + 1) per below 0
+  CASCADE_WORK_FN long long unseen(int t) const {
+    const long long z = least((int)-shown / per, t);
+    return -z * shown - per * (z * (z + 1) / 2);
   }
 };
 
