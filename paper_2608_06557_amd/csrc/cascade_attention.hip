@@ -25,11 +25,13 @@
 // to the workspace and a second launch joins them.
 //
 // Few rows of a request are bound by reading the cache: 4 requests of 115 Ki
-// tokens, 32 heads over 8 of 128 dims, 947 MB in 177 us (5.3 TB/s; a large
-// read reaches 6.2) and 8 for the join; 128 requests of 582 tokens, 64 heads,
-// 157 MB in 35 us (4.5 TB/s: 4 us are the list, and short segments fill and
-// drain), the join and the weights 10 more.  Many rows are bound by the
-// products and the softmax beside them (tile_kernel).
+// tokens, 32 heads over 8 of 128 dims, 947 MB in 177 us (1043 MB fetched, 5.9
+// TB/s; a large read reaches 6.2) and 8 for the join; 128 requests of 582 tokens,
+// 64 heads, 157 MB in 35 to 37 us (4.5 TB/s: 4 us are the list, and short segments
+// fill and drain), the join and the weights 10 more.  Drafts of up to 32 rows wait
+// half of their cycles at two waves a SIMD: 32 requests of 7 Ki tokens, 462 MB in 109
+// us.  Many rows are bound by the products and the softmax beside them
+// (tile_kernel).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -777,10 +779,11 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
 // has about as many cycles as the products.  8 waves on a stage: with 4 each wave
 // widens twice as much and takes 4 % longer.  16 chunks of 512 tokens, 64 heads over
 // 8 of 128 dims, contexts of 7 k: 1.8 to 1.9 ms, 0.95 PFLOP/s of the 1.24 that a large
-// matrix product reaches.  At 32 rows a wave, operands cross from LDS at 128 bytes
-// in a product's cycles, all that LDS gives: products, LDS and softmax
-// take about 1.0, 0.9 and 0.9 ms and overlap in part; 64 rows to a wave halve the LDS
-// reads, but leave one wave to a SIMD and take 25 % longer.
+// matrix product reaches; the matrix units are busy for 45 % of the cycles.  Builds
+// that leave parts out take 1.1 ms for the products alone, 1.2 with their operands'
+// reads from LDS, 1.5 with the softmax, and 2.0 with the widening (before the last
+// steps).  64 rows to a wave halve the LDS reads, but leave one wave to a SIMD and
+// take 25 % longer.
 constexpr int stage_tokens(int dim) { return dim == 256 ? 32 : 64; }
 constexpr int tile_waves(int dim) { return 2 * stage_tokens(dim) / 16; }
 constexpr int tile_rows(int dim) { return 32 * tile_waves(dim); }
