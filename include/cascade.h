@@ -666,6 +666,35 @@ int cascade_attention(const cascade_kv_pool_t *pool, int32_t layer,
                       void *workspace, size_t workspace_bytes, int32_t *status_dev,
                       void *stream);
 
+/* cascade_attention of a batch whose requests share their first tokens (the
+   step's SHARE action, parallel samples, a common system prompt), which are
+   read once for a whole group.  The requests of a group are neighbours in the
+   batch: leader[i] is the first of request i's (i itself where it shares with
+   none), and the first shared_len[leader[i]] cached tokens of each (a multiple of
+   block_tokens; 0 for none; entries of other requests are not read) lie in the
+   same blocks: the rows of the table name the same slots there, of which the first
+   request's are read and the last is checked.  No new token lies in them: every
+   request has kv_len - c >= shared_len.
+   Results are those of cascade_attention up to the order of sums.  args as there, without block_weight
+   (blocks that requests share are not evicted for one of them).
+   workspace: cascade_attention_shared_workspace_bytes(...) bytes, 256-byte
+   aligned, of any content; it grows with n_tokens.
+   Errors as cascade_attention; leaders, lengths or slots that are not as above, or
+   a group of more than max_tokens new tokens, set *status_dev = CASCADE_EINVAL. */
+typedef struct {
+  const int32_t *leader;     /* [n] */
+  const int32_t *shared_len; /* [n] */
+  int32_t max_tokens;        /* most new tokens of one group */
+} cascade_shared_t;
+size_t cascade_attention_shared_workspace_bytes(const cascade_kv_format_t *format,
+                                                const cascade_kv_batch_t *batch,
+                                                int32_t q_heads);
+int cascade_attention_shared(const cascade_kv_pool_t *pool, int32_t layer,
+                             const cascade_kv_format_t *format, const cascade_kv_batch_t *batch,
+                             const cascade_block_table_t *table, const cascade_attention_t *args,
+                             const cascade_shared_t *shared, void *workspace,
+                             size_t workspace_bytes, int32_t *status_dev, void *stream);
+
 /* Drops blocks from inside requests under HBM pressure: of request i's
    b = ceil(kv_len[i]/block_tokens) blocks, the first `sink` and the last
    `recent` (>= 1: the block being filled stays) are kept, and of the others the

@@ -13,7 +13,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libcascade.so")
 SOURCES = ["cascade_step.hip", "cascade_kvcopy.hip", "cascade_prefix.hip", "cascade_reclaim.hip",
            "cascade_hosttier.hip", "cascade_kvappend.hip", "cascade_attention.hip",
-           "cascade_kvevict.hip"]
+           "cascade_attention_shared.hip", "cascade_attention_shared_f16.hip", "cascade_kvevict.hip"]
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [
@@ -39,7 +39,7 @@ def build(verbose: bool = False) -> str:
         subprocess.run(cmd, check=True)
         return obj
 
-    with ThreadPoolExecutor(4) as pool:
+    with ThreadPoolExecutor(8) as pool:
         objs = list(pool.map(compile_one, SOURCES))
     tmp = LIB + ".tmp"
     cmd = [hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs]

@@ -30,6 +30,7 @@ EXPORTED = ["cascade_step_workspace_bytes", "cascade_step", "cascade_step_noallo
             "cascade_tier_chain_workspace_bytes", "cascade_tier_reclaim_chain",
             "cascade_kv_chunk_bytes", "cascade_rope_frequencies", "cascade_kv_append",
             "cascade_attention_workspace_bytes", "cascade_attention", "cascade_kv_evict",
+            "cascade_attention_shared_workspace_bytes", "cascade_attention_shared",
             "cascade_strerror"]
 INDEX_SLOT_BYTES = 16
 BF16, F16 = 0, 1
@@ -134,6 +135,10 @@ class Attention(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("q_heads", C.c_int32), ("scale", C.c_float),
                 ("softcap", C.c_float), ("q", Rows), ("out", Rows), ("lse", C.c_void_p),
                 ("block_weight", C.c_void_p), ("weight_window", C.c_int32)]
+
+
+class Shared(C.Structure):
+    _fields_ = [("leader", C.c_void_p), ("shared_len", C.c_void_p), ("max_tokens", C.c_int32)]
 
 
 class Evict(C.Structure):
@@ -368,6 +373,12 @@ def _kv() -> C.CDLL:
         L.cascade_attention.restype = C.c_int
         L.cascade_attention.argtypes = [P(KvPool), i32, P(KvFormat), P(KvBatch), P(BlockTable),
                                         P(Attention), v, C.c_size_t, v, v]
+        L.cascade_attention_shared_workspace_bytes.restype = C.c_size_t
+        L.cascade_attention_shared_workspace_bytes.argtypes = [P(KvFormat), P(KvBatch), i32]
+        L.cascade_attention_shared.restype = C.c_int
+        L.cascade_attention_shared.argtypes = [P(KvPool), i32, P(KvFormat), P(KvBatch),
+                                               P(BlockTable), P(Attention), P(Shared), v,
+                                               C.c_size_t, v, v]
         L.cascade_kv_evict.restype = C.c_int
         L.cascade_kv_evict.argtypes = [P(BlockTable), P(Evict), v, v]
         _kv_lib = L
@@ -427,6 +438,18 @@ def cascade_attention(pool: KvPool, layer: int, fmt: KvFormat, batch: KvBatch, t
     return int(_kv().cascade_attention(_ref(pool), layer, _ref(fmt), _ref(batch), _ref(table),
                                        _ref(args), workspace, workspace_bytes, status_dev,
                                        stream))
+
+
+def cascade_attention_shared_workspace_bytes(fmt: KvFormat, batch: KvBatch, q_heads: int) -> int:
+    return int(_kv().cascade_attention_shared_workspace_bytes(_ref(fmt), _ref(batch), q_heads))
+
+
+def cascade_attention_shared(pool: KvPool, layer: int, fmt: KvFormat, batch: KvBatch,
+                             table: BlockTable, args: Attention, shared: Shared, workspace: int,
+                             workspace_bytes: int, status_dev: int, stream: int) -> int:
+    return int(_kv().cascade_attention_shared(_ref(pool), layer, _ref(fmt), _ref(batch),
+                                              _ref(table), _ref(args), _ref(shared), workspace,
+                                              workspace_bytes, status_dev, stream))
 
 
 def cascade_kv_evict(table: BlockTable, args: Evict, status_dev: int, stream: int) -> int:

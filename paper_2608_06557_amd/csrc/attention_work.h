@@ -67,6 +67,17 @@ struct Segments {
   }
 };
 
+// The same where every row sees all of the tokens.
+struct EvenSegments {
+  long long len;
+  int count, per;
+  CASCADE_WORK_FN EvenSegments(int len, int count, int tile_tokens) : len(len), count(count), per(tile_tokens) {}
+  CASCADE_WORK_FN int tiles() const { return (count + per - 1) / per; }
+  CASCADE_WORK_FN long long length(int) const { return len; }
+  CASCADE_WORK_FN long long start(int t) const { return t * (len + kFixedKeys); }
+  CASCADE_WORK_FN long long total() const { return start(tiles()); }
+};
+
 // floor(a / b) of whole numbers 0 <= a < 2^52, 0 < b: by doubles, whose
 // quotient is off by one at most
 CASCADE_WORK_FN long long quotient(long long a, long long b) {
@@ -93,6 +104,7 @@ __host__ __device__
 constexpr int list_bytes(int n) { return (20 * n + 8 + 15) & ~15; }
 
 // Where the range of cost `c` begins: a segment and a token of it.
+template <typename S = Segments>
 CASCADE_WORK_FN Place locate(const Cuts &a, int kv_heads, const List &list, int n, int atomic_keys, long long c) {
   Place p = {n, 0, 0, 0};
   if (n == 0 || c >= list.before[n]) return p;
@@ -102,7 +114,7 @@ CASCADE_WORK_FN Place locate(const Cuts &a, int kv_heads, const List &list, int 
     if (list.before[mid] <= c) lo = mid; else hi = mid;
   }
   p.item = lo;
-  const Segments s(list.len[lo], list.count[lo], a.tile_tokens);
+  const S s(list.len[lo], list.count[lo], a.tile_tokens);
   const long long per_head = s.total();
   long long left = c - list.before[lo];
   p.head = (int)quotient(left, per_head);
@@ -151,12 +163,13 @@ CASCADE_WORK_FN int uncut_keys(const Cuts &a, long long total, int groups) {
 
 // The segment that range w, which begins at `at`, is the first to cut, the
 // range before beginning at `prev`; request -1 if there is none.
+template <typename S = Segments>
 CASCADE_WORK_FN Split first_cut(const Cuts &a, const List &list, const Place &at, const Place &prev, long long total,
                                 int groups) {
   const bool inside = at.key > 0 && !(prev.key > 0 && prev.item == at.item && prev.head == at.head &&
                                       prev.tile == at.tile);
   if (!inside) return Split{-1, 0, 0, 0};
-  const Segments seg(list.len[at.item], list.count[at.item], a.tile_tokens);
+  const S seg(list.len[at.item], list.count[at.item], a.tile_tokens);
   const long long stop = list.before[at.item] + at.head * seg.total() + seg.start(at.tile) +
                          seg.length(at.tile) + kFixedKeys;
   // the last range that begins before `stop`

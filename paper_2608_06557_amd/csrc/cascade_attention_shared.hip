@@ -1,0 +1,64 @@
+// cascade_attention_shared.hip -- attention of a batch whose neighbouring
+// requests share their first blocks, on gfx950.
+//
+// Softmax over a row's tokens splits at any token: with (m, sum, O) of the
+// shared ones, the rest goes on from there as from any earlier tile.  So a first
+// launch takes each group's shared tokens once for the rows of all its requests
+// (no row is masked) and leaves every row's state in 32 bits; a second takes
+// each request's other tokens, and a row's first part begins with its state.
+// Both are the kernels of attention_tiles.h: a group of many rows goes to row
+// tiles, where the products bound it instead of the reads of the cache.
+#include "attention_shared.h"
+
+namespace cascade {
+int shared_attention_bf16(const SharedCall &c) { return attend_shared<CASCADE_BF16>(c); }
+
+namespace {
+// The workspace of attention, then the rows' states.
+struct Places {
+  Workspace w;
+  size_t states, sums, total;
+  Places(const cascade_kv_format_t *f, const cascade_kv_batch_t *b, int q_heads) : w(layout(f, b, q_heads, 0)) {
+    const size_t rows = (size_t)b->n_tokens * q_heads;
+    states = w.total;
+    sums = states + aligned(sizeof(float) * rows * f->head_dim);
+    total = sums + aligned(sizeof(float) * rows * 2);
+  }
+};
+}  // namespace
+}  // namespace cascade
+
+using namespace cascade;
+
+extern "C" size_t cascade_attention_shared_workspace_bytes(const cascade_kv_format_t *format,
+                                                           const cascade_kv_batch_t *batch, int32_t q_heads) {
+  if (!kv_format_ok(format) || !batch || batch->n_tokens < 0 || batch->n_entries < 0 || !heads_ok(format, q_heads))
+    return 0;
+  return Places(format, batch, q_heads).total;
+}
+
+extern "C" int cascade_attention_shared(const cascade_kv_pool_t *pool, int32_t layer,
+                                        const cascade_kv_format_t *format, const cascade_kv_batch_t *batch,
+                                        const cascade_block_table_t *table, const cascade_attention_t *args,
+                                        const cascade_shared_t *shared, void *workspace, size_t workspace_bytes,
+                                        int32_t *status_dev, void *stream) {
+  if (!kv_pool_ok(pool, layer, format) || !kv_batch_ok(batch, table) || !attention_ok(args, format) || !shared)
+    return CASCADE_EINVAL;
+  if (args->block_weight || args->weight_window || shared->max_tokens < 0) return CASCADE_EINVAL;
+  if (!workspace || ((uintptr_t)workspace & 255)) return CASCADE_EINVAL;
+  const Places p(format, batch, args->q_heads);
+  if (workspace_bytes < p.total) return CASCADE_ENOSPC;
+  if (batch->n == 0 || batch->n_tokens == 0 || batch->max_new == 0) return CASCADE_OK;
+  if (!kv_rows_ok(&args->q) || !kv_rows_ok(&args->out) || !shared->leader || !shared->shared_len)
+    return CASCADE_EINVAL;
+  Cap cap;
+  Attention a = attention_of(pool, layer, format, batch, table, args, status_dev, cap);
+  char *ws = static_cast<char *>(workspace);
+  a.leader = shared->leader;
+  a.shared_len = shared->shared_len;
+  a.max_tokens = std::min(shared->max_tokens, batch->n_tokens);
+  a.states = reinterpret_cast<float *>(ws + p.states);
+  a.state_sums = reinterpret_cast<float *>(ws + p.sums);
+  const SharedCall c = {a, ws, p.w, cap, static_cast<hipStream_t>(stream)};
+  return args->dtype == CASCADE_BF16 ? shared_attention_bf16(c) : shared_attention_f16(c);
+}

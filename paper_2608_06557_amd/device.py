@@ -541,6 +541,62 @@ class DeviceAttention:
         _raise(self._call(stream_handle(stream)))
 
 
+def _workspace(workspace, size: int, device):
+    """(tensor, its first address on 256 bytes, bytes from there) of a call's
+    workspace, a new one if none is given."""
+    torch = _torch()
+    if workspace is None:
+        workspace = torch.empty(size + 256, dtype=torch.uint8, device=device)
+    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("a workspace is a contiguous uint8 tensor")
+    at = (workspace.data_ptr() + 255) & ~255
+    return workspace, at, max(workspace.data_ptr() + workspace.numel() - at, 0)
+
+
+def _launch(call, device, stream) -> None:
+    """The call on `stream`, or on the current one of the tensors' device."""
+    torch = _torch()
+    if device.type == "cuda" and device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            _raise(call(stream_handle(stream)))
+    else:
+        _raise(call(stream_handle(stream)))
+
+
+class DeviceSharedAttention:
+    """cascade_attention_shared with its arguments and workspace laid out:
+    DeviceAttention of a batch whose neighbours share their first tokens.
+    `leader` (int32, one per request) names the first request of each one's
+    group and `shared_len` there the tokens that the group shares;
+    `most_shared` is the most new tokens of one group."""
+
+    def __init__(self, kv: DeviceKvPool, batch: KvBatch, leader, shared_len, most_shared: int, q, out,
+                 scale: float, softcap: float = 0.0, lse=None, layer: int = 0, workspace=None):
+        torch = _torch()
+        if q.shape != out.shape or q.dtype != out.dtype or q.shape[0] < batch.tokens or \
+                q.shape[2] != kv.head_dim:
+            raise ValueError("q and out do not fit the batch, the pool or each other")
+        self.kv, self.batch, self.layer = kv, batch, layer
+        self.tensors = (q, out, lse, leader, shared_len)
+        _check_device(kv.pool.device, *self.tensors, *batch.tensors, workspace)
+        heads, i32 = q.shape[1], torch.int32
+        self.c_args = cx.Attention(
+            _dtype(q), heads, scale, softcap, kv_rows(q), kv_rows(out),
+            None if lse is None else _check_array(lse, torch.float32, batch.tokens * heads, "lse"), None, 0)
+        self.c_shared = cx.Shared(_check_array(leader, i32, batch.n, "leader"),
+                                  _check_array(shared_len, i32, batch.n, "shared_len"), most_shared)
+        size = cx.cascade_attention_shared_workspace_bytes(kv.c_format, batch.c_batch, heads)
+        if size == 0:
+            raise ValueError("query heads outside the domain")
+        self.workspace, self.ws_ptr, self.ws_bytes = _workspace(workspace, size, q.device)
+        self._call = cx.kv_call("cascade_attention_shared", kv.c_pool, layer, kv.c_format, batch.c_batch,
+                                batch.c_table, self.c_args, self.c_shared, self.ws_ptr, self.ws_bytes,
+                                kv.status.data_ptr())
+
+    def run(self, stream=None) -> None:
+        _launch(self._call, self.kv.pool.device, stream)
+
+
 class DeviceKvEvict:
     """cascade_kv_evict with its arguments laid out: `run` writes the tight
     table of what stays to kv_len_out, row_offsets_out, slots_out and
