@@ -695,6 +695,75 @@ int cascade_attention_shared(const cascade_kv_pool_t *pool, int32_t layer,
                              const cascade_shared_t *shared, void *workspace,
                              size_t workspace_bytes, int32_t *status_dev, void *stream);
 
+/* Bounds of the keys, for cascade_kv_select: a pool whose chunk_bytes is at
+   least cascade_kv_chunk_bytes(format) + cascade_kv_bounds_bytes(format) holds,
+   behind the scales of each chunk, kv_heads rows of head_dim signed bytes: in the
+   K chunk ceil(c / 4), c the largest code of the block's keys in that dim, in the
+   V chunk floor(c / 4) of their least (in units of four of K's scale).  They lie
+   in the chunks, so they move with the blocks.
+   cascade_kv_bounds writes them in one launch, of layer `layer`, for the blocks that hold a
+   request's new tokens (after cascade_kv_append), or with `whole` for all blocks of
+   the requests, over the tokens before kv_len.  A block that requests share is
+   full, or has one request's tokens only.  Requests outside the domain and slots
+   outside [0, num_slots) set *status_dev = CASCADE_EINVAL and are not written (status_dev may be
+   NULL).  Returns CASCADE_EINVAL for NULL pointers, formats or sizes outside the
+   domain, CASCADE_EHIP on a failed launch. */
+size_t cascade_kv_bounds_bytes(const cascade_kv_format_t *format);
+int cascade_kv_bounds(const cascade_kv_pool_t *pool, int32_t layer,
+                      const cascade_kv_format_t *format, const cascade_kv_batch_t *batch,
+                      const cascade_block_table_t *table, int32_t whole, int32_t *status_dev,
+                      void *stream);
+
+/* For each new token and KV head the blocks that promise its largest scores:
+   of the b blocks up to the token's own the first `sink`, the last `recent`
+   (>= 1: the own one), and of the others those with the largest score until `keep` are
+   listed (equal scores: the lower index first), or all if b <= keep.
+     score = scale * max_r 2^(e_r - e) sum_d max(n_rd, 0) u_d + min(n_rd, 0) l_d
+   with u, l and scale the block's bounds and K scale (they have to be up to date), r the query heads
+   of the KV head, e_r the least exponent >= -100 at which q_r is at most 127 * 2^e_r,
+   n_r = q_r / 2^e_r rounded to nearest even, e the largest e_r: up to the roundings
+   of u, l and n a bound on every q . k of the block (for a positive scale of attention).  The sums are
+   whole numbers, the rest powers of two in 32 bits: a selection is the same on any
+   machine.  A NaN or infinite query element counts as 0 and sets *status_dev.
+   selected: device int32[n_tokens][kv_heads][keep], block indices within the request, ascending,
+   then -1; tokens of no request are left as they are.
+   workspace: cascade_kv_select_workspace_bytes(...) bytes, 256-byte aligned, of
+   any content (4 bytes per table entry, KV head and new token of the longest
+   run: it grows with n_entries and max_new).
+   Errors as cascade_attention. */
+typedef struct {
+  int32_t dtype, q_heads;     /* as cascade_attention_t */
+  int32_t keep, sink, recent; /* 1 .. 65536; >= 0; >= 1; sink + recent <= keep */
+  cascade_rows_t q;
+  int32_t *selected;
+} cascade_select_t;
+size_t cascade_kv_select_workspace_bytes(const cascade_kv_format_t *format,
+                                         const cascade_kv_batch_t *batch);
+int cascade_kv_select(const cascade_kv_pool_t *pool, int32_t layer,
+                      const cascade_kv_format_t *format, const cascade_kv_batch_t *batch,
+                      const cascade_block_table_t *table, const cascade_select_t *args,
+                      void *workspace, size_t workspace_bytes, int32_t *status_dev,
+                      void *stream);
+
+/* cascade_attention of each new token and KV head over the tokens of the
+   listed blocks, up to the token itself.  selected: device int32[n_tokens][kv_heads][keep] (keep
+   1 .. 65536), ascending block indices within the request, from the first
+   negative entry on nothing but negative ones.  A token with an empty list gets zeros and lse
+   -infinity.  args as there, without block_weight.  workspace:
+   cascade_attention_selected_workspace_bytes(...) bytes, 256-byte aligned, of any
+   content; it grows with n_tokens only where keep is above 4096.
+   Errors as cascade_attention; a list that is not as above, or names a block
+   behind the token's own, sets *status_dev = CASCADE_EINVAL. */
+size_t cascade_attention_selected_workspace_bytes(const cascade_kv_format_t *format,
+                                                  const cascade_kv_batch_t *batch,
+                                                  int32_t q_heads, int32_t keep);
+int cascade_attention_selected(const cascade_kv_pool_t *pool, int32_t layer,
+                               const cascade_kv_format_t *format, const cascade_kv_batch_t *batch,
+                               const cascade_block_table_t *table,
+                               const cascade_attention_t *args, const int32_t *selected,
+                               int32_t keep, void *workspace, size_t workspace_bytes,
+                               int32_t *status_dev, void *stream);
+
 /* Drops blocks from inside requests under HBM pressure: of request i's
    b = ceil(kv_len[i]/block_tokens) blocks, the first `sink` and the last
    `recent` (>= 1: the block being filled stays) are kept, and of the others the

@@ -13,7 +13,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libcascade.so")
 SOURCES = ["cascade_step.hip", "cascade_kvcopy.hip", "cascade_prefix.hip", "cascade_reclaim.hip",
            "cascade_hosttier.hip", "cascade_kvappend.hip", "cascade_attention.hip",
-           "cascade_attention_shared.hip", "cascade_attention_shared_f16.hip", "cascade_kvevict.hip"]
+           "cascade_attention_shared.hip", "cascade_attention_shared_f16.hip", "cascade_kvselect.hip",
+           "cascade_attention_selected.hip", "cascade_kvevict.hip"]
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [

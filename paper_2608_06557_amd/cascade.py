@@ -31,6 +31,9 @@ EXPORTED = ["cascade_step_workspace_bytes", "cascade_step", "cascade_step_noallo
             "cascade_kv_chunk_bytes", "cascade_rope_frequencies", "cascade_kv_append",
             "cascade_attention_workspace_bytes", "cascade_attention", "cascade_kv_evict",
             "cascade_attention_shared_workspace_bytes", "cascade_attention_shared",
+            "cascade_kv_bounds_bytes", "cascade_kv_bounds", "cascade_kv_select_workspace_bytes",
+            "cascade_kv_select", "cascade_attention_selected_workspace_bytes",
+            "cascade_attention_selected",
             "cascade_strerror"]
 INDEX_SLOT_BYTES = 16
 BF16, F16 = 0, 1
@@ -139,6 +142,11 @@ class Attention(C.Structure):
 
 class Shared(C.Structure):
     _fields_ = [("leader", C.c_void_p), ("shared_len", C.c_void_p), ("max_tokens", C.c_int32)]
+
+
+class Select(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("q_heads", C.c_int32), ("keep", C.c_int32),
+                ("sink", C.c_int32), ("recent", C.c_int32), ("q", Rows), ("selected", C.c_void_p)]
 
 
 class Evict(C.Structure):
@@ -379,6 +387,23 @@ def _kv() -> C.CDLL:
         L.cascade_attention_shared.argtypes = [P(KvPool), i32, P(KvFormat), P(KvBatch),
                                                P(BlockTable), P(Attention), P(Shared), v,
                                                C.c_size_t, v, v]
+        L.cascade_kv_bounds_bytes.restype = C.c_size_t
+        L.cascade_kv_bounds_bytes.argtypes = [P(KvFormat)]
+        L.cascade_kv_bounds.restype = C.c_int
+        L.cascade_kv_bounds.argtypes = [P(KvPool), i32, P(KvFormat), P(KvBatch), P(BlockTable),
+                                        i32, v, v]
+        L.cascade_kv_select_workspace_bytes.restype = C.c_size_t
+        L.cascade_kv_select_workspace_bytes.argtypes = [P(KvFormat), P(KvBatch)]
+        L.cascade_kv_select.restype = C.c_int
+        L.cascade_kv_select.argtypes = [P(KvPool), i32, P(KvFormat), P(KvBatch), P(BlockTable),
+                                        P(Select), v, C.c_size_t, v, v]
+        L.cascade_attention_selected_workspace_bytes.restype = C.c_size_t
+        L.cascade_attention_selected_workspace_bytes.argtypes = [P(KvFormat), P(KvBatch), i32,
+                                                                 i32]
+        L.cascade_attention_selected.restype = C.c_int
+        L.cascade_attention_selected.argtypes = [P(KvPool), i32, P(KvFormat), P(KvBatch),
+                                                 P(BlockTable), P(Attention), v, i32, v,
+                                                 C.c_size_t, v, v]
         L.cascade_kv_evict.restype = C.c_int
         L.cascade_kv_evict.argtypes = [P(BlockTable), P(Evict), v, v]
         _kv_lib = L
@@ -450,6 +475,43 @@ def cascade_attention_shared(pool: KvPool, layer: int, fmt: KvFormat, batch: KvB
     return int(_kv().cascade_attention_shared(_ref(pool), layer, _ref(fmt), _ref(batch),
                                               _ref(table), _ref(args), _ref(shared), workspace,
                                               workspace_bytes, status_dev, stream))
+
+
+def cascade_kv_bounds_bytes(fmt: KvFormat) -> int:
+    return int(_kv().cascade_kv_bounds_bytes(_ref(fmt)))
+
+
+def cascade_kv_bounds(pool: KvPool, layer: int, fmt: KvFormat, batch: KvBatch, table: BlockTable,
+                      whole: int, status_dev: int, stream: int) -> int:
+    return int(_kv().cascade_kv_bounds(_ref(pool), layer, _ref(fmt), _ref(batch), _ref(table),
+                                       whole, status_dev, stream))
+
+
+def cascade_kv_select_workspace_bytes(fmt: KvFormat, batch: KvBatch) -> int:
+    return int(_kv().cascade_kv_select_workspace_bytes(_ref(fmt), _ref(batch)))
+
+
+def cascade_kv_select(pool: KvPool, layer: int, fmt: KvFormat, batch: KvBatch, table: BlockTable,
+                      args: Select, workspace: int, workspace_bytes: int, status_dev: int,
+                      stream: int) -> int:
+    return int(_kv().cascade_kv_select(_ref(pool), layer, _ref(fmt), _ref(batch), _ref(table),
+                                       _ref(args), workspace, workspace_bytes, status_dev,
+                                       stream))
+
+
+def cascade_attention_selected_workspace_bytes(fmt: KvFormat, batch: KvBatch, q_heads: int,
+                                               keep: int) -> int:
+    return int(_kv().cascade_attention_selected_workspace_bytes(_ref(fmt), _ref(batch), q_heads,
+                                                                keep))
+
+
+def cascade_attention_selected(pool: KvPool, layer: int, fmt: KvFormat, batch: KvBatch,
+                               table: BlockTable, args: Attention, selected: int, keep: int,
+                               workspace: int, workspace_bytes: int, status_dev: int,
+                               stream: int) -> int:
+    return int(_kv().cascade_attention_selected(_ref(pool), layer, _ref(fmt), _ref(batch),
+                                                _ref(table), _ref(args), selected, keep,
+                                                workspace, workspace_bytes, status_dev, stream))
 
 
 def cascade_kv_evict(table: BlockTable, args: Evict, status_dev: int, stream: int) -> int:

@@ -115,4 +115,12 @@ __device__ __forceinline__ void kv_report(int32_t *status) {
   if (status) *status = CASCADE_EINVAL;
 }
 
+// Reports requests outside the domain, whether they have new tokens or not.
+// Called by all threads of a workgroup.
+__device__ __forceinline__ void check_requests(const cascade_kv_batch_t &b, const int32_t *row_offsets,
+                                               int block_shift, int32_t *status) {
+  for (int i = threadIdx.x; i < b.n; i += blockDim.x)
+    if (!kv_request(b, row_offsets, block_shift, i).ok) kv_report(status);
+}
+
 }  // namespace cascade

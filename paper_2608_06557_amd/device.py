@@ -367,13 +367,15 @@ class DeviceTiers:
 
 # ------------------------------------------------------- the 8-bit KV cache
 
-def kv_chunk_bytes(kv_heads: int, head_dim: int, block_tokens: int = 16) -> int:
-    """Bytes of one block's K or V of one layer in the 8-bit cache."""
-    size = cx.cascade_kv_chunk_bytes(cx.KvFormat(block_tokens, kv_heads, head_dim))
+def kv_chunk_bytes(kv_heads: int, head_dim: int, block_tokens: int = 16, bounds: bool = False) -> int:
+    """Bytes of one block's K or V of one layer in the 8-bit cache, with the
+    bounds of its keys or without."""
+    fmt = cx.KvFormat(block_tokens, kv_heads, head_dim)
+    size = cx.cascade_kv_chunk_bytes(fmt)
     if size == 0:
         raise ValueError(f"no 8-bit cache of {kv_heads} heads of {head_dim} dims in blocks of "
                          f"{block_tokens} tokens")
-    return size
+    return size + (cx.cascade_kv_bounds_bytes(fmt) if bounds else 0)
 
 
 def _raise(rc: int) -> None:
@@ -413,16 +415,17 @@ def _check_device(device, *tensors) -> None:
 
 class DeviceKvPool:
     """A pool of the 8-bit cache over a byte tensor [layers, 2 (K, V), slots,
-    bytes]; the last dimension holds at least a chunk and may be padded."""
+    bytes]; the last dimension holds at least a chunk and may be padded.
+    `bounds`: chunks hold the bounds of their keys too (DeviceKvBounds)."""
 
-    def __init__(self, pool, kv_heads: int, head_dim: int, block_tokens: int = 16):
+    def __init__(self, pool, kv_heads: int, head_dim: int, block_tokens: int = 16, bounds: bool = False):
         torch = _torch()
-        size = kv_chunk_bytes(kv_heads, head_dim, block_tokens)
+        size = kv_chunk_bytes(kv_heads, head_dim, block_tokens, bounds)
         if pool.dtype != torch.uint8 or pool.dim() != 4 or pool.shape[1] != 2 or \
                 pool.shape[3] < size or pool.stride(3) != 1:
             raise ValueError(f"a uint8 tensor [layers, 2, slots, bytes >= {size}] is needed")
         self.pool, self.kv_heads, self.head_dim = pool, kv_heads, head_dim
-        self.block_tokens, self.chunk_bytes = block_tokens, size
+        self.block_tokens, self.chunk_bytes, self.bounds = block_tokens, size, bounds
         self.c_format = cx.KvFormat(block_tokens, kv_heads, head_dim)
         self.c_pool = cx.KvPool(pool.data_ptr(), pool.shape[0], pool.shape[2], size,
                                 pool.stride(0), pool.stride(1), pool.stride(2))
@@ -430,11 +433,11 @@ class DeviceKvPool:
 
     @classmethod
     def empty(cls, layers: int, slots: int, kv_heads: int, head_dim: int, block_tokens: int = 16,
-              device="cuda:0"):
+              device="cuda:0", bounds: bool = False):
         """A new pool of zeros."""
-        size = kv_chunk_bytes(kv_heads, head_dim, block_tokens)
+        size = kv_chunk_bytes(kv_heads, head_dim, block_tokens, bounds)
         return cls(_torch().zeros(layers, 2, slots, size, dtype=_torch().uint8, device=device),
-                   kv_heads, head_dim, block_tokens)
+                   kv_heads, head_dim, block_tokens, bounds)
 
     def check(self) -> None:
         """Synchronise and raise if a call found bad device data."""
@@ -592,6 +595,91 @@ class DeviceSharedAttention:
         self._call = cx.kv_call("cascade_attention_shared", kv.c_pool, layer, kv.c_format, batch.c_batch,
                                 batch.c_table, self.c_args, self.c_shared, self.ws_ptr, self.ws_bytes,
                                 kv.status.data_ptr())
+
+    def run(self, stream=None) -> None:
+        _launch(self._call, self.kv.pool.device, stream)
+
+
+def _needs_bounds(kv: DeviceKvPool) -> None:
+    if not kv.bounds:
+        raise ValueError("the pool's chunks hold no bounds: make it with bounds=True")
+
+
+class DeviceKvBounds:
+    """cascade_kv_bounds with its arguments laid out: `run` brings the bounds of
+    the batch's keys in `layer` up to date, in the blocks of the new tokens or,
+    with `whole`, in all blocks."""
+
+    def __init__(self, kv: DeviceKvPool, batch: KvBatch, whole: bool = False, layer: int = 0):
+        _needs_bounds(kv)
+        self.kv, self.batch, self.layer = kv, batch, layer
+        _check_device(kv.pool.device, *batch.tensors)
+        self._call = cx.kv_call("cascade_kv_bounds", kv.c_pool, layer, kv.c_format, batch.c_batch,
+                                batch.c_table, int(whole), kv.status.data_ptr())
+
+    def run(self, stream=None) -> None:
+        _launch(self._call, self.kv.pool.device, stream)
+
+
+def _selection(selected, kv: DeviceKvPool, batch: KvBatch) -> int:
+    """Address of a selection [tokens, KV heads, blocks]."""
+    if selected.dim() != 3 or selected.shape[0] < batch.tokens or selected.shape[1] != kv.kv_heads or \
+            selected.shape[2] < 1:
+        raise ValueError("a selection is [tokens, KV heads, blocks]")
+    return _check_array(selected, _torch().int32, 0, "selected")
+
+
+class DeviceKvSelect:
+    """cascade_kv_select with its arguments and workspace laid out: `run` writes
+    the blocks that q [tokens, query heads, dims] reads in `layer` to `selected`
+    (int32 [tokens, KV heads, blocks]), the first `sink` and the last `recent` among
+    them.  The pool's bounds have to be up to date (DeviceKvBounds)."""
+
+    def __init__(self, kv: DeviceKvPool, batch: KvBatch, q, selected, sink: int = 0, recent: int = 1,
+                 layer: int = 0, workspace=None):
+        _needs_bounds(kv)
+        if q.shape[0] < batch.tokens or q.shape[2] != kv.head_dim:
+            raise ValueError("q does not fit the batch or the pool")
+        self.kv, self.batch, self.layer = kv, batch, layer
+        self.tensors = (q, selected)
+        _check_device(kv.pool.device, *self.tensors, *batch.tensors, workspace)
+        self.c_args = cx.Select(_dtype(q), q.shape[1], selected.shape[-1], sink, recent, kv_rows(q),
+                                _selection(selected, kv, batch))
+        size = cx.cascade_kv_select_workspace_bytes(kv.c_format, batch.c_batch)
+        self.workspace, self.ws_ptr, self.ws_bytes = _workspace(workspace, size, q.device)
+        self._call = cx.kv_call("cascade_kv_select", kv.c_pool, layer, kv.c_format, batch.c_batch,
+                                batch.c_table, self.c_args, self.ws_ptr, self.ws_bytes,
+                                kv.status.data_ptr())
+
+    def run(self, stream=None) -> None:
+        _launch(self._call, self.kv.pool.device, stream)
+
+
+class DeviceSelectedAttention:
+    """cascade_attention_selected with its arguments and workspace laid out:
+    DeviceAttention of each token and KV head over the blocks that `selected`
+    (int32 [tokens, KV heads, blocks], as DeviceKvSelect writes it) lists."""
+
+    def __init__(self, kv: DeviceKvPool, batch: KvBatch, q, selected, out, scale: float,
+                 softcap: float = 0.0, lse=None, layer: int = 0, workspace=None):
+        torch = _torch()
+        if q.shape != out.shape or q.dtype != out.dtype or q.shape[0] < batch.tokens or \
+                q.shape[2] != kv.head_dim:
+            raise ValueError("q and out do not fit the batch, the pool or each other")
+        self.kv, self.batch, self.layer = kv, batch, layer
+        self.tensors = (q, out, lse, selected)
+        _check_device(kv.pool.device, *self.tensors, *batch.tensors, workspace)
+        heads, keep = q.shape[1], selected.shape[-1]
+        self.c_args = cx.Attention(
+            _dtype(q), heads, scale, softcap, kv_rows(q), kv_rows(out),
+            None if lse is None else _check_array(lse, torch.float32, batch.tokens * heads, "lse"), None, 0)
+        size = cx.cascade_attention_selected_workspace_bytes(kv.c_format, batch.c_batch, heads, keep)
+        if size == 0:
+            raise ValueError("query heads or selected blocks outside the domain")
+        self.workspace, self.ws_ptr, self.ws_bytes = _workspace(workspace, size, q.device)
+        self._call = cx.kv_call("cascade_attention_selected", kv.c_pool, layer, kv.c_format, batch.c_batch,
+                                batch.c_table, self.c_args, _selection(selected, kv, batch), keep,
+                                self.ws_ptr, self.ws_bytes, kv.status.data_ptr())
 
     def run(self, stream=None) -> None:
         _launch(self._call, self.kv.pool.device, stream)
