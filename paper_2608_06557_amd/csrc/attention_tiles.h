@@ -193,10 +193,16 @@ __device__ __forceinline__ float capped(float x, float cap_in, float cap_y, floa
   return fabsf(y) < 0.5f ? x * qk * series : cap * t;
 }
 
-// What of a batch a launch attends: all that its rows see; or, where requests
-// share their first tokens, those for the rows of a whole group at once (each
-// row's m, sum and O go to `states`), and then the rest, which goes on from there.
-enum class Form { kWhole, kPrefix, kRest };
+// Requests one by one, or with the tokens that a group of them shares taken
+// once for all of the group's rows, beside what is left of each request.
+enum class Form { kWhole, kShared };
+
+// Where what a segment made of a row is found: what, and for parts the
+// workgroup of the second, the last's and the row within the tile.
+struct Source {
+  int kind, w, last, row;
+};
+enum : int { kNothing, kWritten, kState, kParts };  // kParts + Attention::which
 
 struct Attention : Cuts {
   KvView kv;
@@ -217,72 +223,70 @@ struct Attention : Cuts {
   float *parts;            // [gridDim][2][rows][kDim]
   float *part_sums;        // [gridDim][2][rows][2]: m and sum
   int32_t *status;
+  // Form::kShared
   const int32_t *leader, *shared_len;  // of each request, and of a group's first
-  int max_tokens;          // most rows' tokens of one group
-  float *states;           // [n_tokens][q_heads][kDim], as parts
-  float *state_sums;       // [n_tokens][q_heads][2]
+  int max_tokens;          // most new tokens of one group
+  int which;               // of the two kernels
+  float *states;           // [2][n_tokens][q_heads][kDim], as parts: of a request's segments, and of a group's
+  float *state_sums;       // [2][n_tokens][q_heads][2]
+  Source *sources;         // [2][n_tokens][KV heads]
 };
 
-// A request as a launch takes it: kPrefix, the group that request i is the last
-// of; kRest, the request without the tokens that it shares.
-struct Request : KvRequest {
-  int shared;  // kRest: tokens of its prefix
+// The list of Form::kShared holds segments of requests, and of groups, whose
+// `count` is negative; `ids` are their first rows, turned over where a request is
+// in a group.
+struct SharedList : List {
+  int *row;  // their first entries in the table
+  __device__ __forceinline__ SharedList(char *lds, int n) : List(lds, n + n / 2), row(count + n + n / 2) {}
+};
+// A group has two requests at least: one of its own shares nothing.
+__host__ __device__ constexpr int shared_list_bytes(int n) { return (24 * (n + n / 2) + 8 + 15) & ~15; }
+template <Form kForm> struct FormOf {
+  typedef List list;
+  typedef Segments segments;
+  static __host__ __device__ constexpr int bytes(int n) { return list_bytes(n); }
+};
+template <> struct FormOf<Form::kShared> {
+  typedef SharedList list;
+  typedef MixedSegments segments;
+  static __host__ __device__ constexpr int bytes(int n) { return shared_list_bytes(n); }
 };
 
-// `kCheck`: with all that is asked of the request, before it goes into the list.
-template <Form kForm, bool kUniform, bool kCheck = false>
-__device__ __forceinline__ Request request_of(const Attention &a, int i) {
-  const auto load = [](const int32_t *p) { return kUniform ? uniform_load(p) : *p; };
+// A segment's request, or group, as a list has it.
+struct Item : KvRequest {
+  bool even;     // every row sees all of its tokens
+  bool grouped;  // its rows' results are joined with another's
+};
+template <Form kForm, typename L>
+__device__ __forceinline__ Item item_of(const Attention &a, const L &list, int at) {
+  Item r = {};
   if constexpr (kForm == Form::kWhole) {
-    return Request{kv_request<kUniform>(a.batch, a.row_offsets, a.kv.block_shift, i), 0};
-  } else if constexpr (kForm == Form::kPrefix) {
-    Request r = {};
-    r.ok = true;
-    const int first = load(a.leader + i);
-    if (kCheck) {
-      // a group's requests are neighbours
-      r.ok = first >= 0 && first <= i &&
-             (first == i || (load(a.leader + i - 1) == first && load(a.leader + first) == first));
-      if (!r.ok) return r;
-      if (i + 1 < a.batch.n && load(a.leader + i + 1) == first) return r;  // a later one stands for the group
-    }
-    r.first = load(a.batch.token_offsets + first);
-    const int end = load(a.batch.token_offsets + i + 1);
-    r.len = load(a.shared_len + first);
-    r.row = load(a.row_offsets + first);
-    const int row_end = load(a.row_offsets + first + 1);
-    r.count = (int)((unsigned)end - (unsigned)r.first);
-    if (kCheck)
-      r.ok = r.first >= 0 && end >= r.first && end <= a.batch.n_tokens && r.count <= a.max_tokens && r.len >= 0 &&
-             r.len <= kMaxKvLen && r.row >= 0 && row_end >= r.row && row_end <= a.batch.n_entries &&
-             r.len >> a.kv.block_shift <= row_end - r.row;
-    if (r.len == 0) r.count = 0;
-    return r;
+    static_cast<KvRequest &>(r) = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift,
+                                                   __builtin_amdgcn_readfirstlane(list.ids[at]));
   } else {
-    Request r = {kv_request<kUniform>(a.batch, a.row_offsets, a.kv.block_shift, i), 0};
-    const int first = load(a.leader + i), blocks = a.kv.block_shift;
-    if (kCheck) {
-      r.ok &= first >= 0 && first <= i &&
-              (first == i || (load(a.leader + i - 1) == first && load(a.leader + first) == first));
-      if (!r.ok) return r;
-    }
-    r.shared = load(a.shared_len + first);
-    if (kCheck) {
-      r.ok = r.shared >= 0 && (r.shared & ((1 << blocks) - 1)) == 0 && (long long)r.shared + r.count <= r.len;
-      // the last shared block has to be the first request's (the others are taken on trust)
-      if (r.ok && r.shared && first != i) {
-        const int other = load(a.row_offsets + first), at = (r.shared >> blocks) - 1;
-        r.ok = other >= 0 && other <= a.batch.n_entries - 1 - at && a.slots[other + at] == a.slots[r.row + at];
-      }
-      if (!r.ok) return r;
-    }
-    r.row += r.shared >> blocks;
-    r.len -= r.shared;
-    return r;
+    const int first = __builtin_amdgcn_readfirstlane(list.ids[at]);
+    const int count = __builtin_amdgcn_readfirstlane(list.count[at]);
+    r.even = count < 0;
+    r.count = r.even ? -count : count;
+    r.grouped = first < 0;
+    r.first = first < 0 ? ~first : first;
+    r.len = __builtin_amdgcn_readfirstlane(list.len[at]);
+    r.row = __builtin_amdgcn_readfirstlane(list.row[at]);
+  }
+  return r;
+}
+
+// Says where a segment's rows are found.  Called by all threads.
+__device__ __forceinline__ void tell(const Attention &a, const Item &r, int head, int tile, Source s) {
+  const int first = tile * a.tile_tokens, tokens = min(a.tile_tokens, r.count - first);
+  for (int j = threadIdx.x; j < tokens; j += blockDim.x) {
+    const int64_t at = (int64_t)(r.first + first + j) * a.kv.kv_heads + head;
+    const int64_t other = (int64_t)a.batch.n_tokens * a.kv.kv_heads;
+    s.row = j * a.group;
+    a.sources[at + (r.even ? other : 0)] = s;
+    if (!r.grouped) a.sources[at + other] = Source{kNothing, 0, 0, 0};
   }
 }
-template <Form kForm> struct SegmentsOf { typedef Segments type; };
-template <> struct SegmentsOf<Form::kPrefix> { typedef EvenSegments type; };
 
 // ---------------------------------------------------------------- the work
 
@@ -316,26 +320,22 @@ struct Range {
   int items;  // requests in the list
   int group;  // which range it is
 
-  // Fills the list and finds the range; false if there is none.  Called by all
-  // threads.  Records the segment that the range's begin is the first cut of.
-  template <int kW, Form kForm>
-  __device__ __forceinline__ bool find(const Attention &a, const List &list, unsigned long long *scan) {
-    typedef typename SegmentsOf<kForm>::type Segs;
-    const int lane = lane_id();
-    int n = 0;
-    long long total = 0;
+  // Fills the list: its length and cost.  Called by all threads.
+  template <int kW>
+  static __device__ __forceinline__ void fill(const Attention &a, const List &list, unsigned long long *scan, int &n,
+                                              long long &total) {
     for (int i0 = 0; i0 < a.batch.n; i0 += 64 * kW) {
       const int i = i0 + threadIdx.x;
       unsigned long long v[2] = {0, 0}, all[2];
-      Request r = {};
+      KvRequest r = {};
       if (i < a.batch.n) {
-        r = request_of<kForm, false, true>(a, i);
+        r = kv_request(a.batch, a.row_offsets, a.kv.block_shift, i);
         if (!r.ok) {
           kv_report(a.status);
         } else {
           const int64_t rows = (int64_t)r.count * a.group;
           if (rows > a.min_rows && rows <= a.max_rows)
-            v[0] = Segs(r.len, r.count, a.tile_tokens).total() * a.kv.kv_heads;
+            v[0] = Segments(r.len, r.count, a.tile_tokens).total() * a.kv.kv_heads;
         }
       }
       const unsigned long long cost = v[0];
@@ -351,6 +351,92 @@ struct Range {
       n += __builtin_amdgcn_readfirstlane((int)all[1]);
       total += first_lane(all[0]);
     }
+  }
+
+  // The same of requests that share their first tokens: a thread puts its
+  // request in, without them, and if it is the last of its group the group.
+  // What it needs comes in two rounds of loads; what is only told and not
+  // relied on is looked up by one workgroup.
+  template <int kW>
+  static __device__ __forceinline__ void fill(const Attention &a, const SharedList &list, unsigned long long *scan,
+                                              int &n, long long &total) {
+    const int shift = a.kv.block_shift;
+    for (int i0 = 0; i0 < a.batch.n; i0 += 64 * kW) {
+      const int i = i0 + threadIdx.x;
+      unsigned long long v[2] = {0, 0}, all[2];
+      KvRequest r = {}, g = {};  // of the request, of its group
+      unsigned long long cost = 0, group_cost = 0;
+      int shared = 0;
+      if (i < a.batch.n) {
+        r = kv_request(a.batch, a.row_offsets, shift, i);
+        const int first = a.leader[i], before = i > 0 ? a.leader[i - 1] : -1;
+        const int after = i + 1 < a.batch.n ? a.leader[i + 1] : -1;
+        // a group's requests are neighbours
+        r.ok &= first >= 0 && first <= i && (first == i || before == first);
+        if (r.ok && (first < i || after == first)) {
+          shared = a.shared_len[first];
+          const int first_row = a.row_offsets[first], first_token = a.batch.token_offsets[first];
+          r.ok = shared >= 0 && (shared & ((1 << shift) - 1)) == 0 && (long long)shared + r.count <= r.len &&
+                 first_row >= 0 && first_row <= a.batch.n_entries - (shared >> shift);
+          if (r.ok && shared && after != first) {
+            g.first = first_token;
+            g.count = (int)((unsigned)(r.first + r.count) - (unsigned)first_token);
+            g.len = shared;
+            g.row = first_row;
+            g.ok = first_token >= 0 && first_token <= r.first && g.count <= a.max_tokens;
+            if (!g.ok) kv_report(a.status);
+          }
+          if (r.ok && blockIdx.x == 0) {
+            const int last = (shared >> shift) - 1;
+            if (a.leader[first] != first || (shared && a.slots[first_row + last] != a.slots[r.row + last]))
+              kv_report(a.status);
+          }
+        }
+        if (!r.ok) {
+          kv_report(a.status);
+        } else {
+          r.row += shared >> shift;
+          r.len -= shared;
+          const int64_t rows = (int64_t)r.count * a.group, group_rows = (int64_t)g.count * a.group;
+          if (rows > a.min_rows && rows <= a.max_rows)
+            cost = MixedSegments(r.len, r.count, a.tile_tokens).total() * a.kv.kv_heads;
+          if (g.ok && group_rows > a.min_rows && group_rows <= a.max_rows)
+            group_cost = MixedSegments(g.len, -g.count, a.tile_tokens).total() * a.kv.kv_heads;
+        }
+      }
+      v[0] = cost + group_cost;
+      v[1] = (cost > 0) + (group_cost > 0);
+      block_exclusive_scan<2, unsigned long long, kW>(v, all, scan);
+      int at = n + (int)v[1];
+      if (cost) {
+        list.before[at] = total + v[0];
+        list.ids[at] = shared ? ~r.first : r.first;
+        list.len[at] = r.len;
+        list.count[at] = r.count;
+        list.row[at++] = r.row;
+      }
+      if (group_cost) {
+        list.before[at] = total + v[0] + cost;
+        list.ids[at] = ~g.first;
+        list.len[at] = g.len;
+        list.count[at] = -g.count;
+        list.row[at] = g.row;
+      }
+      n += __builtin_amdgcn_readfirstlane((int)all[1]);
+      total += first_lane(all[0]);
+    }
+  }
+
+  // Fills the list and finds the range; false if there is none.  Called by all
+  // threads.  Records the segment that the range's begin is the first cut of.
+  template <int kW, Form kForm>
+  __device__ __forceinline__ bool find(const Attention &a, const typename FormOf<kForm>::list &list,
+                                       unsigned long long *scan) {
+    typedef typename FormOf<kForm>::segments Segs;
+    const int lane = lane_id();
+    int n = 0;
+    long long total = 0;
+    fill<kW>(a, list, scan, n, total);
     if (threadIdx.x == 0) list.before[n] = total;
     __syncthreads();
 
@@ -359,7 +445,7 @@ struct Range {
     const int groups = ranges(a, total, gridDim.x);
     const int block = blockIdx.x;
     if (block >= groups || n == 0) {
-      if (threadIdx.x == 0) a.splits[block] = Split{-1, 0, 0, 0};
+      if (kForm == Form::kWhole && threadIdx.x == 0) a.splits[block] = Split{-1, 0, 0, 0};
       return false;
     }
     const int w = groups >= 8 ? (block & 7) * (groups >> 3) + (block >> 3) : block;
@@ -373,7 +459,14 @@ struct Range {
     items = n;
     group = w;
 
-    if (threadIdx.x == 0) a.splits[w] = first_cut<Segs>(a, list, at, prev, total, groups);
+    if constexpr (kForm == Form::kWhole) {
+      if (threadIdx.x == 0) a.splits[w] = first_cut<Segs>(a, list, at, prev, total, groups);
+    } else if (at.key > 0) {
+      const Split s = first_cut<Segs>(a, list, at, prev, total, groups);
+      // part 0 ends the range of the workgroup before the cut, the others begin theirs
+      if (s.last >= w)
+        tell(a, item_of<kForm>(a, list, at.item), at.head, at.tile, Source{kParts + a.which, w, s.last, 0});
+    }
     return true;
   }
 };
@@ -621,9 +714,9 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
   typedef typename El<kType>::v8 v8;
   extern __shared__ __align__(16) char lds[];
   __shared__ unsigned long long scan[2 * kWaves];
-  const List list(lds, a.batch.n);
+  const typename FormOf<kForm>::list list(lds, a.batch.n);
   // the waves' m and sum, and their O or before it q
-  float *const ms = reinterpret_cast<float *>(lds + list_bytes(a.batch.n)), *const os = ms + 2 * kWaves * 16;
+  float *const ms = reinterpret_cast<float *>(lds + FormOf<kForm>::bytes(a.batch.n)), *const os = ms + 2 * kWaves * 16;
   char *const qs = reinterpret_cast<char *>(os);
   static_assert(kRows * kDim * 2 <= 4 * kWaves * 16 * kPitch, "q fits the place of O");
   const int lane = lane_id(), g = lane >> 4;
@@ -638,9 +731,8 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
   Rowset<kType, kDim, kTiles, kCap> r;
   while (at.item < n) {
     at = uniform(at);  // the compiler does not see that it is
-    const int id = __builtin_amdgcn_readfirstlane(list.ids[at.item]);
-    const Request req = request_of<kForm, true>(a, id);
-    const typename SegmentsOf<kForm>::type seg(req.len, req.count, a.tile_tokens);
+    const Item req = item_of<kForm>(a, list, at.item);
+    const typename FormOf<kForm>::segments seg(req.len, req.even ? -req.count : req.count, a.tile_tokens);
     const int length = (int)seg.length(at.tile);
     const bool last = end.item == at.item && end.head == at.head && end.tile == at.tile;
     const int stop = last ? end.key : length;
@@ -653,37 +745,20 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
     for (int t = 0; t < kTiles; ++t) {
       const int row = 16 * t + (lane & 15), token = at.tile * a.tile_tokens + row / a.group;
       const bool valid = row < tile_rows && token < req.count;
-      r.limit[t] = !valid ? -1 : kForm == Form::kPrefix ? req.len - 1 : shown + token;
+      r.limit[t] = !valid ? -1 : req.even ? req.len - 1 : shown + token;
       const int back = req.count - 1 - token;
       r.log_at[t] = a.logs && valid && back < a.window ? log_place(a, at.head, back, row % a.group) : -1;
       any |= r.log_at[t] >= 0;
     }
     float *const logs = kForm == Form::kWhole && __any(any) ? first_logs(a, req.row) : nullptr;
     r.clear();
-    if constexpr (kForm == Form::kRest) {
-      if (at.key == 0 && req.shared && wave == 0) {
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-          const int row = 16 * t + (lane & 15), token = at.tile * a.tile_tokens + row / a.group;
-          if (r.limit[t] < 0) continue;
-          const int64_t from = (int64_t)(req.first + token) * a.q_heads + at.head * a.group + row % a.group;
-          const f2 ms = *reinterpret_cast<const f2 *>(a.state_sums + 2 * from);
-          r.m[t] = ms[0];
-          r.sum[t] = r.used[t] = g == 0 ? ms[1] : 0.f;
-#pragma unroll
-          for (int d = 0; d < kDim / 16; ++d)
-            r.o[t][d] = *reinterpret_cast<const f4 *>(a.states + from * kDim + 16 * d + 4 * g);
-        }
-      }
-    }
 
     // every row sees the tokens before clear_end, none those from key_end on
     const int first_token = at.tile * a.tile_tokens;
     const int last_token = min(first_token + a.tile_tokens, req.count) - 1;
-    const bool all = kForm == Form::kPrefix;
-    const int clear_end = __builtin_amdgcn_readfirstlane(all ? req.len : shown + first_token + 1);
+    const int clear_end = __builtin_amdgcn_readfirstlane(req.even ? req.len : shown + first_token + 1);
     const int key_end =
-        __builtin_amdgcn_readfirstlane(min(min(stop, req.len), all ? req.len : shown + last_token + 1));
+        __builtin_amdgcn_readfirstlane(min(min(stop, req.len), req.even ? req.len : shown + last_token + 1));
     const int len = __builtin_amdgcn_readfirstlane(req.len);
     // the same in all waves; a request may have no blocks where nothing is seen
     if (at.key < key_end) {
@@ -801,6 +876,8 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
     }
     const bool whole = at.key == 0 && stop == length;
     const int64_t part = ((int64_t)w * 2 + (at.key > 0 ? 0 : 1)) * kRows;
+    if (kForm == Form::kShared && whole)
+      tell(a, req, at.head, at.tile, Source{req.grouped ? kState : kWritten, 0, 0, 0});
     // one row set at a time
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
@@ -833,8 +910,9 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
             sum += ms[(k * 16 + n16) * 2 + 1] * __builtin_amdgcn_exp2f(ms[(k * 16 + n16) * 2] - m);
           const int row = 16 * t + n16, tok = at.tile * a.tile_tokens + row / a.group;
           if (row >= tile_rows || tok >= req.count) continue;
-          if (kForm == Form::kPrefix && whole) {
-            const int64_t to = (int64_t)(req.first + tok) * a.q_heads + at.head * a.group + row % a.group;
+          if (kForm == Form::kShared && whole && req.grouped) {
+            const int64_t to = ((req.even ? a.batch.n_tokens : 0) + (int64_t)(req.first + tok)) * a.q_heads +
+                               at.head * a.group + row % a.group;
             *reinterpret_cast<f4 *>(a.states + to * kDim + d0 + d) = o;
             if (d0 + d == 0) *reinterpret_cast<f2 *>(a.state_sums + 2 * to) = f2{m, sum};
           } else if (whole) {
@@ -880,24 +958,24 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void attentio
 // steps).  64 rows to a wave halve the LDS reads, but leave one wave to a SIMD and
 // take 25 % longer.
 constexpr int stage_tokens(int dim) { return dim == 256 ? 32 : 64; }
-constexpr int tile_waves(int dim) { return 2 * stage_tokens(dim) / 16; }
-constexpr int tile_rows(int dim) { return 32 * tile_waves(dim); }
+constexpr int tile_waves(int stage) { return 2 * stage / 16; }
+constexpr int tile_rows(int stage) { return 32 * tile_waves(stage); }
 // of LDS: K, V, and what of their scales the type does not hold
-constexpr int stage_bytes(int type, int dim) {
-  return stage_tokens(dim) * dim * 4 + (type == CASCADE_F16 ? stage_tokens(dim) / 16 * 8 : 0);
+constexpr int stage_bytes(int type, int dim, int stage) {
+  return stage * dim * 4 + (type == CASCADE_F16 ? stage / 16 * 8 : 0);
 }
-template <int kType, int kDim, Cap kCap, Form kForm = Form::kWhole>
-__global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void tile_kernel(Attention a) {
+template <int kType, int kDim, Cap kCap, Form kForm = Form::kWhole, int kStage = stage_tokens(kDim)>
+__global__ __launch_bounds__(64 * tile_waves(kStage), kDim == 256 ? 1 : 2) void tile_kernel(Attention a) {
   typedef El<kType> E;
   typedef typename E::v8 v8;
-  constexpr int kSlices = kDim / 64, kOut = kDim / 32, kTW = tile_waves(kDim);
-  constexpr int kStage = stage_tokens(kDim), kSubs = kStage / 16, kHalves = kStage / 32;
+  constexpr int kSlices = kDim / 64, kOut = kDim / 32, kTW = tile_waves(kStage);
+  constexpr int kSubs = kStage / 16, kHalves = kStage / 32;
   constexpr int kSide = kStage * kDim * 2;  // bytes of a stage's K or V operands
   constexpr bool kBounded = E::kBounded;
   extern __shared__ __align__(16) char lds[];
   __shared__ unsigned long long scan[2 * kTW];
-  const List list(lds, a.batch.n);
-  char *const stages = lds + list_bytes(a.batch.n);
+  const typename FormOf<kForm>::list list(lds, a.batch.n);
+  char *const stages = lds + FormOf<kForm>::bytes(a.batch.n);
   const int lane = lane_id(), n32 = lane & 31, hg = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(wave_id());
   Range range;
@@ -908,9 +986,8 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
 
   while (at.item < items) {
     at = uniform(at);  // the compiler does not see that it is
-    const int id = __builtin_amdgcn_readfirstlane(list.ids[at.item]);
-    const Request req = request_of<kForm, true>(a, id);
-    const typename SegmentsOf<kForm>::type seg(req.len, req.count, a.tile_tokens);
+    const Item req = item_of<kForm>(a, list, at.item);
+    const typename FormOf<kForm>::segments seg(req.len, req.even ? -req.count : req.count, a.tile_tokens);
     const int length = (int)seg.length(at.tile);
     const bool last = end.item == at.item && end.head == at.head && end.tile == at.tile;
     const int stop = last ? end.key : length;
@@ -920,8 +997,7 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
     const int row = 32 * wave + n32, shown = req.len - req.count;
     const int token = at.tile * a.tile_tokens + row / a.group, head = at.head * a.group + row % a.group;
     const bool valid = row < a.tile_tokens * a.group && token < req.count;
-    const bool all = kForm == Form::kPrefix;
-    const int limit = !valid ? -1 : all ? req.len - 1 : shown + token;  // last cached token that it sees
+    const int limit = !valid ? -1 : req.even ? req.len - 1 : shown + token;  // last cached token that it sees
     v8 q[kDim / 16];
     const char *from_q = a.q.data + (int64_t)(req.first + (valid ? token : 0)) * a.q.token_stride +
                          (valid ? head : 0) * a.q.head_stride + 16 * hg;
@@ -937,9 +1013,9 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
     float *const logs = kForm == Form::kWhole && __any(log_at >= 0) ? first_logs(a, req.row) : nullptr;
     // every row of the wave sees the tokens before clear_end, no row of the tile those from block_end on
     const int clear_end = __builtin_amdgcn_readfirstlane(
-        all ? req.len : shown + at.tile * a.tile_tokens + 32 * wave / a.group + 1);
+        req.even ? req.len : shown + at.tile * a.tile_tokens + 32 * wave / a.group + 1);
     const int block_end = __builtin_amdgcn_readfirstlane(
-        min(stop, all ? req.len : min(req.len, shown + min((at.tile + 1) * a.tile_tokens, req.count))));
+        min(stop, req.even ? req.len : min(req.len, shown + min((at.tile + 1) * a.tile_tokens, req.count))));
     const int first_key = __builtin_amdgcn_readfirstlane(at.key), len = __builtin_amdgcn_readfirstlane(req.len);
 
     f16v o[kOut];
@@ -948,22 +1024,6 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
     float m = kLowest, sum = 0.f, used = 0.f;
-    const int64_t state = (int64_t)(req.first + token) * a.q_heads + head;  // its place in `states`
-    if constexpr (kForm == Form::kRest) {
-      if (at.key == 0 && req.shared && valid) {
-        const f2 ms = *reinterpret_cast<const f2 *>(a.state_sums + 2 * state);
-        m = ms[0];
-        sum = used = hg == 0 ? ms[1] : 0.f;
-#pragma unroll
-        for (int d = 0; d < kOut; ++d)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const f4 x = *reinterpret_cast<const f4 *>(a.states + state * kDim + 32 * d + 8 * j + 4 * hg);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[d][4 * j + i] = x[i];
-          }
-      }
-    }
     const bool exact = a.lse != nullptr;  // only log sums need the sum of the weights unrounded
     if (first_key < block_end) {
       // a wave carries one sub-block's K or V, a stage ahead.  Slots and scales by vector
@@ -1121,7 +1181,7 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
           if (__builtin_expect(apart, false)) scale_o(unit_of(rest(from, 1, 2 * h + u)));
         }
       };
-      char *from = stages, *to = stages + stage_bytes(kType, kDim);
+      char *from = stages, *to = stages + stage_bytes(kType, kDim, kStage);
       look(first_key);
       fetch(first_key);
       put(from);
@@ -1171,7 +1231,10 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
     used += __shfl_xor(used, 32);
     if (!exact) sum = used;
     const float even = evened(sum, used);
-    if (kForm != Form::kPrefix && valid && at.key == 0 && stop == length) {
+    const bool whole = at.key == 0 && stop == length;
+    if (kForm == Form::kShared && whole)
+      tell(a, req, at.head, at.tile, Source{req.grouped ? kState : kWritten, 0, 0, 0});
+    if (valid && whole && (kForm == Form::kWhole || !req.grouped)) {
       const float f = (sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum) * even;
       char *out = a.out.data + (int64_t)(req.first + token) * a.out.token_stride + head * a.out.head_stride + 8 * hg;
 #pragma unroll
@@ -1184,16 +1247,18 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
       if (a.lse && hg == 0)
         a.lse[(int64_t)(req.first + token) * a.q_heads + head] = (m + __builtin_amdgcn_logf(sum)) * kLn2;
     } else if (valid) {
-      const bool whole = kForm == Form::kPrefix && at.key == 0 && stop == length;
-      const int64_t part = whole ? state : ((int64_t)w * 2 + (at.key > 0 ? 0 : 1)) * tile_rows(kDim) + row;
-      float *to = (whole ? a.states : a.parts) + part * kDim + 4 * hg;
+      const bool state = kForm == Form::kShared && whole;
+      const int64_t part =
+          state ? ((req.even ? a.batch.n_tokens : 0) + (int64_t)(req.first + token)) * a.q_heads + head
+                : ((int64_t)w * 2 + (at.key > 0 ? 0 : 1)) * tile_rows(kStage) + row;
+      float *to = (state ? a.states : a.parts) + part * kDim + 4 * hg;
 #pragma unroll
       for (int d = 0; d < kOut; ++d)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           *reinterpret_cast<f4 *>(to + 32 * d + 8 * j) =
               f4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]} * even;
-      if (hg == 0) *reinterpret_cast<f2 *>((whole ? a.state_sums : a.part_sums) + 2 * part) = f2{m, sum};
+      if (hg == 0) *reinterpret_cast<f2 *>((state ? a.state_sums : a.part_sums) + 2 * part) = f2{m, sum};
     }
 
     if (last) break;
@@ -1209,14 +1274,14 @@ __global__ __launch_bounds__(64 * tile_waves(kDim), kDim == 256 ? 1 : 2) void ti
 }
 
 // Joins the parts of cut segments: a wave takes `each` rows, one after another.
-template <int kType, int kDim, Form kForm = Form::kWhole>
+template <int kType, int kDim>
 __global__ __launch_bounds__(kBlock) void join_kernel(Attention a, int rows, int each) {
   constexpr int kLanes = kDim / 4, kParts = 64 / kLanes;
   const Split s = a.splits[blockIdx.x];
   if (s.request < 0) return;
   const int lane = lane_id();
   const int row0 = __builtin_amdgcn_readfirstlane(((int)blockIdx.y * kWaves + wave_id()) * each);
-  const Request req = request_of<kForm, false>(a, s.request);
+  const KvRequest req = kv_request(a.batch, a.row_offsets, a.kv.block_shift, s.request);
   // part 0 ends the range of the workgroup before the cut, the others begin theirs
   const int w = blockIdx.x, parts = s.last - w + 2;
   for (int row = row0; row < row0 + each; ++row) {
@@ -1245,12 +1310,6 @@ __global__ __launch_bounds__(kBlock) void join_kernel(Attention a, int rows, int
     for (int d = 32; d >= kLanes; d >>= 1)
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], d);
-    if constexpr (kForm == Form::kPrefix) {
-      const int64_t to = (int64_t)(req.first + token) * a.q_heads + head;
-      if (lane < kLanes) *reinterpret_cast<f4 *>(a.states + to * kDim + 4 * lane) = o;
-      if (lane == 0) *reinterpret_cast<f2 *>(a.state_sums + 2 * to) = f2{top, sum};
-      continue;
-    }
     if (lane < kLanes) {
       const float f = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
       const u2 x = {narrow2<kType>(o[0] * f, o[1] * f), narrow2<kType>(o[2] * f, o[3] * f)};
@@ -1294,17 +1353,13 @@ inline Workspace layout(const cascade_kv_format_t *f, const cascade_kv_batch_t *
   w.splits = take(sizeof(Split) * kGroups);
   w.tile_splits = take(sizeof(Split) * kTileGroups);
   w.parts = take(sizeof(float) * kGroups * 2 * most_rows(f->head_dim) * f->head_dim);
-  w.tile_parts = take(sizeof(float) * kTileGroups * 2 * tile_rows(f->head_dim) * f->head_dim);
+  w.tile_parts = take(sizeof(float) * kTileGroups * 2 * tile_rows(stage_tokens(f->head_dim)) * f->head_dim);
   w.sums = take(sizeof(float) * kGroups * 2 * most_rows(f->head_dim) * 2);
-  w.tile_sums = take(sizeof(float) * kTileGroups * 2 * tile_rows(f->head_dim) * 2);
+  w.tile_sums = take(sizeof(float) * kTileGroups * 2 * tile_rows(stage_tokens(f->head_dim)) * 2);
   w.lse = take(window ? sizeof(float) * b->n_tokens * q_heads : 0);
   w.logs = take(window ? sizeof(float) * ((size_t)b->n_entries * f->block_tokens >> log_shift(f)) * window * q_heads : 0);
   w.total = at;
   return w;
-}
-
-inline bool heads_ok(const cascade_kv_format_t *f, int q_heads) {
-  return q_heads >= 1 && q_heads % f->kv_heads == 0 && q_heads / f->kv_heads <= 128;
 }
 
 template <Form kForm, int kType, int kDim, int kTiles>
@@ -1314,73 +1369,72 @@ void start(const Attention &a, int grid, Cap cap, hipStream_t stream) {
       cap == Cap::kWide     ? attention_kernel<kType, kDim, kTiles, Cap::kWide, kForm>
       : cap == Cap::kNarrow ? attention_kernel<kType, kDim, kTiles, Cap::kNarrow, kForm>
                             : attention_kernel<kType, kDim, kTiles, Cap::kNone, kForm>;
-  hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * kWaves), list_bytes(a.batch.n) + mix, stream, a);
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * kWaves), FormOf<kForm>::bytes(a.batch.n) + mix, stream, a);
 }
 
-template <Form kForm, int kType, int kDim>
-void start_tiles(const Attention &a, Cap cap, hipStream_t stream) {
-  auto kernel = cap == Cap::kWide     ? tile_kernel<kType, kDim, Cap::kWide, kForm>
-                : cap == Cap::kNarrow ? tile_kernel<kType, kDim, Cap::kNarrow, kForm>
-                                      : tile_kernel<kType, kDim, Cap::kNone, kForm>;
-  hipLaunchKernelGGL(kernel, dim3(kTileGroups), dim3(64 * tile_waves(kDim)),
-                     list_bytes(a.batch.n) + 2 * stage_bytes(kType, kDim), stream, a);
+template <Form kForm, int kType, int kDim, int kStage>
+void start_tiles(const Attention &a, int grid, Cap cap, hipStream_t stream) {
+  auto kernel = cap == Cap::kWide     ? tile_kernel<kType, kDim, Cap::kWide, kForm, kStage>
+                : cap == Cap::kNarrow ? tile_kernel<kType, kDim, Cap::kNarrow, kForm, kStage>
+                                      : tile_kernel<kType, kDim, Cap::kNone, kForm, kStage>;
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * tile_waves(kStage)),
+                     FormOf<kForm>::bytes(a.batch.n) + 2 * stage_bytes(kType, kDim, kStage), stream, a);
 }
 
-// One form of a batch; `tokens`: most new tokens of a request, or of a group.
+// How the few rows of a request, or of a group, are taken: as many as fit a
+// wave's tiles.  `most`: rows of the largest; beyond most_rows() row tiles take
+// it, and what has up to 32 rows goes beside them into the first kernel.
+inline int few_rows(int64_t most, int dim) { return most <= 16 ? 16 : most <= 32 || most > most_rows(dim) ? 32 : 64; }
+
 template <Form kForm, int kType, int kDim>
-void attend(Attention a, char *ws, const Workspace &w, Cap cap, int tokens, hipStream_t s) {
-  const int64_t most = (int64_t)tokens * a.group;  // rows of a request and KV head
+int attend_few(Attention &a, char *ws, const Workspace &w, Cap cap, int small, hipStream_t s) {
   const int64_t table = (int64_t)a.batch.n_entries << a.kv.block_shift;  // no request is longer
   const int64_t keys = table * a.kv.kv_heads;
-  // few rows: 4 waves share a tile's tokens.  More: row tiles, and requests of
-  // up to 32 rows beside them in the first kernel.
-  const bool tiled = most > most_rows(kDim);
-  const int small = most <= 16 ? 16 : most <= 32 || tiled ? 32 : 64;
-  if (!tiled || a.batch.n > 1) {
-    a.min_rows = 0;
-    a.max_rows = small;
-    a.tile_tokens = small / a.group > 0 ? small / a.group : 1;
-    // Up to 512 tokens a cut costs more than it evens out (128 requests of 582
-    // tokens on average, 64 heads: 57 us, with every cut made 64).
-    a.least_keys = a.atomic_keys = table <= kUncut ? kUncut : 512;
-    a.cut_keys = 32;
-    a.range_keys = 256;
-    a.splits = reinterpret_cast<Split *>(ws + w.splits);
-    a.parts = reinterpret_cast<float *>(ws + w.parts);
-    a.part_sums = reinterpret_cast<float *>(ws + w.sums);
-    // as many workgroups as there is work for (a segment's fixed cost counts: 8
-    // requests of 100 tokens 8.0 us, without it 15.1) and as fit the GPU at once
-    const int64_t room = kCUs * waves_per_simd(kDim, small / 16);
-    const int64_t work = (keys + (int64_t)a.batch.n * a.kv.kv_heads * kFixedKeys) / a.range_keys;
-    const int grid = (int)std::min(std::min<int64_t>(kGroups, room), std::max<int64_t>(8, work));
-    if (small == 16)
-      start<kForm, kType, kDim, 1>(a, grid, cap, s);
-    else if (small == 32)
-      start<kForm, kType, kDim, 2>(a, grid, cap, s);
-    else if constexpr (kDim < 256)
-      start<kForm, kType, kDim, 4>(a, grid, cap, s);
-    if (table > a.atomic_keys)  // else none is cut
-      hipLaunchKernelGGL((join_kernel<kType, kDim, kForm>), dim3(grid, small / kWaves), dim3(kBlock), 0, s, a, small, 1);
-  }
-  if (tiled) {
-    a.min_rows = a.batch.n > 1 ? small : 0;
-    a.max_rows = INT64_MAX;
-    a.tile_tokens = tile_rows(kDim) / a.group;
-    // shorter ones are cut where there are few (64 rows of each of 8 KV heads, 2000
-    // tokens: 37 us, uncut 61), but not those of up to 16 stages (512 rows of 600
-    // tokens: 29 us, cut 35)
-    a.least_keys = 16 * stage_tokens(kDim);
-    a.atomic_keys = 2048;
-    a.cut_keys = stage_tokens(kDim);
-    a.range_keys = 256;
-    a.splits = reinterpret_cast<Split *>(ws + w.tile_splits);
-    a.parts = reinterpret_cast<float *>(ws + w.tile_parts);
-    a.part_sums = reinterpret_cast<float *>(ws + w.tile_sums);
-    start_tiles<kForm, kType, kDim>(a, cap, s);
-    if (table > a.least_keys)
-      hipLaunchKernelGGL((join_kernel<kType, kDim, kForm>), dim3(kTileGroups, tile_rows(kDim) / (2 * kWaves)), dim3(kBlock),
-                         0, s, a, tile_rows(kDim), 2);
-  }
+  a.min_rows = 0;
+  a.max_rows = small;
+  a.tile_tokens = small / a.group > 0 ? small / a.group : 1;
+  // Up to 512 tokens a cut costs more than it evens out (128 requests of 582
+  // tokens on average, 64 heads: 57 us, with every cut made 64).
+  a.least_keys = a.atomic_keys = table <= kUncut ? kUncut : 512;
+  a.cut_keys = 32;
+  a.range_keys = 256;
+  a.splits = reinterpret_cast<Split *>(ws + w.splits);
+  a.parts = reinterpret_cast<float *>(ws + w.parts);
+  a.part_sums = reinterpret_cast<float *>(ws + w.sums);
+  // as many workgroups as there is work for (a segment's fixed cost counts: 8
+  // requests of 100 tokens 8.0 us, without it 15.1) and as fit the GPU at once
+  const int64_t room = kCUs * waves_per_simd(kDim, small / 16);
+  const int64_t work = (keys + (int64_t)a.batch.n * a.kv.kv_heads * kFixedKeys) / a.range_keys;
+  const int grid = (int)std::min(std::min<int64_t>(kGroups, room), std::max<int64_t>(8, work));
+  if (small == 16)
+    start<kForm, kType, kDim, 1>(a, grid, cap, s);
+  else if (small == 32)
+    start<kForm, kType, kDim, 2>(a, grid, cap, s);
+  else if constexpr (kDim < 256)
+    start<kForm, kType, kDim, 4>(a, grid, cap, s);
+  return grid;
+}
+
+template <Form kForm, int kType, int kDim, int kStage>
+void attend_tiles(Attention &a, char *ws, const Workspace &w, Cap cap, int small, hipStream_t s) {
+  a.min_rows = small;
+  a.max_rows = INT64_MAX;
+  a.tile_tokens = tile_rows(kStage) / a.group;
+  // shorter ones are cut where there are few (64 rows of each of 8 KV heads, 2000
+  // tokens: 37 us, uncut 61), but not those of up to 16 stages (512 rows of 600
+  // tokens: 29 us, cut 35)
+  a.least_keys = 16 * stage_tokens(kDim);
+  a.atomic_keys = 2048;
+  a.cut_keys = stage_tokens(kDim);
+  a.range_keys = 256;
+  a.splits = reinterpret_cast<Split *>(ws + w.tile_splits);
+  a.parts = reinterpret_cast<float *>(ws + w.tile_parts);
+  a.part_sums = reinterpret_cast<float *>(ws + w.tile_sums);
+  start_tiles<kForm, kType, kDim, kStage>(a, kTileGroups * stage_tokens(kDim) / kStage, cap, s);
+}
+
+inline bool heads_ok(const cascade_kv_format_t *f, int q_heads) {
+  return q_heads >= 1 && q_heads % f->kv_heads == 0 && q_heads / f->kv_heads <= 128;
 }
 
 inline bool attention_ok(const cascade_attention_t *args, const cascade_kv_format_t *format) {

@@ -67,15 +67,17 @@ struct Segments {
   }
 };
 
-// The same where every row sees all of the tokens.
-struct EvenSegments {
+// The same, or with a negative count those of rows that all see every token.
+struct MixedSegments {
+  Segments causal;
+  bool even;
   long long len;
-  int count, per;
-  CASCADE_WORK_FN EvenSegments(int len, int count, int tile_tokens) : len(len), count(count), per(tile_tokens) {}
-  CASCADE_WORK_FN int tiles() const { return (count + per - 1) / per; }
-  CASCADE_WORK_FN long long length(int) const { return len; }
-  CASCADE_WORK_FN long long start(int t) const { return t * (len + kFixedKeys); }
-  CASCADE_WORK_FN long long total() const { return start(tiles()); }
+  CASCADE_WORK_FN MixedSegments(int len, int count, int tile_tokens)
+      : causal(len, count < 0 ? -count : count, tile_tokens), even(count < 0), len(len) {}
+  CASCADE_WORK_FN int tiles() const { return causal.tiles(); }
+  CASCADE_WORK_FN long long length(int t) const { return even ? len : causal.length(t); }
+  CASCADE_WORK_FN long long start(int t) const { return even ? t * (len + kFixedKeys) : causal.start(t); }
+  CASCADE_WORK_FN long long total() const { return even ? start(tiles()) : causal.total(); }
 };
 
 // floor(a / b) of whole numbers 0 <= a < 2^52, 0 < b: by doubles, whose

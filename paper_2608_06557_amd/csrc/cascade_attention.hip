@@ -53,8 +53,23 @@ __global__ __launch_bounds__(kBlock) void weight_kernel(Attention a, float *bloc
 }
 
 template <int kType, int kDim>
-int run(const Attention &a, char *ws, const Workspace &w, Cap cap, float *block_weight, hipStream_t s) {
-  attend<Form::kWhole, kType, kDim>(a, ws, w, cap, a.batch.max_new, s);
+int run(Attention a, char *ws, const Workspace &w, Cap cap, float *block_weight, hipStream_t s) {
+  const int64_t most = (int64_t)a.batch.max_new * a.group;  // rows of a request and KV head
+  const int64_t table = (int64_t)a.batch.n_entries << a.kv.block_shift;
+  const bool tiled = most > most_rows(kDim);
+  const int small = few_rows(most, kDim);
+  if (!tiled || a.batch.n > 1) {
+    const int grid = attend_few<Form::kWhole, kType, kDim>(a, ws, w, cap, small, s);
+    if (table > a.atomic_keys)  // else none is cut
+      hipLaunchKernelGGL((join_kernel<kType, kDim>), dim3(grid, small / kWaves), dim3(kBlock), 0, s, a, small, 1);
+  }
+  if (tiled) {
+    constexpr int kStage = stage_tokens(kDim), kRows = tile_rows(kStage);
+    attend_tiles<Form::kWhole, kType, kDim, kStage>(a, ws, w, cap, a.batch.n > 1 ? small : 0, s);
+    if (table > a.least_keys)
+      hipLaunchKernelGGL((join_kernel<kType, kDim>), dim3(kTileGroups, kRows / (2 * kWaves)), dim3(kBlock), 0, s, a,
+                         kRows, 2);
+  }
   if (block_weight)
     hipLaunchKernelGGL(weight_kernel, dim3((a.batch.n_entries + kWaves - 1) / kWaves), dim3(kBlock), 0,
                        s, a, block_weight);

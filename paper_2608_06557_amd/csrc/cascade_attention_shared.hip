@@ -1,28 +1,29 @@
 // cascade_attention_shared.hip -- attention of a batch whose neighbouring
 // requests share their first blocks, on gfx950.
 //
-// Softmax over a row's tokens splits at any token: with (m, sum, O) of the
-// shared ones, the rest goes on from there as from any earlier tile.  So a first
-// launch takes each group's shared tokens once for the rows of all its requests
-// (no row is masked) and leaves every row's state in 32 bits; a second takes
-// each request's other tokens, and a row's first part begins with its state.
-// Both are the kernels of attention_tiles.h: a group of many rows goes to row
-// tiles, where the products bound it instead of the reads of the cache.
+// Softmax over a row's tokens splits at any token: with (m, sum, O) of some and
+// of the others it is known of all.  So the work is a list of both: each
+// group's shared tokens once, for the rows of all its requests (no row is masked), and each
+// request's other tokens.  The kernels of attention_tiles.h take the list in one
+// go, groups of many rows as row tiles, where the products bound them instead of the
+// reads of the cache; every segment says where it left its rows, and a last launch
+// joins each row's two.
 #include "attention_shared.h"
 
 namespace cascade {
 int shared_attention_bf16(const SharedCall &c) { return attend_shared<CASCADE_BF16>(c); }
 
 namespace {
-// The workspace of attention, then the rows' states.
+// The workspace of attention, then what is known of each row.
 struct Places {
   Workspace w;
-  size_t states, sums, total;
+  size_t states, sums, sources, total;
   Places(const cascade_kv_format_t *f, const cascade_kv_batch_t *b, int q_heads) : w(layout(f, b, q_heads, 0)) {
-    const size_t rows = (size_t)b->n_tokens * q_heads;
+    const size_t rows = 2 * (size_t)b->n_tokens * q_heads;
     states = w.total;
     sums = states + aligned(sizeof(float) * rows * f->head_dim);
-    total = sums + aligned(sizeof(float) * rows * 2);
+    sources = sums + aligned(sizeof(float) * rows * 2);
+    total = sources + aligned(sizeof(Source) * 2 * b->n_tokens * f->kv_heads);
   }
 };
 }  // namespace
@@ -59,6 +60,8 @@ extern "C" int cascade_attention_shared(const cascade_kv_pool_t *pool, int32_t l
   a.max_tokens = std::min(shared->max_tokens, batch->n_tokens);
   a.states = reinterpret_cast<float *>(ws + p.states);
   a.state_sums = reinterpret_cast<float *>(ws + p.sums);
+  a.sources = reinterpret_cast<Source *>(ws + p.sources);
+  if ((int64_t)batch->n_tokens * args->q_heads > INT32_MAX / kBlock) return CASCADE_EINVAL;
   const SharedCall c = {a, ws, p.w, cap, static_cast<hipStream_t>(stream)};
   return args->dtype == CASCADE_BF16 ? shared_attention_bf16(c) : shared_attention_f16(c);
 }
