@@ -23,6 +23,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "cascade.h"
 #include "device_util.h"
 #include "kv_format.h"
@@ -181,9 +183,10 @@ struct Select {
   QRows q;
   int group;   // query heads of a KV head
   int padded;  // the same as a power of two up to 16, or a multiple of 16
+  int shift;   // log2 of a token's rows in a set
   int keep, sink, recent;
   int span;    // table entries of a workgroup
-  float *scores;  // request by request [token][KV head][block], as many as max_new tokens would take
+  float *scores;  // request by request [token][KV head][block], in whole lines of 16
   int32_t *selected;
   int32_t *status;
 };
@@ -191,155 +194,237 @@ struct Select {
 __device__ __forceinline__ int blocks_of(const KvRequest &r, int block_shift) {
   return (int)(((long long)r.len + (1 << block_shift) - 1) >> block_shift);
 }
-__device__ __forceinline__ float *scores_of(const Select &a, const KvRequest &r, int token, int head) {
-  const int64_t first = (int64_t)r.row * a.batch.max_new * a.kv.kv_heads;
-  return a.scores + first + ((int64_t)token * a.kv.kv_heads + head) * blocks_of(r, a.kv.block_shift);
+// A row's scores, and how many there is room for.  Where request i's begin: 16
+// (floor(row / 16) + i) lines' places for each token and head, which leaves room for its blocks
+// rounded up, as the next request's row is at least as many entries further.
+__device__ __forceinline__ int score_pitch(const Select &a, const KvRequest &r) {
+  return (blocks_of(r, a.kv.block_shift) + 15) & ~15;
 }
+__device__ __forceinline__ float *scores_of(const Select &a, const KvRequest &r, int i, int token, int head) {
+  const int64_t first = ((int64_t)(r.row & ~15) + 16 * i) * a.batch.max_new * a.kv.kv_heads;
+  return a.scores + first + ((int64_t)token * a.kv.kv_heads + head) * score_pitch(a, r);
+}
+
+typedef uint16_t us2 __attribute__((ext_vector_type(2)));
 
 template <int kType>
 __device__ __forceinline__ void widen2(unsigned w, float &a, float &b) {
   if constexpr (kType == CASCADE_BF16) {
-    const bf2 x = __builtin_bit_cast(bf2, w);
-    a = (float)x[0], b = (float)x[1];
+    a = __uint_as_float(w << 16), b = __uint_as_float(w & 0xffff0000u);
   } else {
     const h2 x = __builtin_bit_cast(h2, w);
     a = (float)x[0], b = (float)x[1];
   }
 }
 
-// 16 rows of queries in whole numbers, in operand order: lane % 16 is the row, lane
-// / 16 its dims 16 (lane / 16) of each 64.
+// A row of queries (16 of them, a row to lane % 16): its dims 16 (lane / 16) .. of each 64.
 template <int kType, int kDim>
-struct Queries {
-  i4 plus[kDim / 64], minus[kDim / 64];
-  int exponent;  // of the lane's row
-  bool bad = false;
-
+struct Query {
+  static constexpr unsigned kInf = kType == CASCADE_BF16 ? 0x7f80 : 0x7c00;
+  u4 w[kDim / 64][2];
   __device__ __forceinline__ void load(const Select &a, const KvRequest &r, int head, int token, int of_group,
                                        bool valid) {
     const char *from = a.q.data + (int64_t)(r.first + (valid ? token : 0)) * a.q.token_stride +
                        (int64_t)(head * a.group + (valid ? of_group : 0)) * a.q.head_stride + 32 * (lane_id() >> 4);
-    float x[kDim / 64][16], most = 0.f;
 #pragma unroll
     for (int s = 0; s < kDim / 64; ++s)
 #pragma unroll
       for (int v = 0; v < 2; ++v) {
-        const u4 w = *reinterpret_cast<const u4 *>(from + 128 * s + 16 * v);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) widen2<kType>(w[i], x[s][8 * v + 2 * i], x[s][8 * v + 2 * i + 1]);
+        w[s][v] = *reinterpret_cast<const u4 *>(from + 128 * s + 16 * v);
+        w[s][v] = valid ? w[s][v] : u4{0, 0, 0, 0};
       }
+  }
+  // The exponent of its whole numbers; elements that are not finite become 0.
+  __device__ __forceinline__ int exponent(bool &bad) {
+    auto magnitude = [&] {  // 16-bit magnitudes are in the order of their values
+      us2 most = {0, 0};
 #pragma unroll
-    for (int s = 0; s < kDim / 64; ++s)
+      for (int s = 0; s < kDim / 64; ++s)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const bool fine = __builtin_isfinite(x[s][i]);
-        bad |= valid && !fine;
-        x[s][i] = valid && fine ? x[s][i] : 0.f;
-        most = fmaxf(most, fabsf(x[s][i]));
-      }
-    most = fmaxf(most, __shfl_xor(most, 16));
-    most = fmaxf(most, __shfl_xor(most, 32));
-    // the least with most <= 127 * 2^exponent; 127 is 1.984375 * 2^6
-    const unsigned b = __float_as_uint(most);
-    exponent = max((int)(b >> 23) - 127 - 6 + ((b & 0x7fffffu) > 0x7e0000u ? 1 : 0), kMinExponent);
+        for (int i = 0; i < 8; ++i)
+          most = __builtin_elementwise_max(most, __builtin_bit_cast(us2, w[s][i >> 2][i & 3] & 0x7fff7fffu));
+      return most[0] > most[1] ? most[0] : most[1];
+    };
+    unsigned most = magnitude();
+    if (__builtin_expect(__any(most >= kInf), false)) {
+      bad |= most >= kInf;
+#pragma unroll
+      for (int s = 0; s < kDim / 64; ++s)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          unsigned x = w[s][i >> 2][i & 3];
+          x = (x & 0x7fffu) >= kInf ? x & 0xffff0000u : x;
+          x = (x >> 16 & 0x7fffu) >= kInf ? x & 0xffffu : x;
+          w[s][i >> 2][i & 3] = x;
+        }
+      most = magnitude();
+    }
+    float x, none;
+    widen2<kType>(most, x, none);
+    x = fmaxf(x, __shfl_xor(x, 16));
+    x = fmaxf(x, __shfl_xor(x, 32));
+    // the least with x <= 127 * 2^exponent; 127 is 1.984375 * 2^6
+    const unsigned b = __float_as_uint(x);
+    return max((int)(b >> 23) - 127 - 6 + ((b & 0x7fffffu) > 0x7e0000u ? 1 : 0), kMinExponent);
+  }
+};
+
+// 16 rows in whole numbers, in operand order.
+template <int kDim>
+struct Operand {
+  i4 plus[kDim / 64], minus[kDim / 64];
+  template <int kType>
+  __device__ __forceinline__ void round(const Query<kType, kDim> &q, int exponent) {
     const float inverse = __uint_as_float((unsigned)(127 - exponent) << 23);
+    // 1.5 * 2^23 and a whole number up to 127 have that number in the last byte
+    // of their sum, rounded to nearest even
+    constexpr float kMagic = 12582912.f;
 #pragma unroll
     for (int s = 0; s < kDim / 64; ++s)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        int p = 0, m = 0;
+        float x[4];
+        widen2<kType>(q.w[s][i >> 1][2 * (i & 1)], x[0], x[1]);
+        widen2<kType>(q.w[s][i >> 1][2 * (i & 1) + 1], x[2], x[3]);
+        unsigned n[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int n = (int)__builtin_rintf(x[s][4 * i + j] * inverse);
-          p |= max(n, 0) << 8 * j;
-          m |= (min(n, 0) & 255) << 8 * j;
-        }
-        plus[s][i] = p, minus[s][i] = m;
+        for (int j = 0; j < 4; ++j) n[j] = __float_as_uint(__builtin_fmaf(x[j], inverse, kMagic));
+        const unsigned low = __builtin_amdgcn_perm(n[1], n[0], 0x0c0c0400u);
+        const unsigned high = __builtin_amdgcn_perm(n[3], n[2], 0x04000c0cu);
+        const unsigned all = low | high, negative = (all >> 7 & 0x01010101u) * 255u;
+        plus[s][i] = (int)(all & ~negative);
+        minus[s][i] = (int)(all & negative);
       }
   }
 };
 
-// The scores of a wave's `kTiles` row sets over blocks begin .. end of a request.
-template <int kType, int kDim, int kTiles>
-__device__ __forceinline__ void score_blocks(const Select &a, const KvRequest &r, int head, int tile0, int begin,
-                                             int end) {
+// The bounds of 16 blocks and a head as the second operand, from where they lie:
+// lane % 16 is the block, lane / 16 its dims 16 (lane / 16) of each 64.  (Lines that
+// a load takes whole, and an exchange in LDS, are 2 % faster to read, but cost more than that.)
+template <int kDim>
+struct BlockBounds {
+  i4 upper[kDim / 64], lower[kDim / 64];
+  float scale;
+  __device__ __forceinline__ void fetch(const KvView &kv, int head, int slot, bool &bad) {
+    const bool fine = (unsigned)slot < (unsigned)kv.num_slots;
+    bad |= !fine;
+    const char *const chunk = kv.base + (fine ? slot : 0) * kv.slot_stride;
+    const char *const from = chunk + bounds_at(kv, head) + 16 * (lane_id() >> 4);
+#pragma unroll
+    for (int s = 0; s < kDim / 64; ++s) {
+      upper[s] = *reinterpret_cast<const i4 *>(from + 64 * s);
+      lower[s] = *reinterpret_cast<const i4 *>(from + kv.kv_stride + 64 * s);
+    }
+    scale = *reinterpret_cast<const float *>(chunk + scale_at(kv, head));
+  }
+};
+
+// The scores of a wave's `kTiles` row sets over blocks begin .. end of request
+// i, 16 blocks a step.  kWide: a set is a part of a token's query heads, and
+// the parts are taken one after another.  With several sets the next step's
+// bounds are on their way; with one it is the other waves that keep memory busy.
+template <int kType, int kDim, int kTiles, bool kWide>
+__device__ __forceinline__ void score_blocks(const Select &a, const KvRequest &r, int i, int head, int tile0,
+                                             int begin, int end) {
   constexpr int kSteps = kDim / 64;
+  constexpr bool kAhead = kTiles > 1;
   const int lane = lane_id(), n16 = lane & 15, g = lane >> 4;
-  const bool wide = a.padded > 16;  // a token's heads take several row sets, one after another
-  const int per_tile = wide ? 1 : 16 / a.padded, passes = wide ? a.padded / 16 : 1;
+  const int passes = kWide ? a.padded / 16 : 1, shift = kWide ? 4 : a.shift;
+  const int32_t *const slots = a.slots + r.row;
+  bool bad_query = false, bad_slot = false;
+  // the lane's row of set t
+  auto token_of = [&](int t) { return kWide ? tile0 : ((tile0 + t) << (4 - shift)) + (n16 >> shift); };
+  auto head_of = [&](int p) { return kWide ? 16 * p + n16 : n16 & ((1 << shift) - 1); };
+  auto look = [&](int b0) { return slots[min(b0 + n16, end - 1)]; };
+
   int top_all = kMinExponent;
-  if (wide) {
+  if (kWide) {
     for (int p = 0; p < passes; ++p) {
-      Queries<kType, kDim> q;
-      const int of_group = 16 * p + n16;
-      const bool valid = of_group < a.group && tile0 < r.count;
-      q.load(a, r, head, tile0, of_group, valid);
-      top_all = max(top_all, valid ? q.exponent : kMinExponent);
+      Query<kType, kDim> q;
+      const bool valid = head_of(p) < a.group && tile0 < r.count;
+      q.load(a, r, head, tile0, head_of(p), valid);
+      const int e = q.exponent(bad_query);
+      top_all = max(top_all, valid ? e : kMinExponent);
     }
 #pragma unroll
     for (int m = 8; m; m >>= 1) top_all = max(top_all, __shfl_xor(top_all, m));
   }
-  bool bad_query = false, bad_slot = false;
+  const int64_t next = (int64_t)a.kv.kv_heads * score_pitch(a, r);  // from a token to the one after it
   for (int p = 0; p < passes; ++p) {
-    Queries<kType, kDim> q[kTiles];
-    float weight[kTiles][4], pad[kTiles][4];
+    int slot = look(begin);
+    BlockBounds<kDim> now, then;
+    Operand<kDim> q[kTiles];
+    float weight[kTiles][4];
+    float *to[kTiles];  // of the lane's first token
+    int left[kTiles];   // tokens from there on
+    {
+      Query<kType, kDim> raw[kTiles];
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-      const int tile = tile0 + t, token = tile * per_tile + (wide ? 0 : n16 / a.padded);
-      const int of_group = wide ? 16 * p + n16 : n16 & (a.padded - 1);
-      const bool valid = token < r.count && of_group < a.group;
-      q[t].load(a, r, head, token, of_group, valid);
-      bad_query |= q[t].bad;
-      // relative to the largest of the token's heads: every product is exact, and none overflows
-      int top = valid ? q[t].exponent : kMinExponent;
-      for (int m = 1; m < min(a.padded, 16); m <<= 1) top = max(top, __shfl_xor(top, m));
-      if (wide) top = top_all;
-      const float w = valid ? __uint_as_float((unsigned)(127 + max(q[t].exponent - top, -126)) << 23) : 0.f;
+      for (int t = 0; t < kTiles; ++t)
+        raw[t].load(a, r, head, token_of(t), head_of(p), token_of(t) < r.count && head_of(p) < a.group);
+      now.fetch(a.kv, head, slot, bad_slot);
+      slot = look(begin + 16);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        weight[t][i] = __shfl(w, 4 * g + i);
-        pad[t][i] = weight[t][i] > 0.f ? 0.f : -__builtin_inff();
+      for (int t = 0; t < kTiles; ++t) {
+        const bool valid = token_of(t) < r.count && head_of(p) < a.group;
+        const int e = raw[t].exponent(bad_query);
+        q[t].round(raw[t], e);
+        // relative to the largest of the token's heads: every product is exact, and none overflows
+        int top = valid ? e : kMinExponent;
+        for (int m = 1; m < 1 << shift; m <<= 1) top = max(top, __shfl_xor(top, m));
+        if (kWide) top = top_all;
+        // NaN where there is no head: the larger of it and a number is the number
+        const float w = valid ? __uint_as_float((unsigned)(127 + max(e - top, -126)) << 23) : __builtin_nanf("");
+#pragma unroll
+        for (int k = 0; k < 4; ++k) weight[t][k] = __shfl(w, 4 * g + k);
+        const int first = kWide ? tile0 : ((tile0 + t) << (4 - shift)) + (4 * g >> shift);
+        to[t] = scores_of(a, r, i, first, head) + begin + n16;
+        left[t] = (4 * g & ((1 << shift) - 1)) == 0 ? r.count - first : 0;
       }
     }
+#pragma unroll 1
     for (int b0 = begin; b0 < end; b0 += 16) {
-      const int b = b0 + n16;
-      int slot = a.slots[r.row + min(b, end - 1)];
-      if ((unsigned)slot >= (unsigned)a.kv.num_slots) bad_slot = true, slot = 0;
-      const char *const chunk = a.kv.base + slot * a.kv.slot_stride;
-      const char *const from = chunk + bounds_at(a.kv, head) + 16 * g;
-      i4 upper[kSteps], lower[kSteps];
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        upper[s] = *reinterpret_cast<const i4 *>(from + 64 * s);
-        lower[s] = *reinterpret_cast<const i4 *>(from + a.kv.kv_stride + 64 * s);
+      if (kAhead) {
+        then.fetch(a.kv, head, slot, bad_slot);  // past the end the last block's
+        slot = look(b0 + 32);
       }
-      const float scale = *reinterpret_cast<const float *>(chunk + scale_at(a.kv, head));
+      const bool in = b0 + n16 < end;
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) {
         i4 sum = {0, 0, 0, 0};
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
-          sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[t].plus[s], upper[s], sum, 0, 0, 0);
-          sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[t].minus[s], lower[s], sum, 0, 0, 0);
+          sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[t].plus[s], now.upper[s], sum, 0, 0, 0);
+          sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[t].minus[s], now.lower[s], sum, 0, 0, 0);
         }
         float x[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = __builtin_fmaf((float)sum[i], weight[t][i], pad[t][i]);
-        // over the heads of a token: rows 4 g + i of the set
-        int tokens = 4;  // of the lane's 4 rows
-        if (a.padded >= 2) x[0] = fmaxf(x[0], x[1]), x[1] = fmaxf(x[2], x[3]), tokens = 2;
-        if (a.padded >= 4) x[0] = fmaxf(x[0], x[1]), tokens = 1;
-        if (a.padded >= 8) x[0] = fmaxf(x[0], __shfl_xor(x[0], 16));
-        if (a.padded >= 16) x[0] = fmaxf(x[0], __shfl_xor(x[0], 32));
+        for (int k = 0; k < 4; ++k) x[k] = (float)sum[k] * weight[t][k];
+        // over the heads of a token: rows 4 g + k of the set
+        auto put = [&](int k, float x) {
+          float *const at = to[t] + k * next;
+          const float y = __builtin_fmaf(x, now.scale, 0.f);  // no -0
+          if (in && k < left[t]) *at = kWide && p ? fmaxf(*at, y) : y;
+        };
+        if (shift >= 2) {
+          float y = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+          if (shift >= 3) y = fmaxf(y, __shfl_xor(y, 16));
+          if (shift >= 4) y = fmaxf(y, __shfl_xor(y, 32));
+          put(0, y);
+        } else if (shift == 1) {
+          put(0, fmaxf(x[0], x[1]));
+          put(1, fmaxf(x[2], x[3]));
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int token = wide ? tile0 : (tile0 + t) * per_tile + (4 * g + i * (4 / tokens)) / a.padded;
-          const bool first = (4 * g & (min(a.padded, 16) - 1)) == 0;  // of a token's lanes
-          if (i >= tokens || !first || token >= r.count || b >= end) continue;
-          float *const to = scores_of(a, r, token, head) + b;
-          const float y = x[i] * scale + 0.f;  // no -0
-          *to = p ? fmaxf(*to, y) : y;
+          for (int k = 0; k < 4; ++k) put(k, x[k]);
         }
+        to[t] += 16;
+      }
+      if (kAhead) {
+        now = then;
+      } else if (b0 + 16 < end) {
+        now.fetch(a.kv, head, slot, bad_slot);
+        slot = look(b0 + 32);
       }
     }
   }
@@ -355,140 +440,322 @@ struct Candidates {
   }
 };
 
-template <int kType, int kDim, int kTiles>
-__global__ __launch_bounds__(kBlock) void score_kernel(Select a) {
+// A workgroup has `span` table entries.  One row set to a wave: its waves take
+// heads, or parts of the entries where there are few heads, so that what lies side by
+// side is read at one time.  Several: neighbouring ones of a head, which read the same
+// bounds.
+template <int kType, int kDim, int kTiles, bool kWide>
+__global__ __launch_bounds__(kBlock, kTiles > 1 || kDim == 256 ? 2 : 5) void score_kernel(Select a) {
   __shared__ unsigned sums[kWaves];
-  const int e0 = blockIdx.x * a.span, e1 = min(e0 + a.span, a.batch.n_entries);
-  const int per_tile = a.padded > 16 ? 1 : 16 / a.padded;
-  for (int i = owner_of(a.row_offsets, a.batch.n, e0, sums); i < a.batch.n && a.row_offsets[i] < e1; ++i) {
-    const KvRequest r = kv_request(a.batch, a.row_offsets, a.kv.block_shift, i);
-    const int tile0 = blockIdx.y * kTiles;
+  // neighbouring spans on one XCD (workgroups go to the 8 in turn), where a request's queries are then in L2
+  const int span = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+  if ((int64_t)span * a.span >= a.batch.n_entries) return;
+  const int e0 = span * a.span, e1 = min(e0 + a.span, a.batch.n_entries);
+  const int per_tile = 16 >> a.shift, wave = __builtin_amdgcn_readfirstlane(wave_id());
+  const int tile0 = kTiles > 1 ? (blockIdx.y * kWaves + wave) * kTiles : blockIdx.y;
+  for (int i = __builtin_amdgcn_readfirstlane(owner_of(a.row_offsets, a.batch.n, e0, sums));
+       i < a.batch.n && uniform_load(a.row_offsets + i) < e1; ++i) {
+    const KvRequest r = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, i);
     if (!r.ok || tile0 * per_tile >= r.count) continue;
     const Candidates c(a, blocks_of(r, a.kv.block_shift));
     const int begin = max(c.begin, e0 - r.row), end = min(c.end, e1 - r.row);
     if (begin >= end) continue;
-    for (int head = wave_id(); head < a.kv.kv_heads; head += kWaves)
-      score_blocks<kType, kDim, kTiles>(a, r, head, tile0, begin, end);
+    if (kTiles > 1) {
+      score_blocks<kType, kDim, kTiles, kWide>(a, r, i, blockIdx.z, tile0, begin, end);
+    } else {
+      const int heads = a.kv.kv_heads, parts = heads >= kWaves ? 1 : kWaves / heads;
+      const int each = ((end - begin + 16 * parts - 1) / (16 * parts)) * 16;
+      for (int u = wave; u < heads * parts; u += kWaves) {
+        const int from = begin + u / heads * each, to = min(from + each, end);
+        if (from < to) score_blocks<kType, kDim, kTiles, kWide>(a, r, i, u % heads, tile0, from, to);
+      }
+    }
   }
 }
 
 // ------------------------------------------------------------------ select
 
-// Scores in ascending order as whole numbers, NaN last.
+// Scores in ascending order as whole numbers above 0 and below 2^32 - 1, NaN last.
 __device__ __forceinline__ unsigned ordered(float x) {
   const unsigned b = __float_as_uint(x);
-  if ((b & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
+  if ((b & 0x7fffffffu) > 0x7f800000u) return 0xfffffffeu;
   return b >> 31 ? ~b : b | 0x80000000u;
 }
 
-constexpr int kHeld = 8;     // scores of a thread that stay in registers
-constexpr int kDigits = 2048;
+// A list's candidates, begin .. end, of which `want` stay beside the first `sink`
+// and the last `recent` blocks; none if there is no choice.
+struct Row {
+  const float *score;
+  int32_t *out;
+  int begin, end, want;
+};
 
-__global__ __launch_bounds__(kBlock) void select_kernel(Select a) {
+// The row of token and KV head `row`, with what needs no choice written by
+// threads `lane` of `width`.
+__device__ __forceinline__ Row row_of(const Select &a, const KvRequest &q, int i, int token, int head, int lane,
+                                      int width) {
+  Row r = {nullptr, nullptr, 0, 0, 0};
+  const int j = token - q.first, last = q.len - q.count + j;  // cached token
+  const int blocks = last < 0 ? 0 : (last >> a.kv.block_shift) + 1;
+  r.out = a.selected + ((int64_t)token * a.kv.kv_heads + head) * a.keep;
+  if (blocks <= a.keep) {
+    for (int k = lane; k < a.keep; k += width) r.out[k] = k < blocks ? k : -1;
+  } else {
+    r.score = scores_of(a, q, i, j, head);
+    r.begin = a.sink, r.end = blocks - a.recent, r.want = a.keep - a.sink - a.recent;
+    for (int k = lane; k < a.sink; k += width) r.out[k] = k;
+    for (int k = lane; k < a.recent; k += width) r.out[a.keep - a.recent + k] = r.end + k;
+  }
+  return r;
+}
+
+// The least key that stays, by its digits of 11, 11 and 10 bits from the front:
+// histograms in LDS, with a place for what a lane does not count.
+constexpr int kDigits = 2048;
+typedef unsigned Hist[kDigits + 64];
+__device__ __forceinline__ int digit_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
+__device__ __forceinline__ unsigned digit_mask(int pass) { return pass == 2 ? 1023u : 2047u; }
+
+// The digit of the key that has `rank` before it, largest first; `rank` becomes its
+// rank among the `count` with that digit.
+__device__ __forceinline__ unsigned find_digit(const unsigned *hist, unsigned &rank, unsigned &count) {
+  const int lane = lane_id();
+  // 32 digits to a lane, from the largest; lanes begin at different ones, as they share banks
+  unsigned sum = 0;
+  const unsigned *const high = hist + kDigits - 32 * (lane + 1);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint4 h = *reinterpret_cast<const uint4 *>(high + 4 * ((j + lane) & 7));
+    sum += (h.x + h.y) + (h.z + h.w);
+  }
+  unsigned before = wave_inclusive_sum(sum) - sum;
+  int from = __ffsll((unsigned long long)__ballot(rank >= before && rank < before + sum)) - 1;
+  rank -= lane_value(before, from);
+  // and of those a digit to a lane
+  const int top = kDigits - 1 - 32 * from;
+  sum = lane < 32 ? hist[top - lane] : 0;
+  before = wave_inclusive_sum(sum) - sum;
+  from = __ffsll((unsigned long long)__ballot(rank >= before && rank < before + sum)) - 1;
+  rank -= lane_value(before, from);
+  count = lane_value(sum, from);
+  return top - from;
+}
+
+struct Threshold {
+  unsigned key = 0, known = 0;  // its digits so far
+  unsigned rank;                // of it among those that share them
+  unsigned equal = ~0u;         // how many of the keys that share all known digits stay
+
+  // Keys of no candidate are 0.
+  __device__ __forceinline__ void count(unsigned *hist, int pass, unsigned x) const {
+    const bool in = x && ((x ^ key) & known) == 0;
+    atomicAdd(&hist[in ? x >> digit_shift(pass) & digit_mask(pass) : kDigits + lane_id()], 1u);
+  }
+  // Takes the next digit; false if it is the last that is needed.  By each wave for itself.
+  __device__ __forceinline__ bool next(const unsigned *hist, int pass) {
+    unsigned count;
+    key |= find_digit(hist, rank, count) << digit_shift(pass);
+    known |= digit_mask(pass) << digit_shift(pass);
+    const bool all = rank + 1 == count;  // that share these digits stay
+    equal = all ? ~0u : rank + 1;        // or the first of them
+    return !all && pass < 2;
+  }
+};
+
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Writes those of 64 blocks that stay, in order, and moves on: the ones above the
+// threshold and the first of the ones at it.
+__device__ __forceinline__ void put(const Row &r, uint64_t above, uint64_t at, unsigned equal, int first,
+                                    unsigned &place, unsigned &ties) {
+  if (!(above | at)) return;
+  const bool tie = (at >> lane_id() & 1) && ties + rank_in_mask(at) < equal;
+  const uint64_t stay = above | __ballot(tie);
+  if (stay >> lane_id() & 1) r.out[place + rank_in_mask(stay)] = first + lane_id();
+  place += __popcll(stay);
+  ties += __popcll(at);
+}
+__device__ __forceinline__ void put(const Row &r, const Threshold &t, unsigned x, int first, unsigned &place,
+                                    unsigned &ties) {
+  put(r, __ballot((x & t.known) > t.key), __ballot((x & t.known) == t.key), t.equal, first, place, ties);
+}
+
+// A token and head to a wave, its candidates in registers, no barriers: for
+// many rows.
+constexpr int kHeld = 32, kRun = 16;  // registers, and those between two looks at the row's end
+__global__ __launch_bounds__(kBlock) void select_wave_kernel(Select a) {
   if (blockIdx.x == gridDim.x - 1) {
     check_requests(a.batch, a.row_offsets, a.kv.block_shift, a.status);
     return;
   }
-  __shared__ unsigned hist[kDigits], scan[kWaves], found[3], marks[2][kWaves];
-  const int token = blockIdx.x / a.kv.kv_heads, head = blockIdx.x % a.kv.kv_heads;
-  const int i = owner_of(a.batch.token_offsets, a.batch.n, token, scan);
-  if (i >= a.batch.n) return;
-  const KvRequest r = kv_request(a.batch, a.row_offsets, a.kv.block_shift, i);
-  if (!r.ok || token < r.first || token - r.first >= r.count) return;
-  const int j = token - r.first, last = r.len - r.count + j;  // cached token
-  const int blocks = last < 0 ? 0 : (last >> a.kv.block_shift) + 1;
-  int32_t *const out = a.selected + ((int64_t)token * a.kv.kv_heads + head) * a.keep;
-  const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
-  if (blocks <= a.keep) {
-    for (int k = tid; k < a.keep; k += kBlock) out[k] = k < blocks ? k : -1;
+  __shared__ alignas(16) Hist hists[kWaves];
+  __shared__ unsigned sums[kWaves];
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
+  const int64_t row = (int64_t)blockIdx.x * kWaves + wave;
+  const int token = (int)(row / a.kv.kv_heads), head = (int)(row % a.kv.kv_heads);
+  int i = owner_of(a.batch.token_offsets, a.batch.n, (int)((int64_t)blockIdx.x * kWaves / a.kv.kv_heads), sums);
+  while (i < a.batch.n && a.batch.token_offsets[i + 1] <= token) ++i;
+  if (i >= a.batch.n || token >= a.batch.n_tokens) return;
+  const KvRequest q = kv_request(a.batch, a.row_offsets, a.kv.block_shift, i);
+  if (!q.ok || token < q.first || token - q.first >= q.count) return;
+  const Row r = row_of(a, q, i, token, head, lane, 64);
+  if (r.want == 0) return;
+  const int m = __builtin_amdgcn_readfirstlane(r.end - r.begin);
+  float x[kHeld];
+  auto each_run = [&](auto f) {
+#pragma unroll
+    for (int k0 = 0; k0 < kHeld; k0 += kRun) {
+      if (64 * k0 >= m) break;
+#pragma unroll
+      for (int k = k0; k < k0 + kRun; ++k) f(k);
+    }
+  };
+  float least = __builtin_inff(), most = -__builtin_inff();
+  bool odd = false;  // a score that is no number
+  each_run([&](int k) {
+    x[k] = r.score[r.begin + min(64 * k + lane, m - 1)];
+    odd |= !__builtin_isfinite(x[k]);
+  });
+  each_run([&](int k) {
+    least = fminf(least, x[k]), most = fmaxf(most, x[k]);
+    x[k] = 64 * k + lane < m ? x[k] : __builtin_nanf("");  // no candidate
+  });
+  unsigned *const hist = hists[wave];
+  auto clear = [&] {
+#pragma unroll
+    for (int j = 0; j < kDigits / 256; ++j) reinterpret_cast<uint4 *>(hist)[64 * j + lane] = uint4{0, 0, 0, 0};
+    wave_sync();
+  };
+  clear();
+  // equal parts of the scores' range as digits: fewer scores share one than share
+  // 11 bits, adds to one place in LDS take turns, and one pass leaves few
+#pragma unroll
+  for (int d = 32; d; d >>= 1) {
+    least = fminf(least, __shfl_xor(least, d));
+    most = fmaxf(most, __shfl_xor(most, d));
+  }
+  const float per = (kDigits - 1) / (most - least);
+  unsigned place = a.sink, ties = 0;
+  if (!__any(odd) && __builtin_isfinite(per)) {
+    auto digit_of = [&](float x) { return min((unsigned)((x - least) * per), kDigits - 1u); };
+    each_run([&](int k) { atomicAdd(&hist[x[k] == x[k] ? digit_of(x[k]) : kDigits + lane], 1u); });
+    wave_sync();
+    unsigned rank = r.want - 1, count;
+    const unsigned digit = find_digit(hist, rank, count);
+    if (count <= 64) {
+      wave_sync();
+      float *const few = reinterpret_cast<float *>(hist);
+      unsigned n = 0;
+      each_run([&](int k) {
+        const uint64_t in = __ballot(x[k] == x[k] && digit_of(x[k]) == digit);
+        if (!in) return;
+        if (in >> lane & 1) few[n + rank_in_mask(in)] = x[k];
+        n += __popcll(in);
+      });
+      wave_sync();
+      const float mine = lane < (int)count ? few[lane] : -__builtin_inff();
+      unsigned above = 0, at = 0;
+      for (int j = 0; j < (int)count; ++j) {
+        const float other = few[j];
+        above += other > mine, at += other == mine;
+      }
+      const int from = __ffsll((unsigned long long)__ballot(rank >= above && rank < above + at)) - 1;
+      const float threshold = __shfl(mine, from);
+      const unsigned equal = rank + 1 - lane_value(above, from);
+      each_run([&](int k) {
+        put(r, __ballot(x[k] > threshold), __ballot(x[k] == threshold), equal, r.begin + 64 * k, place, ties);
+      });
+      return;
+    }
+    wave_sync();
+    clear();
+  }
+  Threshold t;
+  t.rank = r.want - 1;
+  auto key_of = [&](int k) { return 64 * k + lane < m ? ordered(r.score[r.begin + 64 * k + lane]) : 0; };
+#pragma unroll 1
+  for (int pass = 0;; ++pass) {
+    for (int k = 0; 64 * k < m; ++k) t.count(hist, pass, key_of(k));
+    wave_sync();
+    if (!t.next(hist, pass)) break;
+    wave_sync();
+    clear();
+  }
+  for (int k = 0; 64 * k < m; ++k) put(r, t, key_of(k), r.begin + 64 * k, place, ties);
+}
+
+// A token and head to a workgroup: for few rows, or long ones.  A wave has a
+// run of candidates, 64 at a time, the first kKept of them in registers; each
+// pass has a histogram of its own and one barrier.
+constexpr int kKept = 8;
+__global__ __launch_bounds__(kBlock) void select_block_kernel(Select a) {
+  if (blockIdx.x == gridDim.x - 1) {
+    check_requests(a.batch, a.row_offsets, a.kv.block_shift, a.status);
     return;
   }
-  const int begin = a.sink, end = blocks - a.recent, want = a.keep - a.sink - a.recent;
-  for (int k = tid; k < a.sink; k += kBlock) out[k] = k;
-  for (int k = tid; k < a.recent; k += kBlock) out[a.keep - a.recent + k] = end + k;
-  if (want == 0) return;
-
-  // each wave has a run of candidates, 64 at a time
-  const float *const score = scores_of(a, r, j, head);
-  const int each = ((end - begin + kBlock - 1) / kBlock) * 64;
-  const int from = begin + wave * each, to = min(from + each, end);
-  unsigned held[kHeld];
+  __shared__ alignas(16) Hist hists[3];
+  __shared__ unsigned sums[kWaves], marks[2][kWaves];
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
+  const int token = blockIdx.x / a.kv.kv_heads, head = blockIdx.x % a.kv.kv_heads;
+  for (int d = threadIdx.x; d < (int)(sizeof(hists) / 16); d += kBlock)
+    reinterpret_cast<uint4 *>(hists)[d] = uint4{0, 0, 0, 0};
+  // single tokens are their requests' numbers, and one request has them all: look there first
+  int i = min(token, a.batch.n - 1);
+  KvRequest q = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, i);
+  if (!q.ok || token < q.first || token - q.first >= q.count) {
+    i = __builtin_amdgcn_readfirstlane(owner_of(a.batch.token_offsets, a.batch.n, token, sums));
+    if (i >= a.batch.n) return;
+    q = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, i);
+    if (!q.ok || token < q.first || token - q.first >= q.count) return;
+  }
+  const Row r = row_of(a, q, i, token, head, threadIdx.x, kBlock);
+  if (r.want == 0) return;
+  const int each = ((r.end - r.begin + kBlock - 1) / kBlock) * 64;
+  const int from = __builtin_amdgcn_readfirstlane(min(r.begin + wave * each, r.end));
+  const int to = __builtin_amdgcn_readfirstlane(min(from + each, r.end));
+  unsigned kept[kKept];
 #pragma unroll
-  for (int k = 0; k < kHeld; ++k) {
+  for (int k = 0; k < kKept; ++k) {
     const int b = from + 64 * k + lane;
-    held[k] = b < to ? ordered(score[b]) : 0;
+    kept[k] = b < to ? ordered(r.score[b]) : 0;
   }
   auto each_key = [&](auto f) {
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k)
-      if (from + 64 * k < to) f(held[k], from + 64 * k + lane);
-    for (int b0 = from + 64 * kHeld; b0 < to; b0 += 64) {
+    for (int k = 0; k < kKept; ++k)
+      if (from + 64 * k < to) f(kept[k], from + 64 * k);
+    for (int b0 = from + 64 * kKept; b0 < to; b0 += 64) {
       const int b = b0 + lane;
-      f(b < to ? ordered(score[b]) : 0, b);
+      f(b < to ? ordered(r.score[b]) : 0, b0);
     }
   };
-  // the want-th largest: its digits as far as they are needed
-  unsigned key = 0, known = 0, rank = want - 1, equal = ~0u;
+  Threshold t;
+  t.rank = r.want - 1;
+  __syncthreads();
 #pragma unroll 1
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-    const unsigned mask = pass == 2 ? 1023u : 2047u;
-    for (int d = tid; d < kDigits; d += kBlock) hist[d] = 0;
+  for (int pass = 0;; ++pass) {
+    each_key([&](unsigned x, int) { t.count(hists[pass], pass, x); });
     __syncthreads();
-    each_key([&](unsigned k, int b) {
-      if (b < to && ((k ^ key) & known) == 0) atomicAdd(&hist[k >> shift & mask], 1u);
-    });
-    __syncthreads();
-    // 8 digits to a thread, from the largest
-    unsigned h[8], sum[1] = {0}, all[1];
-#pragma unroll
-    for (int d = 0; d < 8; ++d) sum[0] += h[d] = hist[kDigits - 1 - 8 * tid - d];
-    const unsigned mine = sum[0];
-    block_exclusive_scan<1, unsigned>(sum, all, scan);
-    unsigned at = sum[0];
-    if (rank >= at && rank < at + mine) {
-#pragma unroll
-      for (int d = 0; d < 8; ++d) {
-        if (rank >= at && rank < at + h[d]) {
-          found[0] = kDigits - 1 - 8 * tid - d;
-          found[1] = rank - at;
-          found[2] = h[d];
-        }
-        at += h[d];
-      }
-    }
-    __syncthreads();
-    key |= found[0] << shift;
-    known |= mask << shift;
-    rank = found[1];
-    if (rank + 1 == found[2]) {  // all that share these digits stay
-      equal = ~0u;
-      break;
-    }
-    equal = rank + 1;  // the first of those that share all digits
-    __syncthreads();
+    if (!t.next(hists[pass], pass)) break;
   }
-  // above the key, and equal to it as far as its digits are known
   unsigned above = 0, same = 0;
-  each_key([&](unsigned k, int b) {
-    above += __popcll(__ballot(b < to && (k & known) > key));
-    same += __popcll(__ballot(b < to && (k & known) == key));
+  each_key([&](unsigned x, int) {
+    above += __popcll(__ballot((x & t.known) > t.key));
+    same += __popcll(__ballot((x & t.known) == t.key));
   });
   if (lane == 0) marks[0][wave] = above, marks[1][wave] = same;
   __syncthreads();
   unsigned place = a.sink, ties = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) place += marks[0][w] + min(marks[1][w], equal - min(equal, ties)), ties += marks[1][w];
+    if (w < wave) {
+      place += marks[0][w] + min(marks[1][w], t.equal - min(t.equal, ties));
+      ties += marks[1][w];
+    }
   }
-  each_key([&](unsigned k, int b) {
-    const uint64_t same = __ballot(b < to && (k & known) == key);
-    const bool tie = (same >> lane & 1) && ties + rank_in_mask(same) < equal;
-    const uint64_t stay = __ballot((b < to && (k & known) > key) || tie);
-    if (stay >> lane & 1) out[place + rank_in_mask(stay)] = b;
-    place += __popcll(stay);
-    ties += __popcll(same);
-  });
+  each_key([&](unsigned x, int first) { put(r, t, x, first, place, ties); });
 }
 
 // ------------------------------------------------------------------- host
@@ -498,15 +765,24 @@ bool bounds_fit(const cascade_kv_pool_t *p, const cascade_kv_format_t *f) {
 }
 
 size_t score_bytes(const cascade_kv_format_t *f, const cascade_kv_batch_t *b) {
-  return (sizeof(float) * b->n_entries * b->max_new * f->kv_heads + 255) & ~(size_t)255;
+  return sizeof(float) * ((size_t)b->n_entries + 16 * (size_t)b->n) * b->max_new * f->kv_heads;
 }
 
-template <int kType, int kTiles>
+// Row sets of a wave where there are many: what its registers hold.
+constexpr int many_sets(int dim) { return dim == 256 ? 2 : 4; }
+
+template <int kType, bool kMany, bool kWide>
 void score(const Select &a, dim3 grid, hipStream_t stream) {
-  auto kernel = a.kv.head_dim == 64    ? score_kernel<kType, 64, kTiles>
-                : a.kv.head_dim == 128 ? score_kernel<kType, 128, kTiles>
-                                       : score_kernel<kType, 256, kTiles>;
+  auto kernel = a.kv.head_dim == 64    ? score_kernel<kType, 64, kMany ? many_sets(64) : 1, kWide>
+                : a.kv.head_dim == 128 ? score_kernel<kType, 128, kMany ? many_sets(128) : 1, kWide>
+                                       : score_kernel<kType, 256, kMany ? many_sets(256) : 1, kWide>;
   hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, stream, a);
+}
+template <int kType>
+void score(const Select &a, bool many, dim3 grid, hipStream_t stream) {
+  a.padded > 16 ? score<kType, false, true>(a, grid, stream)
+  : many        ? score<kType, true, false>(a, grid, stream)
+                : score<kType, false, false>(a, grid, stream);
 }
 
 }  // namespace
@@ -544,7 +820,7 @@ extern "C" int cascade_kv_bounds(const cascade_kv_pool_t *pool, int32_t layer, c
 
 extern "C" size_t cascade_kv_select_workspace_bytes(const cascade_kv_format_t *format,
                                                     const cascade_kv_batch_t *batch) {
-  if (!kv_format_ok(format) || !batch || batch->max_new < 0 || batch->n_entries < 0) return 0;
+  if (!kv_format_ok(format) || !batch || batch->n < 0 || batch->max_new < 0 || batch->n_entries < 0) return 0;
   return score_bytes(format, batch) + 256;
 }
 
@@ -571,6 +847,7 @@ extern "C" int cascade_kv_select(const cascade_kv_pool_t *pool, int32_t layer, c
   a.group = args->q_heads / format->kv_heads;
   a.padded = a.group > 16 ? (a.group + 15) & ~15 : 1;
   while (a.padded < a.group) a.padded *= 2;
+  a.shift = a.padded >= 16 ? 4 : __builtin_ctz((unsigned)a.padded);
   a.keep = args->keep;
   a.sink = args->sink;
   a.recent = args->recent;
@@ -578,22 +855,29 @@ extern "C" int cascade_kv_select(const cascade_kv_pool_t *pool, int32_t layer, c
   a.selected = args->selected;
   a.status = status_dev;
   const int64_t rows = (int64_t)batch->n_tokens * format->kv_heads;
-  if (rows >= INT32_MAX) return CASCADE_EINVAL;
+  if (rows >= INT32_MAX / kBlock) return CASCADE_EINVAL;
   const auto s = static_cast<hipStream_t>(stream);
-  const int per_tile = a.padded > 16 ? 1 : 16 / a.padded;
+  const int per_tile = 16 >> a.shift;
   const int tiles = (batch->max_new + per_tile - 1) / per_tile;
   const bool many = tiles >= 4 && a.padded <= 16;
-  const int sets = many ? (tiles + 3) / 4 : tiles;
+  const int each = many ? many_sets(format->head_dim) * kWaves : 1, sets = (tiles + each - 1) / each;
   if (sets > 65535) return CASCADE_EINVAL;
-  a.span = 64;
+  // Large enough that rounding the queries of several sets costs little beside
+  // the products (2001 blocks, 128 sets of 8 heads: entries of 64, 128, 256 and 512 take 46, 34, 28
+  // and 32 us), small where there is little to share: one request's next token takes 6.6 us
+  // by 32 and 8.6 by 64, 128 requests' 48 and 50.
+  const int64_t share = (int64_t)batch->n_entries * format->kv_heads * sets / 512;
+  a.span = many ? (int)std::min<int64_t>(std::max<int64_t>((share + 15) / 16 * 16, 32), 256) : 32;
   if (batch->n_entries > a.keep) {  // else every token keeps all that it sees
-    const dim3 grid((batch->n_entries + a.span - 1) / a.span, sets);
-    if (args->dtype == CASCADE_BF16) {
-      if (many) score<CASCADE_BF16, 4>(a, grid, s); else score<CASCADE_BF16, 1>(a, grid, s);
-    } else {
-      if (many) score<CASCADE_F16, 4>(a, grid, s); else score<CASCADE_F16, 1>(a, grid, s);
-    }
+    const dim3 grid(((batch->n_entries + a.span - 1) / a.span + 7) / 8 * 8, sets, many ? format->kv_heads : 1);
+    args->dtype == CASCADE_BF16 ? score<CASCADE_BF16>(a, many, grid, s) : score<CASCADE_F16>(a, many, grid, s);
   }
-  hipLaunchKernelGGL(select_kernel, dim3((unsigned)rows + 1), dim3(kBlock), 0, s, a);
+  // A wave to a row where all rows fit its registers (none has more candidates than the
+  // table has entries) and there are enough of them to fill the GPU.
+  const bool waves = batch->n_entries <= 64 * kHeld && rows >= 2048;
+  const int64_t groups = waves ? (rows + kWaves - 1) / kWaves : rows;
+  // the last one checks the batch
+  hipLaunchKernelGGL(waves ? select_wave_kernel : select_block_kernel, dim3((unsigned)groups + 1), dim3(kBlock), 0, s,
+                     a);
   return hipGetLastError() == hipSuccess ? CASCADE_OK : CASCADE_EHIP;
 }

@@ -215,6 +215,36 @@ def test_select_most_requests(dev):
     assert torch.equal(got.cpu(), sref.select(pool[0], q, b, 1, 64, 16, 5, 1, 1))
 
 
+@pytest.mark.parametrize("scores", ["", "ties", "two values", "far apart", "infinite", "one above"])
+def test_select_many_rows(dev, scores):
+    """Enough rows for a wave each; scores that fall into one part of their
+    range, or have none."""
+    rng = np.random.default_rng(10)
+    H, h, d, bt, keep = 8, 8, 64, 16, 20
+    b = ref.batch(rng, [3, 290], [2000, 5100], bt)
+    pool = make_pool(rng, 1, b, h, d, bt, spread=1)
+    sref.random_bounds(rng, pool[0], h, d, bt, scores == "ties")
+    n = ref.chunk_bytes(h, d, bt) - 32
+    scale = pool[0, 0, :, n:n + 32].contiguous().view(torch.float32)
+    if scores == "two values":  # all scores alike but for the scale
+        for s in range(2):
+            pool[0, s, :, n + 32:] = pool[0, s, :1, n + 32:]
+        scale[:] = 1.0
+        scale[torch.from_numpy(rng.permutation(b["pool"])[:15])] = 2.0
+    elif scores == "far apart":
+        scale[:] = torch.exp2(torch.from_numpy(rng.integers(-90, 90, scale.shape)).float())
+    elif scores == "infinite":
+        scale[::40] = float("inf")
+    elif scores == "one above":
+        scale[7] = 2.0 ** 40
+    pool[0, 0, :, n:n + 32] = scale.view(torch.uint8)
+    q = rows(rng, b["tokens"], H, d, torch.bfloat16)
+    want = sref.select(pool[0], q, b, h, d, bt, keep, 1, 2)
+    kv = dev.DeviceKvPool(pool.cuda(), h, d, bt, bounds=True)
+    got = run_select(dev, kv, q.cuda(), on_gpu(b), keep, 1, 2)
+    assert torch.equal(got.cpu(), want)
+
+
 @pytest.mark.parametrize("fault", ["slot", "negative slot", "length", "offsets", "row"])
 def test_select_refuses_bad_device_data(dev, fault):
     rng = np.random.default_rng(3)
