@@ -47,32 +47,37 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void selected
   const int token = blockIdx.x / kv_heads, head = blockIdx.x % kv_heads;
   const int tile = blockIdx.y % a.row_tiles, split = blockIdx.y / a.row_tiles;
 
-  unsigned ended[1] = {0};
-  for (int i = threadIdx.x; i < a.batch.n; i += kBlock) ended[0] += a.batch.token_offsets[i + 1] <= token;
-  block_sum<1, unsigned>(ended, sums);
-  const int id = __builtin_amdgcn_readfirstlane((int)ended[0]);
-  if (id >= a.batch.n) return;
-  const KvRequest req = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, id);
-  if (!req.ok || token < req.first || token - req.first >= req.count) return;
+  // the part's first blocks, while the request is looked for
+  const int32_t *const list = a.selected + ((int64_t)token * kv_heads + head) * a.places;
+  const int k0 = split * a.per, k1 = min(k0 + a.per, a.places);
+  int k = k0 + threadIdx.x;
+  int block = k < k1 ? list[k] : -1, before = k > 0 && k < k1 ? list[k - 1] : 0;
+  // single tokens are their requests' numbers, and one request has them all: look there first
+  KvRequest req = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, min(token, a.batch.n - 1));
+  if (!req.ok || token < req.first || token - req.first >= req.count) {
+    const int id = __builtin_amdgcn_readfirstlane(owner_of(a.batch.token_offsets, a.batch.n, token, sums));
+    if (id >= a.batch.n) return;
+    req = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, id);
+    if (!req.ok || token < req.first || token - req.first >= req.count) return;
+  }
   const int last = __builtin_amdgcn_readfirstlane(req.len - req.count + token - req.first);  // cached token
   const int own = last < 0 ? -1 : last >> a.kv.block_shift, bt = 1 << a.kv.block_shift;
 
   // the part's slots, up to the list's end
-  const int32_t *const list = a.selected + ((int64_t)token * kv_heads + head) * a.places;
-  const int k0 = split * a.per, k1 = min(k0 + a.per, a.places);
   int end = k1 - k0;
   bool bad = false, partial = false;
-  for (int k = k0 + threadIdx.x; k < k1; k += kBlock) {
-    const int block = list[k];
+  while (k < k1) {
     if (block < 0) {
       end = min(end, k - k0);
-    } else if (block > own || (k > 0 && (list[k - 1] < 0 || list[k - 1] >= block))) {
+    } else if (block > own || (k > 0 && (before < 0 || before >= block))) {
       bad = true;  // not seen, behind the end or not in order
       slot_list[k - k0] = 0;
     } else {
       partial |= block == own;
       slot_list[k - k0] = a.slots[req.row + block];
     }
+    k += kBlock;
+    if (k < k1) block = list[k], before = list[k - 1];
   }
   __syncthreads();
 #pragma unroll

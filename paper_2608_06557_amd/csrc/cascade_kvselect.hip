@@ -48,15 +48,6 @@ __device__ __forceinline__ int64_t scale_at(const KvView &kv, int head) {
   return ((int64_t)kv.kv_heads * kv.head_dim << kv.block_shift) + 4 * head;
 }
 
-// The request that unit `at` of a list lies in, by the ends of the requests'
-// parts: how many end at or before it.  Called by all threads.
-__device__ __forceinline__ int owner_of(const int32_t *offsets, int n, int at, unsigned *lds) {
-  unsigned ended[1] = {0};
-  for (int i = threadIdx.x; i < n; i += kBlock) ended[0] += offsets[i + 1] <= at;
-  block_sum<1, unsigned>(ended, lds);
-  return (int)ended[0];
-}
-
 // ------------------------------------------------------------------ bounds
 
 struct Bounds {

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "cascade.h"
+#include "device_util.h"
 
 namespace cascade {
 
@@ -113,6 +114,15 @@ __device__ __forceinline__ KvRequest kv_request(const cascade_kv_batch_t &b,
 
 __device__ __forceinline__ void kv_report(int32_t *status) {
   if (status) *status = CASCADE_EINVAL;
+}
+
+// The request that unit `at` of a list lies in, by the ends of the requests'
+// parts: how many end at or before it.  Called by all threads.
+__device__ __forceinline__ int owner_of(const int32_t *offsets, int n, int at, unsigned *lds) {
+  unsigned ended[1] = {0};
+  for (int i = threadIdx.x; i < n; i += kBlock) ended[0] += offsets[i + 1] <= at;
+  block_sum<1, unsigned>(ended, lds);
+  return (int)ended[0];
 }
 
 // Reports requests outside the domain, whether they have new tokens or not.
