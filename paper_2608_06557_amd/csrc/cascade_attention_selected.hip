@@ -24,9 +24,52 @@ struct Selected : Attention {
 
 constexpr int kMostListed = 4096;  // blocks of a part: their slots are in LDS
 
-template <int kType, int kDim, int kTiles, Cap kCap>
+// Up to 8 query heads fill half of a product's 16 columns.  kHalves = 2 gives the
+// other half to the second 16 tokens of a step: K_0 Q_0 + K_1 Q_1, where Q_0 has the
+// heads in the first 8 columns and zeros in the others and Q_1 in the last 8, holds
+// the scores of both in one operand's place, so the softmax has half the work.  A
+// column's weights belong to its 16 tokens; each half keeps an m, a sum and an O of its
+// own, and they are joined like those of two waves.
+template <int kType, int kDim, Cap kCap>
+struct Halves : Rowset<kType, kDim, 1, kCap> {
+  typedef Rowset<kType, kDim, 1, kCap> Base;
+  typedef typename El<kType>::v8 v8;
+  // Weights of tokens key .. key + 32, the lane's half of them.
+  __device__ __forceinline__ void weights(const Attention &a, f4 &s, v8 (&p)[1][1], int key, bool masked) {
+    const int lane = lane_id(), half = lane >> 3 & 1;
+    if (kCap != Cap::kNone) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[i] = capped<kCap>(s[i], a.cap_in, a.cap_y, a.qk, a.cap);
+    }
+    if (masked) {
+      const int seen = this->limit[0] - key - 16 * half - 4 * (lane >> 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[i] = i <= seen ? s[i] : -__builtin_inff();
+    }
+    float &m = this->m[0], &sum = this->sum[0], &used = this->used[0];
+    float top = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])) * a.scale;
+    if (__any(top > m + kSlack)) {
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float now = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - now);
+      m = now;
+      sum *= f;
+      used *= f;
+      this->scale_o(f);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale, -m));
+    sum += (s[0] + s[1]) + (s[2] + s[3]);
+    const unsigned w0 = narrow2<kType>(s[0], s[1]), w1 = narrow2<kType>(s[2], s[3]);
+    used = El<kType>::add2(w1, El<kType>::add2(w0, used));
+    p[0][0] = __builtin_bit_cast(v8, u4{half ? 0 : w0, half ? 0 : w1, half ? w0 : 0, half ? w1 : 0});
+  }
+};
+
+template <int kType, int kDim, int kTiles, Cap kCap, int kHalves = 1>
 __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void selected_kernel(Selected a) {
-  constexpr int kRows = 16 * kTiles;
+  static_assert(kHalves == 1 || kTiles == 1, "half a row set");
+  constexpr int kRows = 16 * kTiles / kHalves;
   constexpr int kPart = kDim < 128 ? kDim : 128;  // dims that one combination takes
   constexpr int kPitch = kPart + 4;
   typedef typename El<kType>::v8 v8;
@@ -40,7 +83,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void selected
   int *const slot_list = reinterpret_cast<int *>(lds);
   float *const ms = reinterpret_cast<float *>(lds + (4 * a.per + 15 & ~15)), *const os = ms + 2 * kWaves * 16;
   char *const qs = reinterpret_cast<char *>(os);
-  static_assert(kRows * kDim * 2 <= 4 * kWaves * 16 * kPitch, "q fits the place of O");
+  static_assert(16 * kTiles * kHalves * kDim * 2 <= 4 * kWaves * 16 * kPitch, "q fits the place of O");
   const int lane = lane_id(), g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(wave_id());
   const int kv_heads = a.kv.kv_heads;
@@ -94,11 +137,11 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void selected
                                                     (ended_own && listed ? bt - 1 - (last & (bt - 1)) : 0));
   if (__any(bad)) kv_report(a.status);
 
-  Rowset<kType, kDim, kTiles, kCap> r;
+  typename std::conditional<kHalves == 2, Halves<kType, kDim, kCap>, Rowset<kType, kDim, kTiles, kCap>>::type r;
   const int first_row = tile * kRows;
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
-    r.limit[t] = first_row + 16 * t + (lane & 15) < a.group ? length - 1 : -1;
+    r.limit[t] = first_row + 16 * t + (lane & (16 / kHalves - 1)) < a.group ? length - 1 : -1;
     r.log_at[t] = -1;
   }
   r.clear();
@@ -114,13 +157,13 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void selected
       slot[1] = __builtin_amdgcn_readfirstlane(slot_list[cache.entry((key >> 4) + 1)]);
     };
     look(key);
-    constexpr int kQs = kTiles * (kDim / 32), kMine = (kQs + kWaves - 1) / kWaves;
+    constexpr int kQs = kTiles * kHalves * (kDim / 32), kMine = (kQs + kWaves - 1) / kWaves;
     u4 q[kMine];
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
-      const int e = min(i * kWaves + wave, kQs - 1), d = e % (kDim / 32);
-      const int row = first_row + e / (kDim / 32) * 16 + (lane & 15);
-      const bool valid = row < a.group;
+      const int e = min(i * kWaves + wave, kQs - 1), d = e % (kDim / 32), set = e / (kDim / 32);
+      const int row = first_row + (kHalves == 2 ? lane & 7 : set * 16 + (lane & 15));
+      const bool valid = row < a.group && (kHalves == 1 || (lane >> 3 & 1) == set);
       q[i] = *reinterpret_cast<const u4 *>(a.q.data + (int64_t)token * a.q.token_stride +
                                            (int64_t)(head * a.group + (valid ? row : 0)) * a.q.head_stride + 32 * g +
                                            128 * (d >> 1) + 16 * (d & 1));
@@ -143,27 +186,44 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void selected
 #pragma unroll
           for (int i = 0; i < kDim / 64; ++i)
 #pragma unroll
-            for (int b = 0; b < 2; ++b) c.v[b][i] &= live[b];
+            for (int b = 0; b < 2; ++b) {
+              c.v[b][i] &= live[b];
+              // a score of one half adds the other's key, times 0
+              if (kHalves == 2 && key + 16 * b + (lane & 15) >= length) c.k[b][i] = u4{0, 0, 0, 0};
+            }
         }
-        f4 x[kTiles][2];
         int q_at = lane * 16;
         asm volatile("" : "+v"(q_at));  // or the loads of q move out of the loop, into registers
         const Units<kType> ku(c.ks);
-        r.template scores<2>(
-            [&](int b, int d) {
-              const u4 w = c.k[b][d >> 1];
-              return widen8<kType>(w[2 * (d & 1)], w[2 * (d & 1) + 1], ku.scale[b], ku.scale[b]);
-            },
-            [&](int t, int d) { return *reinterpret_cast<const v8 *>(qs + (t * (kDim / 32) + d) * 1024 + q_at); }, x);
-        if (__builtin_expect(ku.odd, false)) {
-#pragma unroll
-          for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-            for (int b = 0; b < 2; ++b) x[t][b] *= ku.rest[b];
-        }
-        c.fetch_k(cache, slot, key + kStride);
+        auto k_of = [&](int b, int d) {
+          const u4 w = c.k[b][d >> 1];
+          return widen8<kType>(w[2 * (d & 1)], w[2 * (d & 1) + 1], ku.scale[b], ku.scale[b]);
+        };
+        auto q_of = [&](int t, int d) {
+          return *reinterpret_cast<const v8 *>(qs + (t * (kDim / 32) + d) * 1024 + q_at);
+        };
         v8 p[kTiles][1];
-        r.template weights<2>(a, x, p, key, length, key + 32 > length, nullptr);
+        if constexpr (kHalves == 2) {
+          f4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int d = 0; d < kDim / 32; ++d)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) x = El<kType>::mfma(k_of(b, d), q_of(b, d), x);
+          if (__builtin_expect(ku.odd, false)) x *= lane & 8 ? ku.rest[1] : ku.rest[0];
+          c.fetch_k(cache, slot, key + kStride);
+          r.weights(a, x, p, key, key + 32 > length);
+        } else {
+          f4 x[kTiles][2];
+          r.template scores<2>(k_of, q_of, x);
+          if (__builtin_expect(ku.odd, false)) {
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+              for (int b = 0; b < 2; ++b) x[t][b] *= ku.rest[b];
+          }
+          c.fetch_k(cache, slot, key + kStride);
+          r.template weights<2>(a, x, p, key, length, key + 32 > length, nullptr);
+        }
         const Units<kType> vu(c.vs);
         v8 part[kTiles][1];
 #pragma unroll
@@ -209,9 +269,11 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void selected
       ms[(wave * 16 + lane) * 2 + 1] = r.sum[t];
     }
     __syncthreads();
+    // of a row: the waves', and their halves'
+    constexpr int kJoined = kWaves * kHalves, kApart = 16 / kHalves;
     float top = kLowest;
 #pragma unroll
-    for (int k = 0; k < kWaves; ++k) top = fmaxf(top, ms[(k * 16 + (lane & 15)) * 2]);
+    for (int k = 0; k < kJoined; ++k) top = fmaxf(top, ms[(k * kApart + lane % kApart) * 2]);
     const float f = __builtin_amdgcn_exp2f(r.m[t] - top) * evened(r.sum[t], r.used[t]);
 #pragma unroll
     for (int d0 = 0; d0 < kDim; d0 += kPart) {
@@ -219,19 +281,19 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void selected
       for (int d = d0 / 16; d < (d0 + kPart) / 16; ++d)
         *reinterpret_cast<f4 *>(os + (wave * 16 + (lane & 15)) * kPitch + 16 * d - d0 + 4 * g) = r.o[t][d] * f;
       __syncthreads();
-      for (int j = threadIdx.x; j < 16 * kPart / 4; j += kBlock) {
-        const int n16 = j / (kPart / 4), d = j % (kPart / 4) * 4, row = first_row + 16 * t + n16;
+      for (int j = threadIdx.x; j < kApart * kPart / 4; j += kBlock) {
+        const int n = j / (kPart / 4), d = j % (kPart / 4) * 4, row = first_row + 16 * t + n;
         if (row >= a.group) continue;
         f4 o = {0.f, 0.f, 0.f, 0.f};
         float m = kLowest, sum = 0.f;
 #pragma unroll
-        for (int k = 0; k < kWaves; ++k) {
-          o += *reinterpret_cast<const f4 *>(os + (k * 16 + n16) * kPitch + d);
-          m = fmaxf(m, ms[(k * 16 + n16) * 2]);
+        for (int k = 0; k < kJoined; ++k) {
+          o += *reinterpret_cast<const f4 *>(os + (k * kApart + n) * kPitch + d);
+          m = fmaxf(m, ms[(k * kApart + n) * 2]);
         }
 #pragma unroll
-        for (int k = 0; k < kWaves; ++k)
-          sum += ms[(k * 16 + n16) * 2 + 1] * __builtin_amdgcn_exp2f(ms[(k * 16 + n16) * 2] - m);
+        for (int k = 0; k < kJoined; ++k)
+          sum += ms[(k * kApart + n) * 2 + 1] * __builtin_amdgcn_exp2f(ms[(k * kApart + n) * 2] - m);
         const int h = head * a.group + row;
         const int64_t at = (int64_t)token * a.q_heads + h;
         if (a.splits == 1) {
@@ -323,12 +385,12 @@ struct Parts {
   }
 };
 
-template <int kType, int kDim, int kTiles>
+template <int kType, int kDim, int kTiles, int kHalves = 1>
 void start(const Selected &a, Cap cap, hipStream_t stream) {
   const size_t lds = (4 * a.per + 15 & ~15) + sizeof(float) * kWaves * 16 * (2 + (kDim < 128 ? kDim : 128) + 4);
-  auto kernel = cap == Cap::kWide     ? selected_kernel<kType, kDim, kTiles, Cap::kWide>
-                : cap == Cap::kNarrow ? selected_kernel<kType, kDim, kTiles, Cap::kNarrow>
-                                      : selected_kernel<kType, kDim, kTiles, Cap::kNone>;
+  auto kernel = cap == Cap::kWide     ? selected_kernel<kType, kDim, kTiles, Cap::kWide, kHalves>
+                : cap == Cap::kNarrow ? selected_kernel<kType, kDim, kTiles, Cap::kNarrow, kHalves>
+                                      : selected_kernel<kType, kDim, kTiles, Cap::kNone, kHalves>;
   const dim3 grid(a.batch.n_tokens * a.kv.kv_heads + 1, a.splits * a.row_tiles);  // the last one checks the batch
   hipLaunchKernelGGL(kernel, grid, dim3(kBlock), lds, stream, a);
   if (a.splits > 1) {
@@ -338,12 +400,19 @@ void start(const Selected &a, Cap cap, hipStream_t stream) {
   }
 }
 
+template <int kType, int kDim>
+void start(const Selected &a, const Parts &p, Cap cap, hipStream_t stream) {
+  a.group <= 8 ? start<kType, kDim, 1, 2>(a, cap, stream)
+  : p.tiles == 1 ? start<kType, kDim, 1>(a, cap, stream)
+                 : start<kType, kDim, 2>(a, cap, stream);
+}
+
 template <int kType>
 int start(const Selected &a, const Parts &p, Cap cap, hipStream_t s) {
   switch (a.kv.head_dim) {
-    case 64: p.tiles == 1 ? start<kType, 64, 1>(a, cap, s) : start<kType, 64, 2>(a, cap, s); break;
-    case 128: p.tiles == 1 ? start<kType, 128, 1>(a, cap, s) : start<kType, 128, 2>(a, cap, s); break;
-    default: p.tiles == 1 ? start<kType, 256, 1>(a, cap, s) : start<kType, 256, 2>(a, cap, s);
+    case 64: start<kType, 64>(a, p, cap, s); break;
+    case 128: start<kType, 128>(a, p, cap, s); break;
+    default: start<kType, 256>(a, p, cap, s);
   }
   return hipGetLastError() == hipSuccess ? CASCADE_OK : CASCADE_EHIP;
 }

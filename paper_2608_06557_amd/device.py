@@ -34,9 +34,11 @@ def to_device(a: np.ndarray, device, dtype=None):
 
 
 def stream_handle(stream=None) -> int:
+    if stream is not None:
+        return int(stream.cuda_stream)
+    # torch.cuda.current_stream().cuda_stream, which takes 2.9 us where this takes 0.3
     torch = _torch()
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return int(s.cuda_stream)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 class DeviceStep:
