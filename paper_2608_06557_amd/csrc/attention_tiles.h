@@ -1423,7 +1423,7 @@ void attend_tiles(Attention &a, char *ws, const Workspace &w, Cap cap, int small
   // shorter ones are cut where there are few (64 rows of each of 8 KV heads, 2000
   // tokens: 37 us, uncut 61), but not those of up to 16 stages (512 rows of 600
   // tokens: 29 us, cut 35)
-  a.least_keys = 16 * stage_tokens(kDim);
+  a.least_keys = kForm == Form::kShared ? 256 : 16 * stage_tokens(kDim);
   a.atomic_keys = 2048;
   a.cut_keys = stage_tokens(kDim);
   a.range_keys = 256;

@@ -85,18 +85,30 @@ __device__ __forceinline__ void bound_block(const Bounds &a, int slot, int head,
   for (int c = 0; c < kDim / 64; ++c)
 #pragma unroll
     for (int i = 0; i < 8; ++i) top[c][i] = h2{-inf, -inf}, low[c][i] = h2{inf, inf};
-  for (int t0 = 0; t0 < tokens; t0 += 16) {
-    if (t0 + lane / 4 >= tokens) continue;
+  // 4 KB of codes are on their way at once; past the end the last
+  // sub-block's are read again
+  constexpr int kAtOnce = 256 / kDim;
+  const int last = (tokens - 1) & ~15;
+  for (int t0 = 0; t0 < tokens; t0 += 16 * kAtOnce) {
+    u4 w[kAtOnce][kDim / 64];
 #pragma unroll
-    for (int c = 0; c < kDim / 64; ++c) {
-      const u4 w = *reinterpret_cast<const u4 *>(codes + t0 * kDim + 1024 * c + 16 * lane);
+    for (int j = 0; j < kAtOnce; ++j)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const h2 x = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[i], 1.f, false));
-        const h2 y = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[i], 1.f, true));
-        top[c][2 * i] = larger(top[c][2 * i], x), low[c][2 * i] = smaller(low[c][2 * i], x);
-        top[c][2 * i + 1] = larger(top[c][2 * i + 1], y), low[c][2 * i + 1] = smaller(low[c][2 * i + 1], y);
-      }
+      for (int c = 0; c < kDim / 64; ++c)
+        w[j][c] = *reinterpret_cast<const u4 *>(codes + min(t0 + 16 * j, last) * kDim + 1024 * c + 16 * lane);
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {
+      if (t0 + 16 * j > last) break;
+      if (t0 + 16 * j + lane / 4 >= tokens) continue;  // may be anything
+#pragma unroll
+      for (int c = 0; c < kDim / 64; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const h2 x = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[j][c][i], 1.f, false));
+          const h2 y = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[j][c][i], 1.f, true));
+          top[c][2 * i] = larger(top[c][2 * i], x), low[c][2 * i] = smaller(low[c][2 * i], x);
+          top[c][2 * i + 1] = larger(top[c][2 * i + 1], y), low[c][2 * i + 1] = smaller(low[c][2 * i + 1], y);
+        }
     }
   }
   // lanes 4 t + p hold dims 16 p .. of token t: at each exchange a lane keeps half
@@ -104,18 +116,21 @@ __device__ __forceinline__ void bound_block(const Bounds &a, int slot, int head,
 #pragma unroll
   for (int c = 0; c < kDim / 64; ++c) {
     int first = 0;  // of the dims pairs that are left
+    auto halve = [&](auto left) {
+      constexpr int kKeep = decltype(left)::value, kMask = 8 * kKeep;
+      const bool upper = lane & kMask;
 #pragma unroll
-    for (int keep = 4, mask = 32; keep; keep >>= 1, mask >>= 1) {
-      const bool upper = lane & mask;
-#pragma unroll
-      for (int i = 0; i < keep; ++i) {
-        const h2 mine = upper ? top[c][keep + i] : top[c][i], give = upper ? top[c][i] : top[c][keep + i];
-        top[c][i] = larger(mine, other_lane(give, mask));
-        const h2 mine_low = upper ? low[c][keep + i] : low[c][i], give_low = upper ? low[c][i] : low[c][keep + i];
-        low[c][i] = smaller(mine_low, other_lane(give_low, mask));
+      for (int i = 0; i < kKeep; ++i) {
+        const h2 mine = upper ? top[c][kKeep + i] : top[c][i], give = upper ? top[c][i] : top[c][kKeep + i];
+        top[c][i] = larger(mine, other_lane(give, kMask));
+        const h2 mine_low = upper ? low[c][kKeep + i] : low[c][i], give_low = upper ? low[c][i] : low[c][kKeep + i];
+        low[c][i] = smaller(mine_low, other_lane(give_low, kMask));
       }
-      first += upper ? keep : 0;
-    }
+      first += upper ? kKeep : 0;
+    };
+    halve(std::integral_constant<int, 4>());
+    halve(std::integral_constant<int, 2>());
+    halve(std::integral_constant<int, 1>());
     const h2 u = larger(top[c][0], other_lane(top[c][0], 4)), l = smaller(low[c][0], other_lane(low[c][0], 4));
     if (!(lane & 4)) {
       char *const to = chunk + at + 64 * c + 16 * (lane & 3) + 2 * first;
@@ -130,7 +145,7 @@ __device__ __forceinline__ void bound_block(const Bounds &a, int slot, int head,
 template <int kDim>
 __global__ __launch_bounds__(kBlock) void bounds_kernel(Bounds a) {
   if (blockIdx.x == gridDim.x - 1) {
-    check_requests(a.batch, a.row_offsets, a.kv.block_shift, a.status);
+    if (blockIdx.y == 0) check_requests(a.batch, a.row_offsets, a.kv.block_shift, a.status);
     return;
   }
   __shared__ unsigned sums[kWaves];
@@ -155,7 +170,8 @@ __global__ __launch_bounds__(kBlock) void bounds_kernel(Bounds a) {
         continue;
       }
       const int tokens = min(bt, r.len - (block << a.kv.block_shift));
-      for (int head = wave_id(); head < a.kv.kv_heads; head += kWaves) bound_block<kDim>(a, slot, head, tokens);
+      for (int head = blockIdx.y * kWaves + wave_id(); head < a.kv.kv_heads; head += gridDim.y * kWaves)
+        bound_block<kDim>(a, slot, head, tokens);
     }
   }
 }
@@ -805,7 +821,9 @@ extern "C" int cascade_kv_bounds(const cascade_kv_pool_t *pool, int32_t layer, c
   auto kernel = format->head_dim == 64    ? bounds_kernel<64>
                 : format->head_dim == 128 ? bounds_kernel<128>
                                           : bounds_kernel<256>;
-  hipLaunchKernelGGL(kernel, dim3(grid), dim3(kBlock), 0, static_cast<hipStream_t>(stream), a);
+  // few units: a head to a wave
+  const int heads = a.units <= 512 ? (format->kv_heads + kWaves - 1) / kWaves : 1;
+  hipLaunchKernelGGL(kernel, dim3(grid, heads), dim3(kBlock), 0, static_cast<hipStream_t>(stream), a);
   return hipGetLastError() == hipSuccess ? CASCADE_OK : CASCADE_EHIP;
 }
 
