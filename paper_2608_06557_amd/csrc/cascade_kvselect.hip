@@ -821,8 +821,8 @@ extern "C" int cascade_kv_bounds(const cascade_kv_pool_t *pool, int32_t layer, c
   auto kernel = format->head_dim == 64    ? bounds_kernel<64>
                 : format->head_dim == 128 ? bounds_kernel<128>
                                           : bounds_kernel<256>;
-  // few units: a head to a wave
-  const int heads = a.units <= 512 ? (format->kv_heads + kWaves - 1) / kWaves : 1;
+  // few workgroups: a head to a wave
+  const int heads = grid <= 1024 ? (format->kv_heads + kWaves - 1) / kWaves : 1;
   hipLaunchKernelGGL(kernel, dim3(grid, heads), dim3(kBlock), 0, static_cast<hipStream_t>(stream), a);
   return hipGetLastError() == hipSuccess ? CASCADE_OK : CASCADE_EHIP;
 }
