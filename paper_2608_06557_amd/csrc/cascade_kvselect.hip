@@ -867,9 +867,9 @@ extern "C" int cascade_kv_select(const cascade_kv_pool_t *pool, int32_t layer, c
   if (rows >= INT32_MAX / kBlock) return CASCADE_EINVAL;
   const auto s = static_cast<hipStream_t>(stream);
   const int per_tile = 16 >> a.shift;
-  const int tiles = (batch->max_new + per_tile - 1) / per_tile;
+  const int tiles = (batch->max_new - 1) / per_tile + 1;
   const bool many = tiles >= 4 && a.padded <= 16;
-  const int each = many ? many_sets(format->head_dim) * kWaves : 1, sets = (tiles + each - 1) / each;
+  const int each = many ? many_sets(format->head_dim) * kWaves : 1, sets = (tiles - 1) / each + 1;
   if (sets > 65535) return CASCADE_EINVAL;
   // Large enough that rounding the queries of several sets costs little beside
   // the products (2001 blocks, 128 sets of 8 heads: entries of 64, 128, 256 and 512 take 46, 34, 28
