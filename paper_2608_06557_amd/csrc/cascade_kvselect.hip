@@ -326,114 +326,240 @@ struct BlockBounds {
   }
 };
 
-// The scores of a wave's `kTiles` row sets over blocks begin .. end of request
-// i, 16 blocks a step.  kWide: a set is a part of a token's query heads, and
-// the parts are taken one after another.  With several sets the next step's
-// bounds are on their way; with one it is the other waves that keep memory busy.
-template <int kType, int kDim, int kTiles, bool kWide>
-__device__ __forceinline__ void score_blocks(const Select &a, const KvRequest &r, int i, int head, int tile0,
-                                             int begin, int end) {
-  constexpr int kSteps = kDim / 64;
-  constexpr bool kAhead = kTiles > 1;
-  const int lane = lane_id(), n16 = lane & 15, g = lane >> 4;
-  const int passes = kWide ? a.padded / 16 : 1, shift = kWide ? 4 : a.shift;
-  const int32_t *const slots = a.slots + r.row;
-  bool bad_query = false, bad_slot = false;
-  // the lane's row of set t
-  auto token_of = [&](int t) { return kWide ? tile0 : ((tile0 + t) << (4 - shift)) + (n16 >> shift); };
-  auto head_of = [&](int p) { return kWide ? 16 * p + n16 : n16 & ((1 << shift) - 1); };
-  auto look = [&](int b0) { return slots[min(b0 + n16, end - 1)]; };
+// A row set of a wave: whole queries, and where its tokens' scores go.  kWide: a
+// set is a part (`part`) of one token's query heads.
+template <int kType, int kDim, bool kWide>
+struct RowSet {
+  Operand<kDim> q;
+  float weight[4];  // of rows 4 (lane / 16) .. relative to the largest of a token's; NaN where there is no head
+  float *to;        // the score of the lane's first token and block lane % 16
+  int left;         // tokens from there on
 
+  static __device__ __forceinline__ int token_of(const Select &a, int tile) {
+    return kWide ? tile : (tile << (4 - a.shift)) + ((lane_id() & 15) >> a.shift);
+  }
+  static __device__ __forceinline__ int head_of(const Select &a, int part) {
+    const int n = lane_id() & 15;
+    return kWide ? 16 * part + n : n & ((1 << a.shift) - 1);
+  }
+  static __device__ __forceinline__ bool valid(const Select &a, const KvRequest &r, int tile, int part) {
+    return token_of(a, tile) < r.count && head_of(a, part) < a.group;
+  }
+  static __device__ __forceinline__ void load(Query<kType, kDim> &raw, const Select &a, const KvRequest &r, int head,
+                                              int tile, int part) {
+    raw.load(a, r, head, token_of(a, tile), head_of(a, part), valid(a, r, tile, part));
+  }
+  // `top_all`: the largest exponent of a token whose heads take several sets
+  __device__ __forceinline__ void make(Query<kType, kDim> &raw, const Select &a, const KvRequest &r, int i, int head,
+                                       int tile, int part, int top_all, bool &bad) {
+    const int lane = lane_id(), g = lane >> 4, shift = kWide ? 4 : a.shift;
+    const bool in = valid(a, r, tile, part);
+    const int e = raw.exponent(bad);
+    q.round(raw, e);
+    // relative to the largest of the token's heads: every product is exact, and none overflows
+    int top = in ? e : kMinExponent;
+    for (int m = 1; m < 1 << shift; m <<= 1) top = max(top, __shfl_xor(top, m));
+    if (kWide) top = top_all;
+    // the larger of NaN and a number is the number
+    const float w = in ? __uint_as_float((unsigned)(127 + max(e - top, -126)) << 23) : __builtin_nanf("");
+#pragma unroll
+    for (int k = 0; k < 4; ++k) weight[k] = __shfl(w, 4 * g + k);
+    const int first = kWide ? tile : (tile << (4 - shift)) + (4 * g >> shift);
+    to = scores_of(a, r, i, first, head) + (lane & 15);
+    left = (4 * g & ((1 << shift) - 1)) == 0 ? r.count - first : 0;
+  }
+  // The products with 16 blocks' bounds of dims 64 s ..
+  __device__ __forceinline__ i4 add(const i4 &upper, const i4 &lower, int s, i4 sum) const {
+    sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(q.plus[s], upper, sum, 0, 0, 0);
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(q.minus[s], lower, sum, 0, 0, 0);
+  }
+  // The scores of 16 blocks from `b` on by the sums of their products; `in`: the lane's is one.
+  // `next` lies between two tokens' scores.  `add`: of a token's heads these are not the first.
+  __device__ __forceinline__ void score(const Select &a, i4 sum, float scale, int b, bool in, int64_t next,
+                                        bool add) const {
+    const int shift = kWide ? 4 : a.shift;
+    float x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = (float)sum[k] * weight[k];
+    // over the heads of a token: rows 4 (lane / 16) + k of the set
+    auto put = [&](int k, float x) {
+      float *const at = to + k * next + b;
+      const float y = __builtin_fmaf(x, scale, 0.f);  // no -0
+      if (in && k < left) *at = kWide && add ? fmaxf(*at, y) : y;
+    };
+    if (shift >= 2) {
+      float y = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+      if (shift >= 3) y = fmaxf(y, __shfl_xor(y, 16));
+      if (shift >= 4) y = fmaxf(y, __shfl_xor(y, 32));
+      put(0, y);
+    } else if (shift == 1) {
+      put(0, fmaxf(x[0], x[1]));
+      put(1, fmaxf(x[2], x[3]));
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) put(k, x[k]);
+    }
+  }
+};
+
+// The scores of a wave's row set over blocks begin .. end of request i, 16 blocks
+// a step: it is the other waves that keep memory busy.  A token whose heads
+// take several sets has them one after another.
+template <int kType, int kDim, bool kWide>
+__device__ __forceinline__ void score_blocks(const Select &a, const KvRequest &r, int i, int head, int tile,
+                                             int begin, int end) {
+  const int n16 = lane_id() & 15, parts = kWide ? a.padded / 16 : 1;
+  const int32_t *const slots = a.slots + r.row;
+  const int64_t next = (int64_t)a.kv.kv_heads * score_pitch(a, r);
+  bool bad_query = false, bad_slot = false;
+  auto look = [&](int b0) { return slots[min(b0 + n16, end - 1)]; };
   int top_all = kMinExponent;
   if (kWide) {
-    for (int p = 0; p < passes; ++p) {
-      Query<kType, kDim> q;
-      const bool valid = head_of(p) < a.group && tile0 < r.count;
-      q.load(a, r, head, tile0, head_of(p), valid);
-      const int e = q.exponent(bad_query);
-      top_all = max(top_all, valid ? e : kMinExponent);
+    for (int p = 0; p < parts; ++p) {
+      Query<kType, kDim> raw;
+      RowSet<kType, kDim, kWide>::load(raw, a, r, head, tile, p);
+      const int e = raw.exponent(bad_query);
+      top_all = max(top_all, RowSet<kType, kDim, kWide>::valid(a, r, tile, p) ? e : kMinExponent);
     }
 #pragma unroll
     for (int m = 8; m; m >>= 1) top_all = max(top_all, __shfl_xor(top_all, m));
   }
-  const int64_t next = (int64_t)a.kv.kv_heads * score_pitch(a, r);  // from a token to the one after it
-  for (int p = 0; p < passes; ++p) {
+  for (int p = 0; p < parts; ++p) {
     int slot = look(begin);
-    BlockBounds<kDim> now, then;
-    Operand<kDim> q[kTiles];
-    float weight[kTiles][4];
-    float *to[kTiles];  // of the lane's first token
-    int left[kTiles];   // tokens from there on
+    BlockBounds<kDim> bounds;
+    RowSet<kType, kDim, kWide> set;
     {
-      Query<kType, kDim> raw[kTiles];
-#pragma unroll
-      for (int t = 0; t < kTiles; ++t)
-        raw[t].load(a, r, head, token_of(t), head_of(p), token_of(t) < r.count && head_of(p) < a.group);
-      now.fetch(a.kv, head, slot, bad_slot);
+      Query<kType, kDim> raw;
+      set.load(raw, a, r, head, tile, p);
+      bounds.fetch(a.kv, head, slot, bad_slot);
       slot = look(begin + 16);
-#pragma unroll
-      for (int t = 0; t < kTiles; ++t) {
-        const bool valid = token_of(t) < r.count && head_of(p) < a.group;
-        const int e = raw[t].exponent(bad_query);
-        q[t].round(raw[t], e);
-        // relative to the largest of the token's heads: every product is exact, and none overflows
-        int top = valid ? e : kMinExponent;
-        for (int m = 1; m < 1 << shift; m <<= 1) top = max(top, __shfl_xor(top, m));
-        if (kWide) top = top_all;
-        // NaN where there is no head: the larger of it and a number is the number
-        const float w = valid ? __uint_as_float((unsigned)(127 + max(e - top, -126)) << 23) : __builtin_nanf("");
-#pragma unroll
-        for (int k = 0; k < 4; ++k) weight[t][k] = __shfl(w, 4 * g + k);
-        const int first = kWide ? tile0 : ((tile0 + t) << (4 - shift)) + (4 * g >> shift);
-        to[t] = scores_of(a, r, i, first, head) + begin + n16;
-        left[t] = (4 * g & ((1 << shift) - 1)) == 0 ? r.count - first : 0;
-      }
+      set.make(raw, a, r, i, head, tile, p, top_all, bad_query);
     }
 #pragma unroll 1
     for (int b0 = begin; b0 < end; b0 += 16) {
-      if (kAhead) {
-        then.fetch(a.kv, head, slot, bad_slot);  // past the end the last block's
-        slot = look(b0 + 32);
-      }
-      const bool in = b0 + n16 < end;
+      i4 sum = {0, 0, 0, 0};
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t) {
-        i4 sum = {0, 0, 0, 0};
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-          sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[t].plus[s], now.upper[s], sum, 0, 0, 0);
-          sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[t].minus[s], now.lower[s], sum, 0, 0, 0);
-        }
-        float x[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = (float)sum[k] * weight[t][k];
-        // over the heads of a token: rows 4 g + k of the set
-        auto put = [&](int k, float x) {
-          float *const at = to[t] + k * next;
-          const float y = __builtin_fmaf(x, now.scale, 0.f);  // no -0
-          if (in && k < left[t]) *at = kWide && p ? fmaxf(*at, y) : y;
-        };
-        if (shift >= 2) {
-          float y = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-          if (shift >= 3) y = fmaxf(y, __shfl_xor(y, 16));
-          if (shift >= 4) y = fmaxf(y, __shfl_xor(y, 32));
-          put(0, y);
-        } else if (shift == 1) {
-          put(0, fmaxf(x[0], x[1]));
-          put(1, fmaxf(x[2], x[3]));
-        } else {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) put(k, x[k]);
-        }
-        to[t] += 16;
-      }
-      if (kAhead) {
-        now = then;
-      } else if (b0 + 16 < end) {
-        now.fetch(a.kv, head, slot, bad_slot);
+      for (int s = 0; s < kDim / 64; ++s) sum = set.add(bounds.upper[s], bounds.lower[s], s, sum);
+      set.score(a, sum, bounds.scale, b0, b0 + n16 < end, next, p > 0);
+      if (b0 + 16 < end) {
+        bounds.fetch(a.kv, head, slot, bad_slot);
         slot = look(b0 + 32);
       }
     }
+  }
+  if (__any(bad_query || bad_slot)) kv_report(a.status);
+}
+
+// The bounds of a stage of 32 blocks and a head in LDS, for all waves: each brings
+// those of 8 blocks, by whole lines (16 lanes that ask for 16 blocks are answered one
+// line at a time, which with several row sets a block took longer than the products).
+template <int kDim>
+struct BoundStage {
+  static constexpr int kBlocks = 32, kMine = kBlocks / kWaves, kChunks = kDim / 16, kLoads = kDim / 64;
+  static constexpr int kSlots = kDim == 256 ? 2 : 1;  // a lane's loads of a side are of as many blocks
+  static constexpr int kBytes = 2 * kBlocks * kDim + 4 * kBlocks;
+  u4 raw[kLoads];
+  float scale;
+  int slot[kSlots], scale_slot;
+  // of load k: the side, the block among the wave's, the chunk of 16 bytes
+  static __device__ __forceinline__ int side_of(int k) { return (64 * k + lane_id()) / (kMine * kChunks); }
+  static __device__ __forceinline__ int block_of(int k) { return (64 * k + lane_id()) / kChunks % kMine; }
+  static __device__ __forceinline__ int chunk_of() { return lane_id() % kChunks; }
+  // 16 lanes that read a chunk of 16 blocks meet few banks twice
+  static __device__ __forceinline__ int place(int side, int block, int chunk) {
+    const int turn = kDim == 64 ? block >> 1 & 3 : block & (kChunks - 1);
+    return side * kBlocks * kDim + (block * kChunks + (chunk ^ turn)) * 16;
+  }
+  __device__ __forceinline__ void look(const int32_t *slots, int b0, int end) {
+    const int first = b0 + kMine * wave_id();
+#pragma unroll
+    for (int k = 0; k < kSlots; ++k) slot[k] = slots[min(first + block_of(k), end - 1)];
+    scale_slot = slots[min(first + lane_id() % kMine, end - 1)];
+  }
+  __device__ __forceinline__ void fetch(const KvView &kv, int head, bool &bad) {
+    const char *const from = kv.base + bounds_at(kv, head) + 16 * chunk_of();
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+      const int s = slot[k % kSlots];
+      const bool fine = (unsigned)s < (unsigned)kv.num_slots;
+      bad |= !fine;
+      raw[k] = *reinterpret_cast<const u4 *>(from + (fine ? s : 0) * kv.slot_stride + side_of(k) * kv.kv_stride);
+    }
+    const int s = (unsigned)scale_slot < (unsigned)kv.num_slots ? scale_slot : 0;
+    scale = *reinterpret_cast<const float *>(kv.base + scale_at(kv, head) + s * kv.slot_stride);
+  }
+  __device__ __forceinline__ void put(char *lds) const {
+    const int first = kMine * wave_id();
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k)
+      *reinterpret_cast<u4 *>(lds + place(side_of(k), first + block_of(k), chunk_of())) = raw[k];
+    if (lane_id() < kMine) reinterpret_cast<float *>(lds + 2 * kBlocks * kDim)[first + lane_id()] = scale;
+  }
+  static __device__ __forceinline__ void get(const char *lds, int half, i4 (&upper)[kLoads], i4 (&lower)[kLoads],
+                                             float &scale) {
+    const int block = 16 * half + (lane_id() & 15), g = lane_id() >> 4;
+#pragma unroll
+    for (int s = 0; s < kLoads; ++s) {
+      upper[s] = *reinterpret_cast<const i4 *>(lds + place(0, block, 4 * s + g));
+      lower[s] = *reinterpret_cast<const i4 *>(lds + place(1, block, 4 * s + g));
+    }
+    scale = reinterpret_cast<const float *>(lds + 2 * kBlocks * kDim)[block];
+  }
+};
+
+// The scores of `kTiles` row sets a wave, neighbouring ones of a head, over blocks
+// begin .. end.  Called by all waves; `lds` holds two stages.
+template <int kType, int kDim, int kTiles>
+__device__ __forceinline__ void score_sets(const Select &a, const KvRequest &r, int i, int head, int tile0, int begin,
+                                           int end, char *lds) {
+  typedef BoundStage<kDim> Stage;
+  const int32_t *const slots = a.slots + r.row;
+  const int64_t next = (int64_t)a.kv.kv_heads * score_pitch(a, r);
+  bool bad_query = false, bad_slot = false;
+  Stage stage;
+  RowSet<kType, kDim, false> set[kTiles];
+  stage.look(slots, begin, end);
+  {
+    Query<kType, kDim> raw[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) set[t].load(raw[t], a, r, head, tile0 + t, 0);
+    stage.fetch(a.kv, head, bad_slot);
+    stage.look(slots, begin + Stage::kBlocks, end);
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) set[t].make(raw[t], a, r, i, head, tile0 + t, 0, 0, bad_query);
+  }
+  char *from = lds, *to = lds + Stage::kBytes;
+  __syncthreads();  // what was read of it before
+  stage.put(from);
+  stage.fetch(a.kv, head, bad_slot);  // past the end the last block's
+  stage.look(slots, begin + 2 * Stage::kBlocks, end);
+  __syncthreads();
+#pragma unroll 1
+  for (int b0 = begin; b0 < end; b0 += Stage::kBlocks) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int b = b0 + 16 * half;
+      i4 upper[kDim / 64], lower[kDim / 64];
+      float scale;
+      Stage::get(from, half, upper, lower, scale);
+      i4 sum[kTiles];  // a product waits for the one before it: those of other sets go between
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) sum[t] = i4{0, 0, 0, 0};
+#pragma unroll
+      for (int s = 0; s < kDim / 64; ++s)
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) sum[t] = set[t].add(upper[s], lower[s], s, sum[t]);
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+        set[t].score(a, sum[t], scale, b, b + (lane_id() & 15) < end, next, false);
+    }
+    stage.put(to);
+    stage.fetch(a.kv, head, bad_slot);
+    stage.look(slots, b0 + 3 * Stage::kBlocks, end);
+    __syncthreads();
+    char *const was = from;
+    from = to;
+    to = was;
   }
   if (__any(bad_query || bad_slot)) kv_report(a.status);
 }
@@ -447,37 +573,48 @@ struct Candidates {
   }
 };
 
-// A workgroup has `span` table entries.  One row set to a wave: its waves take
-// heads, or parts of the entries where there are few heads, so that what lies side by
-// side is read at one time.  Several: neighbouring ones of a head, which read the same
-// bounds.
-template <int kType, int kDim, int kTiles, bool kWide>
-__global__ __launch_bounds__(kBlock, kTiles > 1 || kDim == 256 ? 2 : 5) void score_kernel(Select a) {
-  __shared__ unsigned sums[kWaves];
+// Entries span .. of the table, the requests in them one after another.
+template <typename F>
+__device__ __forceinline__ void each_request(const Select &a, int first_token, unsigned *lds, F f) {
   // neighbouring spans on one XCD (workgroups go to the 8 in turn), where a request's queries are then in L2
   const int span = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
   if ((int64_t)span * a.span >= a.batch.n_entries) return;
   const int e0 = span * a.span, e1 = min(e0 + a.span, a.batch.n_entries);
-  const int per_tile = 16 >> a.shift, wave = __builtin_amdgcn_readfirstlane(wave_id());
-  const int tile0 = kTiles > 1 ? (blockIdx.y * kWaves + wave) * kTiles : blockIdx.y;
-  for (int i = __builtin_amdgcn_readfirstlane(owner_of(a.row_offsets, a.batch.n, e0, sums));
+  for (int i = __builtin_amdgcn_readfirstlane(owner_of(a.row_offsets, a.batch.n, e0, lds));
        i < a.batch.n && uniform_load(a.row_offsets + i) < e1; ++i) {
     const KvRequest r = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, i);
-    if (!r.ok || tile0 * per_tile >= r.count) continue;
+    if (!r.ok || first_token >= r.count) continue;
     const Candidates c(a, blocks_of(r, a.kv.block_shift));
     const int begin = max(c.begin, e0 - r.row), end = min(c.end, e1 - r.row);
-    if (begin >= end) continue;
-    if (kTiles > 1) {
-      score_blocks<kType, kDim, kTiles, kWide>(a, r, i, blockIdx.z, tile0, begin, end);
-    } else {
-      const int heads = a.kv.kv_heads, parts = heads >= kWaves ? 1 : kWaves / heads;
-      const int each = ((end - begin + 16 * parts - 1) / (16 * parts)) * 16;
-      for (int u = wave; u < heads * parts; u += kWaves) {
-        const int from = begin + u / heads * each, to = min(from + each, end);
-        if (from < to) score_blocks<kType, kDim, kTiles, kWide>(a, r, i, u % heads, tile0, from, to);
-      }
-    }
+    if (begin < end) f(r, i, begin, end);
   }
+}
+
+// A row set to a wave, which takes heads, or parts of the entries where there
+// are few heads, so that what lies side by side is read at one time.
+template <int kType, int kDim, bool kWide>
+__global__ __launch_bounds__(kBlock, kDim == 256 ? 2 : 5) void score_kernel(Select a) {
+  __shared__ unsigned sums[kWaves];
+  const int wave = __builtin_amdgcn_readfirstlane(wave_id()), tile = blockIdx.y;
+  each_request(a, tile * (16 >> a.shift), sums, [&](const KvRequest &r, int i, int begin, int end) {
+    const int heads = a.kv.kv_heads, parts = heads >= kWaves ? 1 : kWaves / heads;
+    const int each = ((end - begin + 16 * parts - 1) / (16 * parts)) * 16;
+    for (int u = wave; u < heads * parts; u += kWaves) {
+      const int from = begin + u / heads * each, to = min(from + each, end);
+      if (from < to) score_blocks<kType, kDim, kWide>(a, r, i, u % heads, tile, from, to);
+    }
+  });
+}
+
+// Many row sets: `kTiles` to a wave, of one head.
+template <int kType, int kDim, int kTiles>
+__global__ __launch_bounds__(kBlock, 2) void score_sets_kernel(Select a) {
+  __shared__ unsigned sums[kWaves];
+  __shared__ alignas(16) char stages[2 * BoundStage<kDim>::kBytes];
+  const int wave = __builtin_amdgcn_readfirstlane(wave_id()), tile0 = blockIdx.y * kWaves * kTiles;
+  each_request(a, tile0 * (16 >> a.shift), sums, [&](const KvRequest &r, int i, int begin, int end) {
+    score_sets<kType, kDim, kTiles>(a, r, i, blockIdx.z, tile0 + wave * kTiles, begin, end, stages);
+  });
 }
 
 // ------------------------------------------------------------------ select
@@ -778,18 +915,20 @@ size_t score_bytes(const cascade_kv_format_t *f, const cascade_kv_batch_t *b) {
 // Row sets of a wave where there are many: what its registers hold.
 constexpr int many_sets(int dim) { return dim == 256 ? 2 : 4; }
 
-template <int kType, bool kMany, bool kWide>
-void score(const Select &a, dim3 grid, hipStream_t stream) {
-  auto kernel = a.kv.head_dim == 64    ? score_kernel<kType, 64, kMany ? many_sets(64) : 1, kWide>
-                : a.kv.head_dim == 128 ? score_kernel<kType, 128, kMany ? many_sets(128) : 1, kWide>
-                                       : score_kernel<kType, 256, kMany ? many_sets(256) : 1, kWide>;
+template <int kType, int kDim>
+void score(const Select &a, bool many, dim3 grid, hipStream_t stream) {
+  auto kernel = a.padded > 16 ? score_kernel<kType, kDim, true>
+                : many        ? score_sets_kernel<kType, kDim, many_sets(kDim)>
+                              : score_kernel<kType, kDim, false>;
   hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, stream, a);
 }
 template <int kType>
 void score(const Select &a, bool many, dim3 grid, hipStream_t stream) {
-  a.padded > 16 ? score<kType, false, true>(a, grid, stream)
-  : many        ? score<kType, true, false>(a, grid, stream)
-                : score<kType, false, false>(a, grid, stream);
+  switch (a.kv.head_dim) {
+    case 64: score<kType, 64>(a, many, grid, stream); break;
+    case 128: score<kType, 128>(a, many, grid, stream); break;
+    default: score<kType, 256>(a, many, grid, stream);
+  }
 }
 
 }  // namespace
