@@ -25,7 +25,9 @@ struct SharedJoin {
 };
 
 // Joins what is known of each row, a row to a wave: the parts of its request's
-// segment, or its state, and the same of its group's.
+// segment, or its state, and the same of its group's.  A chain of dependent loads,
+// then the parts: 128 tokens of 64 heads of 128 dims 9 us behind 32 groups of 4 tokens, 11 where
+// the row tiles of one group left 8 parts of each row, 33 MB.
 template <int kType, int kDim>
 __global__ __launch_bounds__(kBlock) void join_shared_kernel(Attention a, SharedJoin j) {
   constexpr int kLanes = kDim / 4, kHalves = 64 / kLanes;

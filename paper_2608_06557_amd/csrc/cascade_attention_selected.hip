@@ -10,6 +10,12 @@
 // A workgroup has one token, KV head, row set and part of the list; the parts
 // of one token are joined by a second launch.  It looks its slots up once,
 // into LDS, and the loads of codes run a step ahead.
+//
+// 128 single tokens with lists of 128 blocks of 16 tokens, 64/8 heads of 128 dims, are bound by
+// HBM: 104-106 us, 601 MB fetched (543 without what lines bring along), 5.7 TB/s.  512 tokens of
+// one request, 64 blocks each, find codes in L2: 60 us for 1.07 GB, of which 5.5 us
+// for each of its rounds of workgroups go to slots, first loads and the join of waves.
+// One token: 6.7 us, join 4.3.
 #include "attention_tiles.h"
 
 namespace cascade {
