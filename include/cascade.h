@@ -724,7 +724,9 @@ int cascade_kv_bounds(const cascade_kv_pool_t *pool, int32_t layer,
    n_r = q_r / 2^e_r rounded to nearest even, e the largest e_r: up to the roundings
    of u, l and n a bound on every q . k of the block (for a positive scale of attention).  The sums are
    whole numbers, the rest powers of two in 32 bits: a selection is the same on any
-   machine.  A NaN or infinite query element counts as 0 and sets *status_dev.
+   machine.  A NaN or infinite query element counts as 0 and, in a request with
+   more than `keep` blocks, sets *status_dev.  A NaN score, of a K scale that is not
+   finite, is the largest.
    selected: device int32[n_tokens][kv_heads][keep], block indices within the request, ascending,
    then -1; tokens of no request are left as they are.
    workspace: cascade_kv_select_workspace_bytes(...) bytes, 256-byte aligned, of

@@ -223,3 +223,28 @@ def test_selected_peaked_flat_and_capped_scores(dev, H, scale, cap):
     if scale:  # of none of the query nothing is left
         assert torch.isnan(got[0][1, 3]).all()
     assert torch.equal(got[0].cpu()[~bad], base[0].cpu()[~bad])
+
+
+@pytest.mark.parametrize("heads", [8, 40], ids=["", "wide"])
+@pytest.mark.parametrize("counts", [[3, 2], [3, 290]], ids=["few rows", "many rows"])
+def test_scores_that_are_no_numbers_are_the_largest(dev, counts, heads):
+    """The first of the blocks whose K scale is NaN, beside those that are
+    listed anyway."""
+    rng = np.random.default_rng(27)
+    h, d, bt, keep = 8, 64, 16, 20
+    b = ref.batch(rng, counts, [2000, 5100], bt)
+    pool = make_pool(rng, 1, b, h, d, bt)
+    sref.random_bounds(rng, pool[0], h, d, bt)
+    n = ref.chunk_bytes(h, d, bt) - 32
+    scale = pool[0, 0, :, n:n + 32].contiguous().view(torch.float32)
+    for i in range(2):
+        scale[b["slots"][int(b["rows"][i]) + 10:int(b["rows"][i]) + 50].long()] = float("nan")
+    pool[0, 0, :, n:n + 32] = scale.view(torch.uint8)
+    q = rows(rng, b["tokens"], heads if heads == 8 else 8 * heads, d, torch.bfloat16)
+    kv = dev.DeviceKvPool(pool.cuda(), h, d, bt, bounds=True)
+    got = run_select(dev, kv, q.cuda(), on_gpu(b), keep, 1, 2).cpu()
+    for i in range(2):
+        for j in range(counts[i]):
+            last = int(b["len"][i]) - counts[i] + j
+            want = [0] + list(range(10, 27)) + [last // bt - 1, last // bt]
+            assert (got[int(b["off"][i]) + j] == torch.tensor(want)).all()
