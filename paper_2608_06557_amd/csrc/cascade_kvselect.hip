@@ -200,6 +200,7 @@ struct Select {
   int shift;   // log2 of a token's rows in a set
   int keep, sink, recent;
   int span;    // table entries of a workgroup
+  int spans, sets;  // how many, and sets of rows of a workgroup
   float *scores;  // request by request [token][KV head][block], in whole lines of 16
   int32_t *selected;
   int32_t *status;
@@ -333,6 +334,16 @@ struct BlockBounds {
   }
 };
 
+// The larger of a lane's and that of the lane 16 or 32 further, for both.
+__device__ __forceinline__ float larger16(float x) {
+  const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+__device__ __forceinline__ float larger32(float x) {
+  const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+
 // A row set of a wave: whole queries, and where its tokens' scores go.  kWide: a
 // set is a part (`part`) of one token's query heads.
 template <int kType, int kDim, bool kWide>
@@ -380,31 +391,55 @@ struct RowSet {
     sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(q.plus[s], upper, sum, 0, 0, 0);
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(q.minus[s], lower, sum, 0, 0, 0);
   }
-  // The scores of 16 blocks from `b` on by the sums of their products; `in`: the lane's is one.
-  // `next` lies between two tokens' scores.  `add`: of a token's heads these are not the first.
-  __device__ __forceinline__ void score(const Select &a, i4 sum, float scale, int b, bool in, int64_t next,
-                                        bool add) const {
+  // The scores of 16 blocks from `b` on by the sums of their products with `kTiles` sets; `in`:
+  // the lane's is one.  `next` lies between two tokens' scores.  `add`: of a token's heads these
+  // are not the first.  (Step by step for all sets, each of which has a step's latency to itself
+  // otherwise.)
+  template <int kTiles>
+  static __device__ __forceinline__ void score(const Select &a, const RowSet (&set)[kTiles], const i4 (&sum)[kTiles],
+                                               float scale, int b, bool in, int64_t next, bool add) {
     const int shift = kWide ? 4 : a.shift;
-    float x[4];
+    float x[kTiles][4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) x[k] = (float)sum[k] * weight[k];
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[t][k] = (float)sum[t][k] * set[t].weight[k];
     // over the heads of a token: rows 4 (lane / 16) + k of the set
-    auto put = [&](int k, float x) {
-      float *const at = to + k * next + b;
-      const float y = __builtin_fmaf(x, scale, 0.f);  // no -0
-      if (in && k < left) *at = kWide && add ? fmaxf(*at, y) : y;
+    auto put = [&](int k, const float (&x)[kTiles]) {
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) {
+        float *const at = set[t].to + k * next + b;
+        const float y = __builtin_fmaf(x[t], scale, 0.f);  // no -0
+        if (in && k < set[t].left) *at = kWide && add ? fmaxf(*at, y) : y;
+      }
     };
+    float y[kTiles];
     if (shift >= 2) {
-      float y = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-      if (shift >= 3) y = fmaxf(y, __shfl_xor(y, 16));
-      if (shift >= 4) y = fmaxf(y, __shfl_xor(y, 32));
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) y[t] = fmaxf(fmaxf(x[t][0], x[t][1]), fmaxf(x[t][2], x[t][3]));
+      if (shift >= 3) {
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) y[t] = larger16(y[t]);
+      }
+      if (shift >= 4) {
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) y[t] = larger32(y[t]);
+      }
       put(0, y);
     } else if (shift == 1) {
-      put(0, fmaxf(x[0], x[1]));
-      put(1, fmaxf(x[2], x[3]));
+#pragma unroll
+      for (int k = 0; k < 4; k += 2) {
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) y[t] = fmaxf(x[t][k], x[t][k + 1]);
+        put(k / 2, y);
+      }
     } else {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) put(k, x[k]);
+      for (int k = 0; k < 4; ++k) {
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) y[t] = x[t][k];
+        put(k, y);
+      }
     }
   }
 };
@@ -434,7 +469,7 @@ __device__ __forceinline__ void score_blocks(const Select &a, const KvRequest &r
   for (int p = 0; p < parts; ++p) {
     int slot = look(begin);
     BlockBounds<kDim> bounds;
-    RowSet<kType, kDim, kWide> set;
+    RowSet<kType, kDim, kWide> sets[1], &set = sets[0];
     {
       Query<kType, kDim> raw;
       set.load(raw, a, r, head, tile, p);
@@ -444,10 +479,10 @@ __device__ __forceinline__ void score_blocks(const Select &a, const KvRequest &r
     }
 #pragma unroll 1
     for (int b0 = begin; b0 < end; b0 += 16) {
-      i4 sum = {0, 0, 0, 0};
+      i4 sum[1] = {i4{0, 0, 0, 0}};
 #pragma unroll
-      for (int s = 0; s < kDim / 64; ++s) sum = set.add(bounds.upper[s], bounds.lower[s], s, sum);
-      set.score(a, sum, bounds.scale, b0, b0 + n16 < end, next, p > 0);
+      for (int s = 0; s < kDim / 64; ++s) sum[0] = set.add(bounds.upper[s], bounds.lower[s], s, sum[0]);
+      set.score(a, sets, sum, bounds.scale, b0, b0 + n16 < end, next, p > 0);
       if (b0 + 16 < end) {
         bounds.fetch(a.kv, head, slot, bad_slot);
         slot = look(b0 + 32);
@@ -556,9 +591,7 @@ __device__ __forceinline__ void score_sets(const Select &a, const KvRequest &r, 
       for (int s = 0; s < kDim / 64; ++s)
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) sum[t] = set[t].add(upper[s], lower[s], s, sum[t]);
-#pragma unroll
-      for (int t = 0; t < kTiles; ++t)
-        set[t].score(a, sum[t], scale, b, b + (lane_id() & 15) < end, next, false);
+      set[0].score(a, set, sum, scale, b, b + (lane_id() & 15) < end, next, false);
     }
     stage.put(to);
     stage.fetch(a.kv, head, bad_slot);
@@ -580,11 +613,12 @@ struct Candidates {
   }
 };
 
+// Neighbouring pieces of work on one XCD (workgroups go to the 8 in turn; blockIdx.x is one of a multiple of 8).
+__device__ __forceinline__ int piece() { return (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3); }
+
 // Entries span .. of the table, the requests in them one after another.
 template <typename F>
-__device__ __forceinline__ void each_request(const Select &a, int first_token, unsigned *lds, F f) {
-  // neighbouring spans on one XCD (workgroups go to the 8 in turn), where a request's queries are then in L2
-  const int span = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+__device__ __forceinline__ void each_request(const Select &a, int span, int first_token, unsigned *lds, F f) {
   if ((int64_t)span * a.span >= a.batch.n_entries) return;
   const int e0 = span * a.span, e1 = min(e0 + a.span, a.batch.n_entries);
   for (int i = __builtin_amdgcn_readfirstlane(owner_of(a.row_offsets, a.batch.n, e0, lds));
@@ -603,7 +637,7 @@ template <int kType, int kDim, bool kWide>
 __global__ __launch_bounds__(kBlock, kDim == 256 ? 2 : 5) void score_kernel(Select a) {
   __shared__ unsigned sums[kWaves];
   const int wave = __builtin_amdgcn_readfirstlane(wave_id()), tile = blockIdx.y;
-  each_request(a, tile * (16 >> a.shift), sums, [&](const KvRequest &r, int i, int begin, int end) {
+  each_request(a, piece(), tile * (16 >> a.shift), sums, [&](const KvRequest &r, int i, int begin, int end) {
     const int heads = a.kv.kv_heads, parts = heads >= kWaves ? 1 : kWaves / heads;
     const int each = ((end - begin + 16 * parts - 1) / (16 * parts)) * 16;
     for (int u = wave; u < heads * parts; u += kWaves) {
@@ -613,14 +647,17 @@ __global__ __launch_bounds__(kBlock, kDim == 256 ? 2 : 5) void score_kernel(Sele
   });
 }
 
-// Many row sets: `kTiles` to a wave, of one head.
+// Many row sets: `kTiles` to a wave, of one head.  An XCD has one head, or few, whose queries and
+// bounds are then in its L2.
 template <int kType, int kDim, int kTiles>
 __global__ __launch_bounds__(kBlock, 2) void score_sets_kernel(Select a) {
   __shared__ unsigned sums[kWaves];
   __shared__ alignas(16) char stages[2 * BoundStage<kDim>::kBytes];
-  const int wave = __builtin_amdgcn_readfirstlane(wave_id()), tile0 = blockIdx.y * kWaves * kTiles;
-  each_request(a, tile0 * (16 >> a.shift), sums, [&](const KvRequest &r, int i, int begin, int end) {
-    score_sets<kType, kDim, kTiles>(a, r, i, blockIdx.z, tile0 + wave * kTiles, begin, end, stages);
+  const int wave = __builtin_amdgcn_readfirstlane(wave_id());
+  const int at = piece(), head = at / (a.spans * a.sets), tile0 = at / a.spans % a.sets * kWaves * kTiles;
+  if (head >= a.kv.kv_heads) return;
+  each_request(a, at % a.spans, tile0 * (16 >> a.shift), sums, [&](const KvRequest &r, int i, int begin, int end) {
+    score_sets<kType, kDim, kTiles>(a, r, i, head, tile0 + wave * kTiles, begin, end, stages);
   });
 }
 
@@ -734,6 +771,25 @@ __device__ __forceinline__ void put(const Row &r, const Threshold &t, unsigned x
   put(r, __ballot((x & t.known) > t.key), __ballot((x & t.known) == t.key), t.equal, first, place, ties);
 }
 
+// The score with `rank` before it, largest first, of up to 64 finite ones in LDS, and how many of those
+// equal to it stay.
+struct Few {
+  float threshold;
+  unsigned equal;
+  __device__ __forceinline__ Few(const float *few, unsigned count, unsigned rank) {
+    const int lane = lane_id();
+    const float mine = lane < (int)count ? few[lane] : -__builtin_inff();
+    unsigned above = 0, at = 0;
+    for (int j = 0; j < (int)count; ++j) {
+      const float other = few[j];
+      above += other > mine, at += other == mine;
+    }
+    const int from = __ffsll((unsigned long long)__ballot(rank >= above && rank < above + at)) - 1;
+    threshold = __shfl(mine, from);
+    equal = rank + 1 - lane_value(above, from);
+  }
+};
+
 // A token and head to a wave, its candidates in registers, no barriers: for
 // many rows.
 constexpr int kHeld = 32, kRun = 16;  // registers, and those between two looks at the row's end
@@ -791,8 +847,12 @@ __global__ __launch_bounds__(kBlock) void select_wave_kernel(Select a) {
   const float per = (kDigits - 1) / (most - least);
   unsigned place = a.sink, ties = 0;
   if (!__any(odd) && __builtin_isfinite(per)) {
-    auto digit_of = [&](float x) { return min((unsigned)((x - least) * per), kDigits - 1u); };
-    each_run([&](int k) { atomicAdd(&hist[x[k] == x[k] ? digit_of(x[k]) : kDigits + lane], 1u); });
+    unsigned place_of[kHeld];  // a place behind the digits is no candidate's
+    each_run([&](int k) {
+      const unsigned digit = min((unsigned)((x[k] - least) * per), kDigits - 1u);
+      place_of[k] = 64 * k + lane < m ? digit : kDigits + lane;
+      atomicAdd(&hist[place_of[k]], 1u);
+    });
     wave_sync();
     unsigned rank = r.want - 1, count;
     const unsigned digit = find_digit(hist, rank, count);
@@ -801,23 +861,16 @@ __global__ __launch_bounds__(kBlock) void select_wave_kernel(Select a) {
       float *const few = reinterpret_cast<float *>(hist);
       unsigned n = 0;
       each_run([&](int k) {
-        const uint64_t in = __ballot(x[k] == x[k] && digit_of(x[k]) == digit);
+        const uint64_t in = __ballot(place_of[k] == digit);
         if (!in) return;
         if (in >> lane & 1) few[n + rank_in_mask(in)] = x[k];
         n += __popcll(in);
       });
       wave_sync();
-      const float mine = lane < (int)count ? few[lane] : -__builtin_inff();
-      unsigned above = 0, at = 0;
-      for (int j = 0; j < (int)count; ++j) {
-        const float other = few[j];
-        above += other > mine, at += other == mine;
-      }
-      const int from = __ffsll((unsigned long long)__ballot(rank >= above && rank < above + at)) - 1;
-      const float threshold = __shfl(mine, from);
-      const unsigned equal = rank + 1 - lane_value(above, from);
+      const Few found(few, count, rank);
       each_run([&](int k) {
-        put(r, __ballot(x[k] > threshold), __ballot(x[k] == threshold), equal, r.begin + 64 * k, place, ties);
+        put(r, __ballot(x[k] > found.threshold), __ballot(x[k] == found.threshold), found.equal, r.begin + 64 * k,
+            place, ties);
       });
       return;
     }
@@ -839,20 +892,24 @@ __global__ __launch_bounds__(kBlock) void select_wave_kernel(Select a) {
 }
 
 // A token and head to a workgroup: for few rows, or long ones.  A wave has a
-// run of candidates, 64 at a time, the first kKept of them in registers; each
-// pass has a histogram of its own and one barrier.
-constexpr int kKept = 8;
+// run of candidates, 64 at a time, the first kKept of them in registers.
+constexpr int kKept = 16;
 __global__ __launch_bounds__(kBlock) void select_block_kernel(Select a) {
   if (blockIdx.x == gridDim.x - 1) {
     check_requests(a.batch, a.row_offsets, a.kv.block_shift, a.status);
     return;
   }
   __shared__ alignas(16) Hist hists[3];
-  __shared__ unsigned sums[kWaves], marks[2][kWaves];
+  __shared__ unsigned sums[kWaves], marks[2][kWaves], listed;
+  __shared__ float widths[2][kWaves];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
   const int token = blockIdx.x / a.kv.kv_heads, head = blockIdx.x % a.kv.kv_heads;
-  for (int d = threadIdx.x; d < (int)(sizeof(hists) / 16); d += kBlock)
-    reinterpret_cast<uint4 *>(hists)[d] = uint4{0, 0, 0, 0};
+  auto clear = [&](Hist &h) {
+    for (int d = threadIdx.x; d < (int)(sizeof(Hist) / 16); d += kBlock)
+      reinterpret_cast<uint4 *>(h)[d] = uint4{0, 0, 0, 0};
+  };
+  clear(hists[0]);
+  if (threadIdx.x == 0) listed = 0;
   // single tokens are their requests' numbers, and one request has them all: look there first
   int i = min(token, a.batch.n - 1);
   KvRequest q = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, i);
@@ -867,45 +924,101 @@ __global__ __launch_bounds__(kBlock) void select_block_kernel(Select a) {
   const int each = ((r.end - r.begin + kBlock - 1) / kBlock) * 64;
   const int from = __builtin_amdgcn_readfirstlane(min(r.begin + wave * each, r.end));
   const int to = __builtin_amdgcn_readfirstlane(min(from + each, r.end));
-  unsigned kept[kKept];
+  float kept[kKept];
 #pragma unroll
-  for (int k = 0; k < kKept; ++k) {
-    const int b = from + 64 * k + lane;
-    kept[k] = b < to ? ordered(r.score[b]) : 0;
-  }
-  auto each_key = [&](auto f) {
+  for (int k = 0; k < kKept; ++k) kept[k] = from + 64 * k < to ? r.score[min(from + 64 * k + lane, to - 1)] : 0.f;
+  // f(score, whether it is one, block of lane 0)
+  auto each_score = [&](auto f) {
 #pragma unroll
     for (int k = 0; k < kKept; ++k)
-      if (from + 64 * k < to) f(kept[k], from + 64 * k);
-    for (int b0 = from + 64 * kKept; b0 < to; b0 += 64) {
-      const int b = b0 + lane;
-      f(b < to ? ordered(r.score[b]) : 0, b0);
+      if (from + 64 * k < to) f(kept[k], from + 64 * k + lane < to, from + 64 * k);
+    for (int b0 = from + 64 * kKept; b0 < to; b0 += 64) f(r.score[min(b0 + lane, to - 1)], b0 + lane < to, b0);
+  };
+  // where the waves before this one put theirs, by what each has above the threshold and at it
+  unsigned place = a.sink, ties = 0;
+  auto begin_at = [&](unsigned above, unsigned at, unsigned equal) {
+    if (lane == 0) marks[0][wave] = above, marks[1][wave] = at;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wave) {
+        place += marks[0][w] + min(marks[1][w], equal - min(equal, ties));
+        ties += marks[1][w];
+      }
     }
+  };
+
+  // equal parts of the scores' range as digits, as in select_wave_kernel
+  float least = __builtin_inff(), most = -__builtin_inff();
+  bool odd = false;
+  each_score([&](float x, bool, int) {
+    odd |= !__builtin_isfinite(x);
+    least = fminf(least, x), most = fmaxf(most, x);
+  });
+  if (__any(odd)) least = -__builtin_inff(), most = __builtin_inff();
+#pragma unroll
+  for (int d = 32; d; d >>= 1) {
+    least = fminf(least, __shfl_xor(least, d));
+    most = fmaxf(most, __shfl_xor(most, d));
+  }
+  if (lane == 0) widths[0][wave] = least, widths[1][wave] = most;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) least = fminf(least, widths[0][w]), most = fmaxf(most, widths[1][w]);
+  const float width = most - least, per = (kDigits - 1) / width;
+  if (__builtin_isfinite(width) && __builtin_isfinite(per)) {
+    auto digit_of = [&](float x) { return min((unsigned)((x - least) * per), kDigits - 1u); };
+    each_score([&](float x, bool in, int) { atomicAdd(&hists[0][in ? digit_of(x) : kDigits + lane], 1u); });
+    __syncthreads();
+    unsigned rank = r.want - 1, count;
+    const unsigned digit = find_digit(hists[0], rank, count);
+    if (count <= 64) {
+      float *const few = reinterpret_cast<float *>(hists[1]);  // in any order
+      each_score([&](float x, bool in, int) {
+        const uint64_t these = __ballot(in && digit_of(x) == digit);
+        if (!these) return;
+        unsigned first = 0;
+        if (lane == 0) first = atomicAdd(&listed, (unsigned)__popcll(these));
+        first = __builtin_amdgcn_readfirstlane(first);
+        if (these >> lane & 1) few[first + rank_in_mask(these)] = x;
+      });
+      __syncthreads();
+      const Few found(few, count, rank);
+      unsigned above = 0, at = 0;
+      each_score([&](float x, bool in, int) {
+        above += __popcll(__ballot(in && x > found.threshold));
+        at += __popcll(__ballot(in && x == found.threshold));
+      });
+      begin_at(above, at, found.equal);
+      each_score([&](float x, bool in, int first) {
+        put(r, __ballot(in && x > found.threshold), __ballot(in && x == found.threshold), found.equal, first, place,
+            ties);
+      });
+      return;
+    }
+  }
+  clear(hists[1]);
+  clear(hists[2]);
+  __syncthreads();
+  clear(hists[0]);  // for the last pass
+  auto each_key = [&](auto f) {
+    each_score([&](float x, bool in, int first) { f(in ? ordered(x) : 0u, first); });
   };
   Threshold t;
   t.rank = r.want - 1;
-  __syncthreads();
 #pragma unroll 1
   for (int pass = 0;; ++pass) {
-    each_key([&](unsigned x, int) { t.count(hists[pass], pass, x); });
+    unsigned *const hist = hists[pass < 2 ? pass + 1 : 0];
+    each_key([&](unsigned x, int) { t.count(hist, pass, x); });
     __syncthreads();
-    if (!t.next(hists[pass], pass)) break;
+    if (!t.next(hist, pass)) break;
   }
-  unsigned above = 0, same = 0;
+  unsigned above = 0, at = 0;
   each_key([&](unsigned x, int) {
     above += __popcll(__ballot((x & t.known) > t.key));
-    same += __popcll(__ballot((x & t.known) == t.key));
+    at += __popcll(__ballot((x & t.known) == t.key));
   });
-  if (lane == 0) marks[0][wave] = above, marks[1][wave] = same;
-  __syncthreads();
-  unsigned place = a.sink, ties = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) {
-      place += marks[0][w] + min(marks[1][w], t.equal - min(t.equal, ties));
-      ties += marks[1][w];
-    }
-  }
+  begin_at(above, at, t.equal);
   each_key([&](unsigned x, int first) { put(r, t, x, first, place, ties); });
 }
 
@@ -1013,18 +1126,24 @@ extern "C" int cascade_kv_select(const cascade_kv_pool_t *pool, int32_t layer, c
   if (rows >= INT32_MAX / kBlock) return CASCADE_EINVAL;
   const auto s = static_cast<hipStream_t>(stream);
   const int per_tile = 16 >> a.shift;
-  const int tiles = (batch->max_new - 1) / per_tile + 1;
+  const int tiles = (std::min(batch->max_new, batch->n_tokens) - 1) / per_tile + 1;
   const bool many = tiles >= 4 && a.padded <= 16;
   const int each = many ? many_sets(format->head_dim) * kWaves : 1, sets = (tiles - 1) / each + 1;
-  if (sets > 65535) return CASCADE_EINVAL;
-  // Large enough that rounding the queries of several sets costs little beside
-  // the products (2001 blocks, 128 sets of 8 heads: entries of 64, 128, 256 and 512 take 46, 34, 28
-  // and 32 us), small where there is little to share: one request's next token takes 6.6 us
-  // by 32 and 8.6 by 64, 128 requests' 48 and 50.
+  if (!many && sets > 65535) return CASCADE_EINVAL;
+  // One round of workgroups where there are many sets: each begins with 5 us of loads and of rounding its
+  // queries, and 32 blocks more take 2 us (512 tokens, 64 heads: of 4000 blocks 61 us, with at most 256
+  // entries to a workgroup 81; of 2001 blocks 39 and 45).  Small where there is little to share:
+  // one request's next token takes 6.6 us by 32 and 8.6 by 64, 128 requests' 48 and 50.
   const int64_t share = (int64_t)batch->n_entries * format->kv_heads * sets / 512;
-  a.span = many ? (int)std::min<int64_t>(std::max<int64_t>((share + 15) / 16 * 16, 32), 256) : 32;
+  a.span = many ? (int)std::min<int64_t>(std::max<int64_t>((share + 31) / 32 * 32, 32), 1024) : 32;
   if (batch->n_entries > a.keep) {  // else every token keeps all that it sees
-    const dim3 grid(((batch->n_entries + a.span - 1) / a.span + 7) / 8 * 8, sets, many ? format->kv_heads : 1);
+    // of many row sets no more workgroups than a launch takes
+    auto pieces = [&] { return ((int64_t)(batch->n_entries - 1) / a.span + 1) * sets * format->kv_heads; };
+    while (many && pieces() > 1 << 22 && a.span < batch->n_entries) a.span *= 2;
+    a.spans = (batch->n_entries - 1) / a.span + 1;
+    a.sets = sets;
+    const int64_t groups = many ? pieces() : a.spans;
+    const dim3 grid((unsigned)((groups + 7) / 8 * 8), many ? 1 : sets);
     args->dtype == CASCADE_BF16 ? score<CASCADE_BF16>(a, many, grid, s) : score<CASCADE_F16>(a, many, grid, s);
   }
   // A wave to a row where all rows fit its registers (none has more candidates than the

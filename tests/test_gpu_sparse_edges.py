@@ -248,3 +248,49 @@ def test_scores_that_are_no_numbers_are_the_largest(dev, counts, heads):
             last = int(b["len"][i]) - counts[i] + j
             want = [0] + list(range(10, 27)) + [last // bt - 1, last // bt]
             assert (got[int(b["off"][i]) + j] == torch.tensor(want)).all()
+
+
+@pytest.mark.parametrize("blocks", [180, 5300])  # the second is more than a workgroup's registers hold
+@pytest.mark.parametrize("scores", ["", "ties", "two values", "infinite", "one above", "far apart"])
+def test_select_few_rows_of_any_scores(dev, scores, blocks):
+    """Rows that a workgroup each takes: scores that fall into one part of their
+    range, or have none."""
+    rng = np.random.default_rng(28)
+    H, h, d, bt, keep = 4, 4, 64, 16, 41
+    b = ref.batch(rng, [1, 2, 0], [blocks * 16 - 3, blocks * 8, 50], bt)
+    pool = make_pool(rng, 1, b, h, d, bt, spread=1)
+    sref.random_bounds(rng, pool[0], h, d, bt, scores == "ties")
+    n = ref.chunk_bytes(h, d, bt) - 16
+    scale = pool[0, 0, :, n:n + 16].contiguous().view(torch.float32)
+    if scores == "two values":  # all scores alike but for the scale
+        for s in range(2):
+            pool[0, s, :, n + 16:] = pool[0, s, :1, n + 16:]
+        scale[:] = 1.0
+        scale[torch.from_numpy(rng.permutation(b["pool"])[:15])] = 2.0
+    elif scores == "infinite":
+        scale[::40] = float("inf")
+    elif scores == "one above":
+        scale[7] = 2.0 ** 40
+    elif scores == "far apart":
+        scale[:] = torch.exp2(torch.from_numpy(rng.integers(-90, 90, scale.shape)).float())
+    pool[0, 0, :, n:n + 16] = scale.view(torch.uint8)
+    q = rows(rng, b["tokens"], H, d, torch.bfloat16)
+    want = sref.select(pool[0], q, b, h, d, bt, keep, 1, 2)
+    kv = dev.DeviceKvPool(pool.cuda(), h, d, bt, bounds=True)
+    assert torch.equal(run_select(dev, kv, q.cuda(), on_gpu(b), keep, 1, 2).cpu(), want)
+
+
+@pytest.mark.parametrize("h", [3, 8])
+def test_select_long_spans(dev, h):
+    """Workgroups of over 200 table entries, and a request that begins and ends
+    inside one; heads that do not divide the XCDs evenly."""
+    rng = np.random.default_rng(29)
+    d, bt, keep = 64, 16, 9
+    group = 16 if h == 3 else 6
+    b = ref.batch(rng, [300, 2, 40], [24000, 900, 8000], bt)
+    pool = make_pool(rng, 1, b, h, d, bt)
+    sref.random_bounds(rng, pool[0], h, d, bt)
+    q = rows(rng, b["tokens"], group * h, d, torch.float16)
+    want = sref.select(pool[0], q, b, h, d, bt, keep, 1, 2)
+    kv = dev.DeviceKvPool(pool.cuda(), h, d, bt, bounds=True)
+    assert torch.equal(run_select(dev, kv, q.cuda(), on_gpu(b), keep, 1, 2).cpu(), want)
