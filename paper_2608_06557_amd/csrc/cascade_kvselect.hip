@@ -23,11 +23,13 @@
 // and its scale is read, so 128 single tokens over 84 thousand blocks are bound
 // by HBM: 49 us, 210 MB fetched (the bounds are 173; the 1 KB of a block begin inside a
 // line), 4.3 TB/s.  With many rows of one request the bounds come from LDS for four
-// waves' row sets: 128 sets of 8 heads over 2001 blocks 25 us, by the vector
+// waves' row sets: 128 sets of each of 8 KV heads over 2001 blocks 23 us, by the vector
 // instructions of scaling and of the heads' largest, and by their latency.
-// select: a row's candidates stay in registers, of a workgroup or of one wave; a radix
-// selection in LDS finds the least score that stays, and ballots write the blocks in
-// order.  1024 rows of up to 2000 blocks 10 us, 4096 rows of 2000 19 us.
+// select: a row's candidates stay in registers, of a workgroup or of one wave; a
+// histogram of their range in LDS leaves few in the part where the least score that
+// stays is (else a radix selection over the scores' bits finds it), and ballots write
+// the blocks in order.  1024 rows of 660 blocks 9.6 us, 4096 rows of 2000 17 us (a wave
+// to a row), of 4000 35 us (a workgroup).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
