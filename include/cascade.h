@@ -680,7 +680,10 @@ int cascade_attention(const cascade_kv_pool_t *pool, int32_t layer,
    workspace: cascade_attention_shared_workspace_bytes(...) bytes, 256-byte
    aligned, of any content; it grows with n_tokens.
    Errors as cascade_attention; leaders, lengths or slots that are not as above, or
-   a group of more than max_tokens new tokens, set *status_dev = CASCADE_EINVAL. */
+   a group of more than max_tokens new tokens, set *status_dev = CASCADE_EINVAL.  Rows of
+   a request outside the domain, or with a leader or length that is not as above, are left
+   as they were, and so are all rows of a group that has too many new tokens or whose last
+   request is such a one. */
 typedef struct {
   const int32_t *leader;     /* [n] */
   const int32_t *shared_len; /* [n] */

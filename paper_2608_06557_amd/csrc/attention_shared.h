@@ -24,6 +24,27 @@ struct SharedJoin {
   PartSet of[2];
 };
 
+// Whether what `sources` says of a token was said by this call: a request that has
+// it was taken, and the group if it is in one.  Called by all lanes, where
+// something was refused.
+__device__ __forceinline__ bool taken(const Attention &a, int token) {
+  const int lane = lane_id();
+  bool alone = false, found = false;
+  int leader = -1;
+  for (int i = lane; i < a.batch.n; i += 64) {
+    const int what = a.taken[i];
+    if (what == kRefused || token < a.batch.token_offsets[i] || token >= a.batch.token_offsets[i + 1]) continue;
+    if (what == kAlone) alone = true;
+    else leader = a.leader[i];
+  }
+  if (__any(alone)) return true;
+  const uint64_t in = __ballot(leader >= 0);
+  if (!in) return false;
+  leader = __builtin_amdgcn_readlane(leader, __ffsll((unsigned long long)in) - 1);
+  for (int i = lane; i < a.batch.n; i += 64) found |= a.taken[i] == kGroup && a.leader[i] == leader;
+  return __any(found);
+}
+
 // Joins what is known of each row, a row to a wave: the parts of its request's
 // segment, or its state, and the same of its group's.  A chain of dependent loads,
 // then the parts: 128 tokens of 64 heads of 128 dims 9 us behind 32 groups of 4 tokens, 11 where
@@ -36,6 +57,7 @@ __global__ __launch_bounds__(kBlock) void join_shared_kernel(Attention a, Shared
   if (row >= rows) return;
   const int lane = lane_id(), token = (int)(row / a.q_heads), head = (int)(row % a.q_heads);
   // rows of no request stay as they are
+  const int refused = uniform_load(a.taken + a.batch.n);
   if (token < uniform_load(a.batch.token_offsets) || token >= uniform_load(a.batch.token_offsets + a.batch.n)) return;
   const float *parts[2], *sums[2];  // of the first of each
   int count[2], step[2];            // how many, and rows from one place to the next
@@ -47,7 +69,7 @@ __global__ __launch_bounds__(kBlock) void join_shared_kernel(Attention a, Shared
     if (k == 0 && s.kind == kWritten) return;
     const bool split = s.kind >= kParts;
     const PartSet &p = j.of[s.kind == kParts + 1];
-    // nothing was told of a request outside the domain: whatever its source says is bounded
+    // within the workspace whatever was told
     const int w = min(max(s.w, 1), p.groups - 1);
     const int in_tile = min(max(s.row, 0) + head % a.group, p.rows - 1);
     const int64_t first = split ? (int64_t)(w - 1) * 2 * p.rows + in_tile : (k ? rows : 0) + row;
@@ -56,6 +78,7 @@ __global__ __launch_bounds__(kBlock) void join_shared_kernel(Attention a, Shared
     count[k] = split ? min(max(s.last, w), p.groups - 1) - w + 2 : s.kind == kState;
     step[k] = split ? p.rows : 0;
   }
+  if (__builtin_expect(refused, false) && !taken(a, token)) return;
   // two places a workgroup: part 0 ends its range, the others begin theirs
   const int all = count[0] + count[1];
   auto place = [&](int c, int &k) -> int64_t {

@@ -230,7 +230,12 @@ struct Attention : Cuts {
   float *states;           // [2][n_tokens][q_heads][kDim], as parts: of a request's segments, and of a group's
   float *state_sums;       // [2][n_tokens][q_heads][2]
   Source *sources;         // [2][n_tokens][KV heads]
+  int *taken;              // [n]: Taken of each request; then whether something was refused
 };
+
+// What became of a request: refused, taken by itself, or with the rest of its
+// group, which its last request brings if that is not refused.
+enum Taken : int { kRefused, kAlone, kGrouped, kGroup };
 
 // The list of Form::kShared holds segments of requests, and of groups, whose
 // `count` is negative; `ids` are their first rows, turned over where a request is
@@ -356,11 +361,13 @@ struct Range {
   // The same of requests that share their first tokens: a thread puts its
   // request in, without them, and if it is the last of its group the group.
   // What it needs comes in two rounds of loads; what is only told and not
-  // relied on is looked up by one workgroup.
+  // relied on is looked up by one workgroup, which also says what was refused.
   template <int kW>
   static __device__ __forceinline__ void fill(const Attention &a, const SharedList &list, unsigned long long *scan,
                                               int &n, long long &total) {
     const int shift = a.kv.block_shift;
+    const bool says = a.which == 0 && blockIdx.x == 0;
+    bool refused = false;
     for (int i0 = 0; i0 < a.batch.n; i0 += 64 * kW) {
       const int i = i0 + threadIdx.x;
       unsigned long long v[2] = {0, 0}, all[2];
@@ -403,6 +410,8 @@ struct Range {
           if (g.ok && group_rows > a.min_rows && group_rows <= a.max_rows)
             group_cost = MixedSegments(g.len, -g.count, a.tile_tokens).total() * a.kv.kv_heads;
         }
+        refused |= !r.ok || (g.len && !g.ok);
+        if (says) a.taken[i] = !r.ok ? kRefused : !shared ? kAlone : g.ok ? kGroup : kGrouped;
       }
       v[0] = cost + group_cost;
       v[1] = (cost > 0) + (group_cost > 0);
@@ -424,6 +433,10 @@ struct Range {
       }
       n += __builtin_amdgcn_readfirstlane((int)all[1]);
       total += first_lane(all[0]);
+    }
+    if (says) {
+      refused = __syncthreads_or(refused);
+      if (threadIdx.x == 0) a.taken[a.batch.n] = refused;
     }
   }
 

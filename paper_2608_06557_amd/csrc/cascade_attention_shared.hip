@@ -24,13 +24,14 @@ namespace {
 // The workspace of attention, then what is known of each row.
 struct Places {
   Workspace w;
-  size_t states, sums, sources, total;
+  size_t states, sums, sources, taken, total;
   Places(const cascade_kv_format_t *f, const cascade_kv_batch_t *b, int q_heads) : w(layout(f, b, q_heads, 0)) {
     const size_t rows = 2 * (size_t)b->n_tokens * q_heads;
     states = w.total;
     sums = states + aligned(sizeof(float) * rows * f->head_dim);
     sources = sums + aligned(sizeof(float) * rows * 2);
-    total = sources + aligned(sizeof(Source) * 2 * b->n_tokens * f->kv_heads);
+    taken = sources + aligned(sizeof(Source) * 2 * b->n_tokens * f->kv_heads);
+    total = taken + aligned(sizeof(int) * (kMaxBatch + 1));
   }
 };
 }  // namespace
@@ -68,6 +69,7 @@ extern "C" int cascade_attention_shared(const cascade_kv_pool_t *pool, int32_t l
   a.states = reinterpret_cast<float *>(ws + p.states);
   a.state_sums = reinterpret_cast<float *>(ws + p.sums);
   a.sources = reinterpret_cast<Source *>(ws + p.sources);
+  a.taken = reinterpret_cast<int *>(ws + p.taken);
   if ((int64_t)batch->n_tokens * args->q_heads > INT32_MAX / kBlock) return CASCADE_EINVAL;
   const SharedCall c = {a, ws, p.w, cap, static_cast<hipStream_t>(stream)};
   return args->dtype == CASCADE_BF16 ? shared_attention_bf16(c) : shared_attention_f16(c);
