@@ -358,6 +358,24 @@ struct Range {
     }
   }
 
+  // Whether request i of each lane, which names `first` as the one before names
+  // `before`, follows that one without a gap: all from there on name it.  A wave has 64
+  // neighbours, so it is told by where the run of equal names began, and only a run that came
+  // in from another wave is looked up.  Called by all lanes.
+  static __device__ __forceinline__ bool follows(const Attention &a, int i, int first, int before) {
+    const int lane = lane_id(), i0 = i - lane;
+    const uint64_t begins = __ballot(first == i || i == 0 || first != before);
+    bool same = true;
+    if (!(begins & 1)) {
+      const int head = __builtin_amdgcn_readfirstlane(first);
+      same = head >= 0 && head < i0 && i0 < a.batch.n;
+      for (int j = same ? head + lane : i0; j < i0; j += 64) same &= a.leader[j] == head;
+      same = __all(same);
+    }
+    const uint64_t mine = begins & ~0ull >> (63 - lane);
+    return mine ? first == i0 + 63 - __clzll((long long)mine) : same;
+  }
+
   // The same of requests that share their first tokens: a thread puts its
   // request in, without them, and if it is the last of its group the group.
   // What it needs comes in two rounds of loads; what is only told and not
@@ -374,12 +392,12 @@ struct Range {
       KvRequest r = {}, g = {};  // of the request, of its group
       unsigned long long cost = 0, group_cost = 0;
       int shared = 0;
+      const int here = min(i, a.batch.n - 1);
+      r = kv_request(a.batch, a.row_offsets, shift, here);
+      const int first = a.leader[here], before = a.leader[max(here - 1, 0)];
+      const int after = here + 1 < a.batch.n ? a.leader[here + 1] : -1;
+      r.ok &= follows(a, i, first, before);
       if (i < a.batch.n) {
-        r = kv_request(a.batch, a.row_offsets, shift, i);
-        const int first = a.leader[i], before = i > 0 ? a.leader[i - 1] : -1;
-        const int after = i + 1 < a.batch.n ? a.leader[i + 1] : -1;
-        // a group's requests are neighbours
-        r.ok &= first >= 0 && first <= i && (first == i || before == first);
         if (r.ok && (first < i || after == first)) {
           shared = a.shared_len[first];
           const int first_row = a.row_offsets[first], first_token = a.batch.token_offsets[first];
@@ -395,8 +413,7 @@ struct Range {
           }
           if (r.ok && blockIdx.x == 0) {
             const int last = (shared >> shift) - 1;
-            if (a.leader[first] != first || (shared && a.slots[first_row + last] != a.slots[r.row + last]))
-              kv_report(a.status);
+            if (shared && a.slots[first_row + last] != a.slots[r.row + last]) kv_report(a.status);
           }
         }
         if (!r.ok) {

@@ -87,3 +87,43 @@ def test_refused_rows_stay(dev, fault, heads):
         part = {k: v[good] for k, v in e.items() if k != "weight"}
         check_attention((out[good], lse[good], None), part, "bf16", d, 0)
         assert torch.equal(out, results[0][0]) and torch.equal(lse, results[0][1])
+
+
+# leaders that name a request apart from them, or no first one; the rows that are left, and the groups beside
+APART = {
+    "behind one": ([0, 1, 0, 0], [2, 3], []),
+    "behind a group": ([0, 0, 2, 2, 0, 0], [4, 5], [(0, 2), (2, 4)]),
+    "of a member": ([0, 0, 1, 1], [2, 3], [(0, 2)]),
+    "of the next": ([1, 1, 1, 3], [0], [(1, 3)]),
+    "of a group far behind": ([0] * 70 + [70] * 70 + [0] * 70, list(range(140, 210)), [(0, 70), (70, 140)]),
+    "across waves": ([0] * 30 + [29] * 100 + [130] * 140 + [127] * 30, list(range(30, 130)) + list(range(270, 300)),
+                     [(0, 30), (130, 270)]),
+}
+
+
+@pytest.mark.parametrize("case", APART)
+def test_groups_that_are_no_neighbours_leave_others_alone(dev, case):
+    """Requests that name a first one they do not follow are refused, and what
+    lies between is right."""
+    leader, left, groups = APART[case]
+    rng = np.random.default_rng(13)
+    H, h, d, bt, n = 4, 2, 64, 16, len(leader)
+    shared = 3200 if n < 9 else 256
+    b = shared_batch(rng, [(0, [(1, shared + 800 if n < 9 else shared + 60)])] * n, bt)
+    for first, end in groups:
+        at = int(b["rows"][first])
+        for i in range(first + 1, end):
+            row = int(b["rows"][i])
+            b["slots"][row:row + shared // bt] = b["slots"][at:at + shared // bt].clone()
+    pool = ref.random_pool(rng, 1, b["pool"], h, d, bt)
+    q = rows(rng, n, H, d, torch.bfloat16)
+    e = ref.attend(pool[0], q, b, h, d, bt, 0.2)
+    b["leader"] = torch.tensor(leader, dtype=torch.int32)
+    b["shared"][:] = shared
+    out, lse, op = attend_over(dev, pool.cuda(), q.cuda(), b, h, d, bt, n)
+    with pytest.raises(RuntimeError):
+        op.kv.check()
+    good = [t for t in range(n) if t not in left]
+    part = {k: v[good] for k, v in e.items() if k != "weight"}
+    check_attention((out[good], lse[good], None), part, "bf16", d, 0)
+    assert (out[left] == 7).all() and (lse[left] == 7).all()
