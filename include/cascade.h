@@ -721,7 +721,7 @@ int cascade_kv_bounds(const cascade_kv_pool_t *pool, int32_t layer,
    of the b blocks up to the token's own the first `sink`, the last `recent`
    (>= 1: the own one), and of the others those with the largest score until `keep` are
    listed (equal scores: the lower index first), or all if b <= keep.
-     score = scale * max_r 2^(e_r - e) sum_d max(n_rd, 0) u_d + min(n_rd, 0) l_d
+     score = scale * max_r 2^max(e_r - e, -126) sum_d max(n_rd, 0) u_d + min(n_rd, 0) l_d
    with u, l and scale the block's bounds and K scale (they have to be up to date), r the query heads
    of the KV head, e_r the least exponent >= -100 at which q_r is at most 127 * 2^e_r,
    n_r = q_r / 2^e_r rounded to nearest even, e the largest e_r: up to the roundings

@@ -404,12 +404,13 @@ struct RowSet {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(q.minus[s], lower, sum, 0, 0, 0);
   }
   // The scores of 16 blocks from `b` on by the sums of their products with `kTiles` sets; `in`:
-  // the lane's is one.  `next` lies between two tokens' scores.  `add`: of a token's heads these
-  // are not the first.  (Step by step for all sets, each of which has a step's latency to itself
+  // the lane's is one.  `next` lies between two tokens' scores.  `add`, `more`: of a token's heads
+  // these are not the first, not the last; scaled is the largest of all, as a scale that is not
+  // finite makes the largest score of another part.  (Step by step for all sets, each of which has a step's latency to itself
   // otherwise.)
   template <int kTiles>
   static __device__ __forceinline__ void score(const Select &a, const RowSet (&set)[kTiles], const i4 (&sum)[kTiles],
-                                               float scale, int b, bool in, int64_t next, bool add) {
+                                               float scale, int b, bool in, int64_t next, bool add, bool more) {
     const int shift = kWide ? 4 : a.shift;
     float x[kTiles][4];
 #pragma unroll
@@ -421,8 +422,10 @@ struct RowSet {
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) {
         float *const at = set[t].to + k * next + b;
-        const float y = __builtin_fmaf(x[t], scale, 0.f);  // no -0
-        if (in && k < set[t].left) *at = kWide && add ? fmaxf(*at, y) : y;
+        if (in && k < set[t].left) {
+          const float y = kWide && add ? fmaxf(*at, x[t]) : x[t];
+          *at = kWide && more ? y : __builtin_fmaf(y, scale, 0.f);  // no -0
+        }
       }
     };
     float y[kTiles];
@@ -494,7 +497,7 @@ __device__ __forceinline__ void score_blocks(const Select &a, const KvRequest &r
       i4 sum[1] = {i4{0, 0, 0, 0}};
 #pragma unroll
       for (int s = 0; s < kDim / 64; ++s) sum[0] = set.add(bounds.upper[s], bounds.lower[s], s, sum[0]);
-      set.score(a, sets, sum, bounds.scale, b0, b0 + n16 < end, next, p > 0);
+      set.score(a, sets, sum, bounds.scale, b0, b0 + n16 < end, next, p > 0, p + 1 < parts);
       if (b0 + 16 < end) {
         bounds.fetch(a.kv, head, slot, bad_slot);
         slot = look(b0 + 32);
@@ -603,7 +606,7 @@ __device__ __forceinline__ void score_sets(const Select &a, const KvRequest &r, 
       for (int s = 0; s < kDim / 64; ++s)
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) sum[t] = set[t].add(upper[s], lower[s], s, sum[t]);
-      set[0].score(a, set, sum, scale, b, b + (lane_id() & 15) < end, next, false);
+      set[0].score(a, set, sum, scale, b, b + (lane_id() & 15) < end, next, false, false);
     }
     stage.put(to);
     stage.fetch(a.kv, head, bad_slot);
