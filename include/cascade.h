@@ -734,13 +734,19 @@ int cascade_kv_bounds(const cascade_kv_pool_t *pool, int32_t layer,
    then -1; tokens of no request are left as they are.
    workspace: cascade_kv_select_workspace_bytes(...) bytes, 256-byte aligned, of
    any content (4 bytes per table entry, KV head and new token of the longest
-   run: it grows with n_entries and max_new).
-   Errors as cascade_attention. */
+   run: it grows with n_entries and max_new), or with most_blocks
+   256 + 4 * n_tokens * kv_heads * (most_blocks rounded up to 16) bytes if that is less, which
+   it is where single tokens and a chunk share a batch.  It may be smaller, down to what the same
+   batch with max_new = 1 needs: the tokens of each request are then taken in runs, as many at a
+   time as it holds, by two launches for each run.
+   Errors as cascade_attention; CASCADE_EINVAL also for tables of over 2^28 entries. */
 typedef struct {
   int32_t dtype, q_heads;     /* as cascade_attention_t */
   int32_t keep, sink, recent; /* 1 .. 65536; >= 0; >= 1; sink + recent <= keep */
   cascade_rows_t q;
   int32_t *selected;
+  int32_t most_blocks;        /* most blocks of one request, or 0: not known.  A request of more is
+                                 outside the domain, its rows are left as they were */
 } cascade_select_t;
 size_t cascade_kv_select_workspace_bytes(const cascade_kv_format_t *format,
                                          const cascade_kv_batch_t *batch);

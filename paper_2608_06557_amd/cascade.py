@@ -146,7 +146,8 @@ class Shared(C.Structure):
 
 class Select(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("q_heads", C.c_int32), ("keep", C.c_int32),
-                ("sink", C.c_int32), ("recent", C.c_int32), ("q", Rows), ("selected", C.c_void_p)]
+                ("sink", C.c_int32), ("recent", C.c_int32), ("q", Rows), ("selected", C.c_void_p),
+                ("most_blocks", C.c_int32)]
 
 
 class Evict(C.Structure):

@@ -203,7 +203,9 @@ struct Select {
   int keep, sink, recent;
   int span;    // table entries of a workgroup
   int spans, sets;  // how many, and sets of rows of a workgroup
-  float *scores;  // request by request [token][KV head][block], in whole lines of 16
+  int first, run;   // the new tokens of each request that are scored and selected, and how many at most
+  int most, pitch;  // by tokens: blocks of a request, and those in whole lines of 16; else any and 0
+  float *scores;  // [token][KV head][pitch], or request by request [token of the run][KV head][block], in lines of 16
   int32_t *selected;
   int32_t *status;
 };
@@ -211,14 +213,16 @@ struct Select {
 __device__ __forceinline__ int blocks_of(const KvRequest &r, int block_shift) {
   return (int)(((long long)r.len + (1 << block_shift) - 1) >> block_shift);
 }
-// A row's scores, and how many there is room for.  Where request i's begin: 16
-// (floor(row / 16) + i) lines' places for each token and head, which leaves room for its blocks
-// rounded up, as the next request's row is at least as many entries further.
+// A row's scores, and how many there is room for; `token` is one of the run.  By tokens a row's
+// place is its number.  By requests, where request i's begin: 16 (floor(row / 16) + i) lines' places for each
+// token and head, which leaves room for its blocks rounded up, as the next request's row is at
+// least as many entries further.
 __device__ __forceinline__ int score_pitch(const Select &a, const KvRequest &r) {
-  return (blocks_of(r, a.kv.block_shift) + 15) & ~15;
+  return a.pitch ? a.pitch : (blocks_of(r, a.kv.block_shift) + 15) & ~15;
 }
 __device__ __forceinline__ float *scores_of(const Select &a, const KvRequest &r, int i, int token, int head) {
-  const int64_t first = ((int64_t)(r.row & ~15) + 16 * i) * a.batch.max_new * a.kv.kv_heads;
+  const int64_t first = a.pitch ? (int64_t)r.first * a.kv.kv_heads * a.pitch
+                                : ((int64_t)(r.row & ~15) + 16 * i) * a.run * a.kv.kv_heads;
   return a.scores + first + ((int64_t)token * a.kv.kv_heads + head) * score_pitch(a, r);
 }
 
@@ -631,16 +635,20 @@ struct Candidates {
 // Neighbouring pieces of work on one XCD (workgroups go to the 8 in turn; blockIdx.x is one of a multiple of 8).
 __device__ __forceinline__ int piece() { return (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3); }
 
-// Entries span .. of the table, the requests in them one after another.
+// Entries span .. of the table, the requests in them one after another, with the
+// tokens of the run as their new ones.
 template <typename F>
 __device__ __forceinline__ void each_request(const Select &a, int span, int first_token, unsigned *lds, F f) {
   if ((int64_t)span * a.span >= a.batch.n_entries) return;
   const int e0 = span * a.span, e1 = e0 + min(a.span, a.batch.n_entries - e0);
   for (int i = __builtin_amdgcn_readfirstlane(owner_of(a.row_offsets, a.batch.n, e0, lds));
        i < a.batch.n && uniform_load(a.row_offsets + i) < e1; ++i) {
-    const KvRequest r = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, i);
-    if (!r.ok || first_token >= r.count) continue;
-    const Candidates c(a, blocks_of(r, a.kv.block_shift));
+    KvRequest r = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, i);
+    r.first += a.first;
+    r.count = min(r.count - a.first, a.run);
+    const int blocks = blocks_of(r, a.kv.block_shift);
+    if (!r.ok || blocks > a.most || first_token >= r.count) continue;
+    const Candidates c(a, blocks);
     const int begin = max(c.begin, e0 - r.row), end = min(c.end, e1 - r.row);
     if (begin < end) f(r, i, begin, end);
   }
@@ -704,7 +712,9 @@ __device__ __forceinline__ Row row_of(const Select &a, const KvRequest &q, int i
   if (blocks <= a.keep) {
     for (int k = lane; k < a.keep; k += width) r.out[k] = k < blocks ? k : -1;
   } else {
-    r.score = scores_of(a, q, i, j, head);
+    KvRequest run = q;  // as each_request has it
+    run.first += a.first;
+    r.score = scores_of(a, run, i, j - a.first, head);
     r.begin = a.sink, r.end = blocks - a.recent, r.want = a.keep - a.sink - a.recent;
     for (int k = lane; k < a.sink; k += width) r.out[k] = k;
     for (int k = lane; k < a.recent; k += width) r.out[a.keep - a.recent + k] = r.end + k;
@@ -770,6 +780,16 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_wave_barrier();
 }
 
+// Whether a token is a new one of request `q` and of the run; reports a request of too many blocks.
+__device__ __forceinline__ bool in_run(const Select &a, const KvRequest &q, int token) {
+  if (!q.ok || token < q.first || token - q.first >= q.count) return false;
+  if (blocks_of(q, a.kv.block_shift) > a.most) {
+    kv_report(a.status);
+    return false;
+  }
+  return (unsigned)(token - q.first - a.first) < (unsigned)a.run;
+}
+
 // Writes those of 64 blocks that stay, in order, and moves on: the ones above the
 // threshold and the first of the ones at it.
 __device__ __forceinline__ void put(const Row &r, uint64_t above, uint64_t at, unsigned equal, int first,
@@ -822,7 +842,7 @@ __global__ __launch_bounds__(kBlock) void select_wave_kernel(Select a) {
   while (i < a.batch.n && a.batch.token_offsets[i + 1] <= token) ++i;
   if (i >= a.batch.n || token >= a.batch.n_tokens) return;
   const KvRequest q = kv_request(a.batch, a.row_offsets, a.kv.block_shift, i);
-  if (!q.ok || token < q.first || token - q.first >= q.count) return;
+  if (!in_run(a, q, token)) return;
   const Row r = row_of(a, q, i, token, head, lane, 64);
   if (r.want == 0) return;
   const int m = __builtin_amdgcn_readfirstlane(r.end - r.begin);
@@ -928,8 +948,8 @@ __global__ __launch_bounds__(kBlock) void select_block_kernel(Select a) {
     i = __builtin_amdgcn_readfirstlane(owner_of(a.batch.token_offsets, a.batch.n, token, sums));
     if (i >= a.batch.n) return;
     q = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, i);
-    if (!q.ok || token < q.first || token - q.first >= q.count) return;
   }
+  if (!in_run(a, q, token)) return;
   const Row r = row_of(a, q, i, token, head, threadIdx.x, kBlock);
   if (r.want == 0) return;
   if (r.end - r.begin <= 64) {  // one wave's, a score to a lane: how many are above it?
@@ -1052,9 +1072,14 @@ bool bounds_fit(const cascade_kv_pool_t *p, const cascade_kv_format_t *f) {
   return p->chunk_bytes >= kv_chunk_bytes(f) + (int64_t)f->kv_heads * f->head_dim;
 }
 
+// Places for the scores of one new token of each request.
 size_t score_bytes(const cascade_kv_format_t *f, const cascade_kv_batch_t *b) {
-  return sizeof(float) * ((size_t)b->n_entries + 16 * (size_t)b->n) * b->max_new * f->kv_heads;
+  return sizeof(float) * ((size_t)b->n_entries + 16 * (size_t)b->n) * f->kv_heads;
 }
+constexpr size_t kRoom = 256;      // of a workspace beside them
+constexpr int kMostRun = 32768;    // new tokens of a request that are ever scored at one time: a grid's second dimension
+// The most new tokens of a request.
+int most_tokens(const cascade_kv_batch_t *b) { return std::min(b->max_new, b->n_tokens); }
 
 // Row sets of a wave where there are many: what its registers hold.
 constexpr int many_sets(int dim) { return dim == 256 ? 2 : 4; }
@@ -1112,8 +1137,10 @@ extern "C" int cascade_kv_bounds(const cascade_kv_pool_t *pool, int32_t layer, c
 
 extern "C" size_t cascade_kv_select_workspace_bytes(const cascade_kv_format_t *format,
                                                     const cascade_kv_batch_t *batch) {
-  if (!kv_format_ok(format) || !batch || batch->n < 0 || batch->max_new < 0 || batch->n_entries < 0) return 0;
-  return score_bytes(format, batch) + 256;
+  if (!kv_format_ok(format) || !batch || batch->n < 0 || batch->max_new < 0 || batch->n_tokens < 0 ||
+      batch->n_entries < 0)
+    return 0;
+  return score_bytes(format, batch) * std::min(most_tokens(batch), kMostRun) + kRoom;
 }
 
 extern "C" int cascade_kv_select(const cascade_kv_pool_t *pool, int32_t layer, const cascade_kv_format_t *format,
@@ -1124,10 +1151,17 @@ extern "C" int cascade_kv_select(const cascade_kv_pool_t *pool, int32_t layer, c
     return CASCADE_EINVAL;
   if ((args->dtype != CASCADE_BF16 && args->dtype != CASCADE_F16) || args->q_heads < 1 ||
       args->q_heads % format->kv_heads || args->q_heads / format->kv_heads > 128 || args->sink < 0 ||
-      args->recent < 1 || args->keep > 65536 || (int64_t)args->sink + args->recent > args->keep)
+      args->most_blocks < 0 || args->recent < 1 || args->keep > 65536 || (int64_t)args->sink + args->recent > args->keep)
     return CASCADE_EINVAL;
   if (!workspace || ((uintptr_t)workspace & 255)) return CASCADE_EINVAL;
-  if (workspace_bytes < cascade_kv_select_workspace_bytes(format, batch)) return CASCADE_ENOSPC;
+  const int64_t rows = (int64_t)batch->n_tokens * format->kv_heads;
+  if (rows >= INT32_MAX / kBlock) return CASCADE_EINVAL;
+  // by tokens where that takes less, and is known to fit
+  const size_t one = score_bytes(format, batch), all = one * std::min(most_tokens(batch), kMostRun);
+  const int64_t lines = ((int64_t)args->most_blocks + 15) & ~15;
+  const size_t by_tokens = sizeof(float) * rows * lines;
+  const bool known = args->most_blocks > 0 && by_tokens <= all && workspace_bytes >= by_tokens + kRoom;
+  if (!known && workspace_bytes < one * std::min(most_tokens(batch), 1) + kRoom) return CASCADE_ENOSPC;
   if (batch->n == 0 || batch->n_tokens == 0 || batch->max_new == 0) return CASCADE_OK;
   if (!kv_rows_ok(&args->q) || !args->selected) return CASCADE_EINVAL;
   Select a = {};
@@ -1146,30 +1180,29 @@ extern "C" int cascade_kv_select(const cascade_kv_pool_t *pool, int32_t layer, c
   a.scores = static_cast<float *>(workspace);
   a.selected = args->selected;
   a.status = status_dev;
-  const int64_t rows = (int64_t)batch->n_tokens * format->kv_heads;
-  if (rows >= INT32_MAX / kBlock) return CASCADE_EINVAL;
   const auto s = static_cast<hipStream_t>(stream);
-  const int per_tile = 16 >> a.shift;
-  const int tiles = (std::min(batch->max_new, batch->n_tokens) - 1) / per_tile + 1;
+  // As many tokens at a time as the workspace holds, by 64, which fill a workgroup's row sets; where
+  // every token keeps all that it sees there are no scores.
+  const bool scored = batch->n_entries > a.keep;
+  const int tokens = most_tokens(batch);
+  a.most = args->most_blocks ? args->most_blocks : INT32_MAX;
+  a.pitch = known ? (int)lines : 0;
+  a.run = scored ? std::min(tokens, kMostRun) : tokens;
+  if (scored && !known) a.run = (int)std::min<size_t>((workspace_bytes - kRoom) / one, a.run);
+  if (a.run < tokens && a.run > 64) a.run &= -64;
+  const int tiles = (a.run - 1) / (16 >> a.shift) + 1;
   const bool many = tiles >= 4 && a.padded <= 16;
   const int each = many ? many_sets(format->head_dim) * kWaves : 1, sets = (tiles - 1) / each + 1;
-  if (!many && sets > 65535) return CASCADE_EINVAL;
   // One round of workgroups where there are many sets: each begins with 5 us of loads and of rounding its
   // queries, and 32 blocks more take 2 us (512 tokens, 64 heads: of 4000 blocks 61 us, with at most 256
   // entries to a workgroup 81; of 2001 blocks 39 and 45).  Small where there is little to share:
   // one request's next token takes 6.6 us by 32 and 8.6 by 64, 128 requests' 48 and 50.
   const int64_t share = (int64_t)batch->n_entries * format->kv_heads * sets / 512;
   a.span = many ? (int)std::min<int64_t>(std::max<int64_t>((share + 31) / 32 * 32, 32), 1024) : 32;
-  if (batch->n_entries > a.keep) {  // else every token keeps all that it sees
-    // of many row sets no more workgroups than a launch takes
-    auto pieces = [&] { return ((int64_t)(batch->n_entries - 1) / a.span + 1) * sets * format->kv_heads; };
-    while (many && pieces() > 1 << 22 && a.span < batch->n_entries) a.span *= 2;
-    a.spans = (batch->n_entries - 1) / a.span + 1;
-    a.sets = sets;
-    const int64_t groups = many ? pieces() : a.spans;
-    const dim3 grid((unsigned)((groups + 7) / 8 * 8), many ? 1 : sets);
-    args->dtype == CASCADE_BF16 ? score<CASCADE_BF16>(a, many, grid, s) : score<CASCADE_F16>(a, many, grid, s);
-  }
+  a.spans = (batch->n_entries - 1) / a.span + 1;
+  a.sets = sets;
+  const int64_t pieces = ((many ? (int64_t)a.spans * sets * format->kv_heads : a.spans) + 7) / 8 * 8;
+  if (scored && pieces > INT32_MAX / kBlock) return CASCADE_EINVAL;
   // A wave to a row where all rows fit its registers (none has more candidates than the
   // table has entries) and there are enough of them to fill the GPU.
   const bool waves = batch->n_entries <= 64 * kHeld && rows >= 2048;
@@ -1178,6 +1211,12 @@ extern "C" int cascade_kv_select(const cascade_kv_pool_t *pool, int32_t layer, c
   const bool longer = batch->n_entries > (int64_t)64 * kWaves * 8 * batch->n;
   const int64_t groups = waves ? (rows + kWaves - 1) / kWaves : rows;
   auto kernel = waves ? select_wave_kernel : longer ? select_block_kernel<16> : select_block_kernel<8>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)groups + 1), dim3(kBlock), 0, s, a);  // the last one checks the batch
+  for (a.first = 0; a.first < tokens; a.first += a.run) {
+    if (scored) {
+      const dim3 grid((unsigned)pieces, many ? 1 : sets);
+      args->dtype == CASCADE_BF16 ? score<CASCADE_BF16>(a, many, grid, s) : score<CASCADE_F16>(a, many, grid, s);
+    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)groups + 1), dim3(kBlock), 0, s, a);  // the last one checks the batch
+  }
   return hipGetLastError() == hipSuccess ? CASCADE_OK : CASCADE_EHIP;
 }

@@ -635,10 +635,13 @@ class DeviceKvSelect:
     """cascade_kv_select with its arguments and workspace laid out: `run` writes
     the blocks that q [tokens, query heads, dims] reads in `layer` to `selected`
     (int32 [tokens, KV heads, blocks]), the first `sink` and the last `recent` among
-    them.  The pool's bounds have to be up to date (DeviceKvBounds)."""
+    them.  The pool's bounds have to be up to date (DeviceKvBounds).  `most_blocks`,
+    if it is known, is the most blocks of one request: single tokens beside a chunk
+    need a fraction of the workspace then.  By a smaller workspace than its own the
+    tokens are taken in runs."""
 
     def __init__(self, kv: DeviceKvPool, batch: KvBatch, q, selected, sink: int = 0, recent: int = 1,
-                 layer: int = 0, workspace=None):
+                 layer: int = 0, workspace=None, most_blocks: int = 0):
         _needs_bounds(kv)
         if q.shape[0] < batch.tokens or q.shape[2] != kv.head_dim:
             raise ValueError("q does not fit the batch or the pool")
@@ -646,8 +649,10 @@ class DeviceKvSelect:
         self.tensors = (q, selected)
         _check_device(kv.pool.device, *self.tensors, *batch.tensors, workspace)
         self.c_args = cx.Select(_dtype(q), q.shape[1], selected.shape[-1], sink, recent, kv_rows(q),
-                                _selection(selected, kv, batch))
+                                _selection(selected, kv, batch), most_blocks)
         size = cx.cascade_kv_select_workspace_bytes(kv.c_format, batch.c_batch)
+        if most_blocks > 0:
+            size = min(size, 256 + 4 * batch.tokens * kv.kv_heads * (-(-most_blocks // 16) * 16))
         self.workspace, self.ws_ptr, self.ws_bytes = _workspace(workspace, size, q.device)
         self._call = cx.kv_call("cascade_kv_select", kv.c_pool, layer, kv.c_format, batch.c_batch,
                                 batch.c_table, self.c_args, self.ws_ptr, self.ws_bytes,
