@@ -158,7 +158,7 @@ __global__ __launch_bounds__(kBlock) void bounds_kernel(Bounds a) {
     return;
   }
   __shared__ unsigned sums[kWaves];
-  const int u0 = blockIdx.x * a.group, u1 = min(u0 + a.group, a.units);
+  const int u0 = blockIdx.x * a.group, u1 = u0 + min(a.group, a.units - u0);
   int i = owner_of(a.whole ? a.row_offsets : a.batch.token_offsets, a.batch.n, u0, sums);
   const int bt = 1 << a.kv.block_shift;
   for (int u = u0; i < a.batch.n && u < u1; ++i) {
@@ -1124,6 +1124,7 @@ extern "C" int cascade_kv_bounds(const cascade_kv_pool_t *pool, int32_t layer, c
   a.slots = table->slots;
   a.whole = whole;
   a.group = a.units <= 2048 ? 1 : whole ? 4 : 16;
+  while ((a.units - 1) / a.group >= INT32_MAX / kBlock - 1) a.group *= 2;  // a launch has below 2^32 threads
   a.status = status_dev;
   const int grid = (a.units - 1) / a.group + 2;  // the last one checks the batch
   auto kernel = format->head_dim == 64    ? bounds_kernel<64>
