@@ -415,6 +415,16 @@ def _check_device(device, *tensors) -> None:
             raise ValueError(f"a tensor lies on {t.device}, not {device}")
 
 
+def _launch(call, device, stream) -> None:
+    """The call on `stream`, or on the current one of the tensors' device."""
+    torch = _torch()
+    if device.type == "cuda" and device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            _raise(call(stream_handle(stream)))
+    else:
+        _raise(call(stream_handle(stream)))
+
+
 class DeviceKvPool:
     """A pool of the 8-bit cache over a byte tensor [layers, 2 (K, V), slots,
     bytes]; the last dimension holds at least a chunk and may be padded.
@@ -502,7 +512,7 @@ class DeviceKvAppend:
                                 self.c_rope, self.positions, kv.status.data_ptr())
 
     def run(self, stream=None) -> None:
-        _raise(self._call(stream_handle(stream)))
+        _launch(self._call, self.kv.pool.device, stream)
 
 
 class DeviceAttention:
@@ -543,7 +553,7 @@ class DeviceAttention:
                                 kv.status.data_ptr())
 
     def run(self, stream=None) -> None:
-        _raise(self._call(stream_handle(stream)))
+        _launch(self._call, self.kv.pool.device, stream)
 
 
 def _workspace(workspace, size: int, device):
@@ -556,16 +566,6 @@ def _workspace(workspace, size: int, device):
         raise ValueError("a workspace is a contiguous uint8 tensor")
     at = (workspace.data_ptr() + 255) & ~255
     return workspace, at, max(workspace.data_ptr() + workspace.numel() - at, 0)
-
-
-def _launch(call, device, stream) -> None:
-    """The call on `stream`, or on the current one of the tensors' device."""
-    torch = _torch()
-    if device.type == "cuda" and device.index != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            _raise(call(stream_handle(stream)))
-    else:
-        _raise(call(stream_handle(stream)))
 
 
 class DeviceSharedAttention:
@@ -725,7 +725,7 @@ class DeviceKvEvict:
                                 self.status.data_ptr())
 
     def run(self, stream=None) -> None:
-        _raise(self._call(stream_handle(stream)))
+        _launch(self._call, self.status.device, stream)
 
     def check(self) -> None:
         """Synchronise and raise if a call found bad device data."""
