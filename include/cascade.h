@@ -731,7 +731,8 @@ int cascade_kv_bounds(const cascade_kv_pool_t *pool, int32_t layer,
    more than `keep` blocks, sets *status_dev.  A NaN score, of a K scale that is not
    finite, is the largest.
    selected: device int32[n_tokens][kv_heads][keep], block indices within the request, ascending,
-   then -1; tokens of no request are left as they are.
+   then -1; tokens of no request are left as they are, and where token_offsets or row_offsets
+   fall the tokens of the requests from there on may be.
    workspace: cascade_kv_select_workspace_bytes(...) bytes, 256-byte aligned, of
    any content (4 bytes per table entry, KV head and new token of the longest
    run: it grows with n_entries and max_new), or with most_blocks

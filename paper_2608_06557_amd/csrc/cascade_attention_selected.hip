@@ -84,8 +84,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void selected
     return;
   }
   extern __shared__ __align__(16) char lds[];
-  __shared__ unsigned sums[kWaves];
-  __shared__ int ends[kWaves];
+  __shared__ int owners[kWaves], ends[kWaves];
   int *const slot_list = reinterpret_cast<int *>(lds);
   float *const ms = reinterpret_cast<float *>(lds + (4 * a.per + 15 & ~15)), *const os = ms + 2 * kWaves * 16;
   char *const qs = reinterpret_cast<char *>(os);
@@ -104,7 +103,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void selected
   // single tokens are their requests' numbers, and one request has them all: look there first
   KvRequest req = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, min(token, a.batch.n - 1));
   if (!req.ok || token < req.first || token - req.first >= req.count) {
-    const int id = __builtin_amdgcn_readfirstlane(owner_of(a.batch.token_offsets, a.batch.n, token, sums));
+    const int id = __builtin_amdgcn_readfirstlane(owner_of(a.batch.token_offsets, a.batch.n, token, owners));
     if (id >= a.batch.n) return;
     req = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, id);
     if (!req.ok || token < req.first || token - req.first >= req.count) return;
@@ -323,16 +322,13 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(kDim, kTiles)) void selected
 template <int kType, int kDim>
 __global__ __launch_bounds__(kBlock) void join_selected_kernel(Selected a) {
   constexpr int kLanes = kDim / 4, kParts = 64 / kLanes;
-  __shared__ unsigned sums[kWaves];
+  __shared__ int owners[kWaves];
   const int lane = lane_id();
   const int64_t row0 = (int64_t)blockIdx.x * kWaves, row = row0 + wave_id();
   const int token = (int)(row / a.q_heads), head = (int)(row % a.q_heads);
   // rows of no request stay as they are
-  unsigned ended[1] = {0};
-  const int first = (int)(row0 / a.q_heads);
-  for (int i = threadIdx.x; i < a.batch.n; i += kBlock) ended[0] += a.batch.token_offsets[i + 1] <= first;
-  block_sum<1, unsigned>(ended, sums);
-  int id = __builtin_amdgcn_readfirstlane((int)ended[0]);
+  int id = __builtin_amdgcn_readfirstlane(
+      owner_of(a.batch.token_offsets, a.batch.n, (int)(row0 / a.q_heads), owners));
   const int mine = __builtin_amdgcn_readfirstlane(token);
   while (id < a.batch.n && a.batch.token_offsets[id + 1] <= mine) ++id;
   if (id >= a.batch.n || mine >= a.batch.n_tokens) return;

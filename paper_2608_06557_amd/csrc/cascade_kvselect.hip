@@ -157,9 +157,9 @@ __global__ __launch_bounds__(kBlock) void bounds_kernel(Bounds a) {
     if (blockIdx.y == 0) check_requests(a.batch, a.row_offsets, a.kv.block_shift, a.status);
     return;
   }
-  __shared__ unsigned sums[kWaves];
+  __shared__ int owners[kWaves];
   const int u0 = blockIdx.x * a.group, u1 = u0 + min(a.group, a.units - u0);
-  int i = owner_of(a.whole ? a.row_offsets : a.batch.token_offsets, a.batch.n, u0, sums);
+  int i = owner_of(a.whole ? a.row_offsets : a.batch.token_offsets, a.batch.n, u0, owners);
   const int bt = 1 << a.kv.block_shift;
   for (int u = u0; i < a.batch.n && u < u1; ++i) {
     const KvRequest r = kv_request(a.batch, a.row_offsets, a.kv.block_shift, i);
@@ -206,6 +206,8 @@ struct Select {
   int first, run;   // the new tokens of each request that are scored and selected, and how many at most
   int most, pitch;  // by tokens: blocks of a request, and those in whole lines of 16; else any and 0
   float *scores;  // [token][KV head][pitch], or request by request [token of the run][KV head][block], in lines of 16
+  int *limit;       // the first request behind which offsets fall: from there on none is scored
+  int scored;       // whether any is
   int32_t *selected;
   int32_t *status;
 };
@@ -636,13 +638,21 @@ struct Candidates {
 __device__ __forceinline__ int piece() { return (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3); }
 
 // Entries span .. of the table, the requests in them one after another, with the
-// tokens of the run as their new ones.
+// tokens of the run as their new ones.  Requests up to where offsets fall: their entries and
+// scores are in order and apart, whatever comes behind them.
 template <typename F>
-__device__ __forceinline__ void each_request(const Select &a, int span, int first_token, unsigned *lds, F f) {
+__device__ __forceinline__ void each_request(const Select &a, int span, int first_token, int *lds, F f) {
   if ((int64_t)span * a.span >= a.batch.n_entries) return;
   const int e0 = span * a.span, e1 = e0 + min(a.span, a.batch.n_entries - e0);
-  for (int i = __builtin_amdgcn_readfirstlane(owner_of(a.row_offsets, a.batch.n, e0, lds));
-       i < a.batch.n && uniform_load(a.row_offsets + i) < e1; ++i) {
+  int first[2];  // that ends behind e0, and whose end is before its begin
+  first_of(a.batch.n, first, lds, [&](int i, bool (&found)[2]) {
+    const int end = a.row_offsets[i + 1];
+    found[0] = end > e0;
+    found[1] = (end < a.row_offsets[i]) | (a.batch.token_offsets[i + 1] < a.batch.token_offsets[i]);
+  });
+  const int limit = __builtin_amdgcn_readfirstlane(first[1]);
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.limit = limit;
+  for (int i = __builtin_amdgcn_readfirstlane(first[0]); i < limit && uniform_load(a.row_offsets + i) < e1; ++i) {
     KvRequest r = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, i);
     r.first += a.first;
     r.count = min(r.count - a.first, a.run);
@@ -658,9 +668,9 @@ __device__ __forceinline__ void each_request(const Select &a, int span, int firs
 // are few heads, so that what lies side by side is read at one time.
 template <int kType, int kDim, bool kWide>
 __global__ __launch_bounds__(kBlock, kDim == 256 ? 2 : 5) void score_kernel(Select a) {
-  __shared__ unsigned sums[kWaves];
+  __shared__ int owners[2 * kWaves];
   const int wave = __builtin_amdgcn_readfirstlane(wave_id()), tile = blockIdx.y;
-  each_request(a, piece(), tile * (16 >> a.shift), sums, [&](const KvRequest &r, int i, int begin, int end) {
+  each_request(a, piece(), tile * (16 >> a.shift), owners, [&](const KvRequest &r, int i, int begin, int end) {
     const int heads = a.kv.kv_heads, parts = heads >= kWaves ? 1 : kWaves / heads;
     const int each = ((end - begin + 16 * parts - 1) / (16 * parts)) * 16;
     for (int u = wave; u < heads * parts; u += kWaves) {
@@ -674,12 +684,12 @@ __global__ __launch_bounds__(kBlock, kDim == 256 ? 2 : 5) void score_kernel(Sele
 // bounds are then in its L2.
 template <int kType, int kDim, int kTiles>
 __global__ __launch_bounds__(kBlock, 2) void score_sets_kernel(Select a) {
-  __shared__ unsigned sums[kWaves];
+  __shared__ int owners[2 * kWaves];
   __shared__ alignas(16) char stages[2 * BoundStage<kDim>::kBytes];
   const int wave = __builtin_amdgcn_readfirstlane(wave_id());
   const int at = piece(), head = at / (a.spans * a.sets), tile0 = at / a.spans % a.sets * kWaves * kTiles;
   if (head >= a.kv.kv_heads) return;
-  each_request(a, at % a.spans, tile0 * (16 >> a.shift), sums, [&](const KvRequest &r, int i, int begin, int end) {
+  each_request(a, at % a.spans, tile0 * (16 >> a.shift), owners, [&](const KvRequest &r, int i, int begin, int end) {
     score_sets<kType, kDim, kTiles>(a, r, i, head, tile0 + wave * kTiles, begin, end, stages);
   });
 }
@@ -780,9 +790,17 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// Whether a token is a new one of request `q` and of the run; reports a request of too many blocks.
+// The first request that is not taken.
+__device__ __forceinline__ int limit_of(const Select &a) {
+  const int limit = uniform_load(a.limit);
+  return a.scored ? limit : a.batch.n;
+}
+// Whether a token is a new one of request i.
+__device__ __forceinline__ bool has(const KvRequest &q, int i, int limit, int token) {
+  return q.ok && i < limit && token >= q.first && token - q.first < q.count;
+}
+// Whether it is one of the run; reports a request of too many blocks.
 __device__ __forceinline__ bool in_run(const Select &a, const KvRequest &q, int token) {
-  if (!q.ok || token < q.first || token - q.first >= q.count) return false;
   if (blocks_of(q, a.kv.block_shift) > a.most) {
     kv_report(a.status);
     return false;
@@ -834,15 +852,16 @@ __global__ __launch_bounds__(kBlock) void select_wave_kernel(Select a) {
     return;
   }
   __shared__ alignas(16) Hist hists[kWaves];
-  __shared__ unsigned sums[kWaves];
+  __shared__ int owners[kWaves];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
+  const int limit = limit_of(a);
   const int64_t row = (int64_t)blockIdx.x * kWaves + wave;
   const int token = (int)(row / a.kv.kv_heads), head = (int)(row % a.kv.kv_heads);
-  int i = owner_of(a.batch.token_offsets, a.batch.n, (int)((int64_t)blockIdx.x * kWaves / a.kv.kv_heads), sums);
+  int i = owner_of(a.batch.token_offsets, a.batch.n, (int)((int64_t)blockIdx.x * kWaves / a.kv.kv_heads), owners);
   while (i < a.batch.n && a.batch.token_offsets[i + 1] <= token) ++i;
   if (i >= a.batch.n || token >= a.batch.n_tokens) return;
   const KvRequest q = kv_request(a.batch, a.row_offsets, a.kv.block_shift, i);
-  if (!in_run(a, q, token)) return;
+  if (!has(q, i, limit, token) || !in_run(a, q, token)) return;
   const Row r = row_of(a, q, i, token, head, lane, 64);
   if (r.want == 0) return;
   const int m = __builtin_amdgcn_readfirstlane(r.end - r.begin);
@@ -931,7 +950,8 @@ __global__ __launch_bounds__(kBlock) void select_block_kernel(Select a) {
     return;
   }
   __shared__ alignas(16) Hist hists[3];
-  __shared__ unsigned sums[kWaves], marks[2][kWaves], listed;
+  __shared__ int owners[kWaves];
+  __shared__ unsigned marks[2][kWaves], listed;
   __shared__ float widths[2][kWaves];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
   const int token = blockIdx.x / a.kv.kv_heads, head = blockIdx.x % a.kv.kv_heads;
@@ -942,12 +962,14 @@ __global__ __launch_bounds__(kBlock) void select_block_kernel(Select a) {
   for (Hist &h : hists) clear(h);
   if (threadIdx.x == 0) listed = 0;
   // single tokens are their requests' numbers, and one request has them all: look there first
+  const int limit = limit_of(a);
   int i = min(token, a.batch.n - 1);
   KvRequest q = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, i);
-  if (!q.ok || token < q.first || token - q.first >= q.count) {
-    i = __builtin_amdgcn_readfirstlane(owner_of(a.batch.token_offsets, a.batch.n, token, sums));
+  if (!has(q, i, limit, token)) {
+    i = __builtin_amdgcn_readfirstlane(owner_of(a.batch.token_offsets, a.batch.n, token, owners));
     if (i >= a.batch.n) return;
     q = kv_request<true>(a.batch, a.row_offsets, a.kv.block_shift, i);
+    if (!has(q, i, limit, token)) return;
   }
   if (!in_run(a, q, token)) return;
   const Row r = row_of(a, q, i, token, head, threadIdx.x, kBlock);
@@ -1076,7 +1098,7 @@ bool bounds_fit(const cascade_kv_pool_t *p, const cascade_kv_format_t *f) {
 size_t score_bytes(const cascade_kv_format_t *f, const cascade_kv_batch_t *b) {
   return sizeof(float) * ((size_t)b->n_entries + 16 * (size_t)b->n) * f->kv_heads;
 }
-constexpr size_t kRoom = 256;      // of a workspace beside them
+constexpr size_t kRoom = 256;      // of a workspace before them
 constexpr int kMostRun = 32768;    // new tokens of a request that are ever scored at one time: a grid's second dimension
 // The most new tokens of a request.
 int most_tokens(const cascade_kv_batch_t *b) { return std::min(b->max_new, b->n_tokens); }
@@ -1178,7 +1200,7 @@ extern "C" int cascade_kv_select(const cascade_kv_pool_t *pool, int32_t layer, c
   a.keep = args->keep;
   a.sink = args->sink;
   a.recent = args->recent;
-  a.scores = static_cast<float *>(workspace);
+  a.scores = reinterpret_cast<float *>(static_cast<char *>(workspace) + kRoom);
   a.selected = args->selected;
   a.status = status_dev;
   const auto s = static_cast<hipStream_t>(stream);
@@ -1186,6 +1208,8 @@ extern "C" int cascade_kv_select(const cascade_kv_pool_t *pool, int32_t layer, c
   // every token keeps all that it sees there are no scores.
   const bool scored = batch->n_entries > a.keep;
   const int tokens = most_tokens(batch);
+  a.limit = static_cast<int *>(workspace);
+  a.scored = scored;
   a.most = args->most_blocks ? args->most_blocks : INT32_MAX;
   a.pitch = known ? (int)lines : 0;
   a.run = scored ? std::min(tokens, kMostRun) : tokens;

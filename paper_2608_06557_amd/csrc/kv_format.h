@@ -116,13 +116,39 @@ __device__ __forceinline__ void kv_report(int32_t *status) {
   if (status) *status = CASCADE_EINVAL;
 }
 
-// The request that unit `at` of a list lies in, by the ends of the requests'
-// parts: how many end at or before it.  Called by all threads.
-__device__ __forceinline__ int owner_of(const int32_t *offsets, int n, int at, unsigned *lds) {
-  unsigned ended[1] = {0};
-  for (int i = threadIdx.x; i < n; i += kBlock) ended[0] += offsets[i + 1] <= at;
-  block_sum<1, unsigned>(ended, lds);
-  return (int)ended[0];
+// The first of 0 .. n that f finds, n if none, for each of kWhat answers: f(i, answers).
+// Called by all threads; lds: kWhat * kWaves, not used again.
+template <int kWhat, typename F>
+__device__ __forceinline__ void first_of(int n, int (&first)[kWhat], int *lds, F f) {
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
+#pragma unroll
+  for (int k = 0; k < kWhat; ++k) first[k] = n;
+  for (int base = 64 * wave; base < n; base += kBlock) {
+    bool found[kWhat];
+    f(min(base + lane, n - 1), found);
+#pragma unroll
+    for (int k = 0; k < kWhat; ++k) {
+      const uint64_t in = __ballot(found[k]);
+      if (in) first[k] = min(first[k], base + __ffsll((unsigned long long)in) - 1);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kWhat; ++k)
+    if (lane == 0) lds[k * kWaves + wave] = first[k];
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kWhat; ++k)
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) first[k] = min(first[k], lds[k * kWaves + w]);
+}
+
+// The request that unit `at` of a list lies in, by the ends of the requests' parts: the
+// first that ends behind it (and not how many end before, which an offset that falls
+// somewhere would change for all).  As first_of.
+__device__ __forceinline__ int owner_of(const int32_t *offsets, int n, int at, int *lds) {
+  int first[1];
+  first_of(n, first, lds, [&](int i, bool (&found)[1]) { found[0] = offsets[i + 1] > at; });
+  return first[0];
 }
 
 // Reports requests outside the domain, whether they have new tokens or not.
