@@ -666,9 +666,11 @@ int cascade_attention(const cascade_kv_pool_t *pool, int32_t layer,
                       void *workspace, size_t workspace_bytes, int32_t *status_dev,
                       void *stream);
 
-/* cascade_attention of a batch whose requests share their first tokens (the
-   step's SHARE action, parallel samples, a common system prompt), which are
-   read once for a whole group.  The requests of a group are neighbours in the
+/* cascade_attention of a batch whose requests share their first tokens (parallel
+   samples, a common system prompt, requests that the step lets SHARE one's blocks),
+   which are read once for a whole group.  The caller says what is shared: requests that
+   reference one's blocks need not be neighbours in a step's batch, nor reference equally
+   many; here the requests of a group are neighbours in the
    batch: leader[i] is the first of request i's (i itself where it shares with
    none), and the first shared_len[leader[i]] cached tokens of each (a multiple of
    block_tokens; 0 for none; entries of other requests are not read) lie in the
@@ -678,7 +680,8 @@ int cascade_attention(const cascade_kv_pool_t *pool, int32_t layer,
    Results are those of cascade_attention up to the order of sums.  args as there, without block_weight
    (blocks that requests share are not evicted for one of them).
    workspace: cascade_attention_shared_workspace_bytes(...) bytes, 256-byte
-   aligned, of any content; it grows with n_tokens.
+   aligned, of any content; it grows with n_tokens, by 8 (head_dim + 2) q_heads bytes each
+   (two 32-bit states of each row) and more.
    Errors as cascade_attention; leaders, lengths or slots that are not as above, or
    a group of more than max_tokens new tokens, set *status_dev = CASCADE_EINVAL.  Rows of
    a request outside the domain, or with a leader or length that is not as above, are left

@@ -47,7 +47,7 @@ __device__ __forceinline__ bool taken(const Attention &a, int token) {
 
 // Joins what is known of each row, a row to a wave: the parts of its request's
 // segment, or its state, and the same of its group's.  A chain of dependent loads,
-// then the parts: 128 tokens of 64 heads of 128 dims 9 us behind 32 groups of 4 tokens, 11 where
+// then the parts: 128 tokens of 64 heads of 128 dims 9 us behind 32 groups of 4 tokens, 12 where
 // the row tiles of one group left 8 parts of each row, 33 MB.
 template <int kType, int kDim>
 __global__ __launch_bounds__(kBlock) void join_shared_kernel(Attention a, SharedJoin j) {
@@ -129,9 +129,10 @@ void attend_shared(const SharedCall &c) {
   const int64_t most = (int64_t)std::max(a.max_tokens, a.batch.max_new) * a.group;  // rows of a request or group
   const bool tiled = most > most_rows(kDim);
   // Where groups need row tiles and no request has over 16 rows, those of up to 32
-  // are groups: the requests' form is theirs alone (128 single tokens of 611 tokens each
-  // beside a group of 1024 rows 49 us, in the 32-row form 53; 100 batches of 1 to 128
-  // requests 1 % less on average, 4 % more at most).
+  // are groups: the requests' form is theirs alone.  128 single tokens of 611 tokens each
+  // beside a group of 1024 rows 49 us, in the 32-row form 53.  Groups of 17 to 32 rows are row tiles
+  // then, which costs more where there are many: one group of 128 tokens beside 31 of four, behind 8 and
+  // 4 Ki tokens, 64/8 heads, 262 us, in the 32-row form 209; the 31 beside one of nine 145 and 136.
   const int64_t rest = (int64_t)a.batch.max_new * a.group;
   const int small = tiled && rest <= 16 ? 16 : few_rows(most, kDim);
   SharedJoin j = {};
@@ -144,8 +145,10 @@ void attend_shared(const SharedCall &c) {
     attend_tiles<Form::kShared, kType, kDim, kStage>(a, c.workspace, c.places, c.cap, small, c.stream);
     j.of[1] = PartSet{a.parts, a.part_sums, kTileGroups * stage_tokens(kDim) / kStage, tile_rows(kStage)};
   };
-  // Tiles of half the rows, unless a group fills four whole ones: 12 groups of 81
-  // rows on average 102 us, in whole ones 166; a group of 1024 rows 60, in whole ones 52.
+  // Tiles of half the rows, unless a group fills four whole ones: 12 groups of 104
+  // rows on average 102 us, in whole ones 166; a group of 1024 rows 60, in whole ones 52.  Between them
+  // they are alike or whole ones faster: calls of four groups of 256, 384, 512, 768 and 1016 rows behind
+  // 8 Ki tokens 114, 160, 194, 280 and 361 us, in whole ones 111, 161, 184, 265 and 338.
   if (tiled && most < 1024)
     tiles(std::integral_constant<int, 32>());
   else if (tiled)

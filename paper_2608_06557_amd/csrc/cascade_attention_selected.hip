@@ -13,9 +13,9 @@
 //
 // 128 single tokens with lists of 128 blocks of 16 tokens, 64/8 heads of 128 dims, are bound by
 // HBM: 104-106 us, 601 MB fetched (543 without what lines bring along), 5.7 TB/s.  512 tokens of
-// one request, 64 blocks each, find codes in L2: 60 us for 1.07 GB, of which 5.5 us
-// for each of its rounds of workgroups go to slots, first loads and the join of waves.
-// One token: 6.7 us, join 4.3.
+// one request, 64 blocks each, find codes in L2: 60 us for 1.07 GB in close succession (66 to 70 after a
+// pause, before the clock has risen), of which 5.5 us for each of its rounds of workgroups go to
+// slots, first loads and the join of waves.  One token: 6.6 us, join 4.2.
 #include "attention_tiles.h"
 
 namespace cascade {
@@ -363,7 +363,10 @@ __global__ __launch_bounds__(kBlock) void join_selected_kernel(Selected a) {
 
 // ------------------------------------------------------------------- host
 
-// How a list is divided: into as many parts as fill the GPU, of 256 tokens at least.
+// How a list is divided: into as many parts as fill the GPU, of 256 tokens at least.  That pays
+// from 2 Ki listed tokens on: one token of 32/8 heads of 128 dims over 512, 1 Ki and 2 Ki 11.3, 11.2 and
+// 11.2 us, in parts of 1 Ki at least 7.7, 9.8 and 14.0; 8 tokens 11.5, 13.1 and 16.6 against 8.2, 12.1
+// and 16.8; 32 tokens 15.7, 21.2 and 31.8 against 11.1, 16.1 and 31.6.
 struct Parts {
   int tiles, row_tiles, splits, per;
   size_t parts, sums, total;

@@ -10,11 +10,16 @@
 // joins each row's two.
 //
 // Groups of few rows are bound by HBM: 32 groups of 4 tokens behind 1 to 32 Ki tokens, 64/8
-// heads of 128 dims, 172 us, 851 MB fetched (776 needed), 4.9 TB/s, two waves a SIMD with
+// heads of 128 dims, 173 us, 851 MB fetched (776 needed), 4.9 TB/s, two waves a SIMD with
 // 32 rows and 65 % of their cycles in waits (codes two steps ahead do not fit the
-// registers: 204).  Large groups' row tiles: 1024 rows behind 8 Ki tokens 52 us, the matrix units busy
+// registers: 204).  Large groups' row tiles: 1024 rows behind 8 Ki tokens 49 us, the matrix units busy
 // 25 % of the cycles, in 16 stages a workgroup, its list and its parts.  One launch each for
 // groups and requests, with a join each, took 2 to 30 % longer in all than one list.
+//
+// Against cascade_attention over the same tables: 17.4 us and 19.5 for 4 tokens behind 4 Ki, 181 and 374 for
+// those 32 groups, 110 and 278 for 128 tokens behind 8 Ki.  What is shared twice or more pays from
+// about 2 Ki tokens on (128 tokens in groups of 2, 4, 16: of 1 Ki 87, 75 and 86 us against 86, 71 and 64; of
+// 2 Ki 114, 88 and 91 against 125, 105 and 82; of 4 Ki 168, 116 and 102 against 210, 179 and 140).
 #include "attention_shared.h"
 
 namespace cascade {

@@ -13,22 +13,22 @@
 // order of sums.
 //
 // bounds: one wave reads a block and head's codes in operand order, 16 dims of
-// a token in a lane, and halves the dims it answers for at each exchange.  4.4 us
-// for 128 single tokens and 8.1 us for 512 blocks of 8 heads x 128 dims, inputs in
+// a token in a lane, and halves the dims it answers for at each exchange.  4.5 us
+// for 128 single tokens and 8.5 us for 512 blocks of 8 heads x 128 dims, inputs in
 // HBM: the launch and three dependent loads (offsets, slot, codes).
 // score: a wave holds the queries of 16 rows (tokens and heads of a group) as the
 // first operand and takes 16 blocks at a time as the second, so a lane has one
 // block's scores of 4 rows, and the largest over a group's heads is taken in
 // registers.  Nothing but a block's bounds, 2 head_dim bytes a head,
 // and its scale is read, so 128 single tokens over 84 thousand blocks are bound
-// by HBM: 49 us, 210 MB fetched (the bounds are 173; the 1 KB of a block begin inside a
+// by HBM: 48 us, 209 MB fetched (the bounds are 173; the 1 KB of a block begin inside a
 // line), 4.3 TB/s.  With many rows of one request the bounds come from LDS for four
 // waves' row sets: 128 sets of each of 8 KV heads over 2001 blocks 23 us, by the vector
 // instructions of scaling and of the heads' largest, and by their latency.
 // select: a row's candidates stay in registers, of a workgroup or of one wave; a
 // histogram of their range in LDS leaves few in the part where the least score that
 // stays is (else a radix selection over the scores' bits finds it), and ballots write
-// the blocks in order.  1024 rows of 660 blocks 8.6 us, 4096 rows of 2000 17 us (a wave
+// the blocks in order.  1024 rows of 660 blocks 9.0 us, 4096 rows of 2000 17 us (a wave
 // to a row), of 4000 35 us (a workgroup).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -1221,7 +1221,8 @@ extern "C" int cascade_kv_select(const cascade_kv_pool_t *pool, int32_t layer, c
   // One round of workgroups where there are many sets: each begins with 5 us of loads and of rounding its
   // queries, and 32 blocks more take 2 us (512 tokens, 64 heads: of 4000 blocks 61 us, with at most 256
   // entries to a workgroup 81; of 2001 blocks 39 and 45).  Small where there is little to share:
-  // one request's next token takes 6.6 us by 32 and 8.6 by 64, 128 requests' 48 and 50.
+  // one request's next token takes 6.6 us by 32 and 8.6 by 64, 128 requests' 48 and 50.  One form for
+  // the whole batch, by its longest run: 128 single tokens 47 us, a chunk of 512 57, both in one call 208.
   const int64_t share = (int64_t)batch->n_entries * format->kv_heads * sets / 512;
   a.span = many ? (int)std::min<int64_t>(std::max<int64_t>((share + 31) / 32 * 32, 32), 1024) : 32;
   a.spans = (batch->n_entries - 1) / a.span + 1;
