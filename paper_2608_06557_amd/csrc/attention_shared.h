@@ -41,7 +41,10 @@ __device__ __forceinline__ bool taken(const Attention &a, int token) {
   const uint64_t in = __ballot(leader >= 0);
   if (!in) return false;
   leader = __builtin_amdgcn_readlane(leader, __ffsll((unsigned long long)in) - 1);
-  for (int i = lane; i < a.batch.n; i += 64) found |= a.taken[i] == kGroup && a.leader[i] == leader;
+  // the group's rows end where its last request's do
+  const bool behind = token >= a.batch.token_offsets[leader];
+  for (int i = lane; i < a.batch.n; i += 64)
+    found |= behind && a.taken[i] == kGroup && a.leader[i] == leader && token < a.batch.token_offsets[i + 1];
   return __any(found);
 }
 

@@ -127,3 +127,27 @@ def test_groups_that_are_no_neighbours_leave_others_alone(dev, case):
     part = {k: v[good] for k, v in e.items() if k != "weight"}
     check_attention((out[good], lse[good], None), part, "bf16", d, 0)
     assert (out[left] == 7).all() and (lse[left] == 7).all()
+
+
+def test_a_group_whose_offsets_fall_inside(dev):
+    """Its rows end before the first request's do: what they miss is left, by
+    whatever workspace (rows that two requests have are either's)."""
+    rng = np.random.default_rng(14)
+    H, h, d, bt = 4, 2, 64, 16
+    b = shared_batch(rng, [(64, [(5, 20), (1, 30), (2, 40)]), (0, [(4, 30)])], bt)
+    pool = ref.random_pool(rng, 1, b["pool"], h, d, bt)
+    q, other = (rows(rng, b["tokens"], H, d, torch.bfloat16) for _ in range(2))
+    e = ref.attend(pool[0], q, b, h, d, bt, 0.2)
+    pool = pool.cuda()
+    before = attend_over(dev, pool, other.cuda(), b, h, d, bt, b["most_shared"])[2].workspace.clone()
+    b["off"] = torch.tensor([0, 5, 2, 4, 12], dtype=torch.int32)  # the second is refused, the third has rows 2 and 3
+    b["len"][3] = 1 << 20  # and the last, which would have row 4
+    for fill in (lambda w: w.copy_(before), lambda w: w.fill_(0xff), lambda w: w.fill_(2)):
+        w = before.clone()
+        fill(w)
+        out, lse, op = attend_over(dev, pool, q.cuda(), b, h, d, bt, b["most_shared"], w)
+        with pytest.raises(RuntimeError):
+            op.kv.check()
+        part = {k: v[:2] for k, v in e.items() if k != "weight"}
+        check_attention((out[:2], lse[:2], None), part, "bf16", d, 0)
+        assert (out[4:] == 7).all() and (lse[4:] == 7).all()
