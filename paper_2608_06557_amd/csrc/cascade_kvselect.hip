@@ -411,9 +411,9 @@ struct RowSet {
   }
   // The scores of 16 blocks from `b` on by the sums of their products with `kTiles` sets; `in`:
   // the lane's is one.  `next` lies between two tokens' scores.  `add`, `more`: of a token's heads
-  // these are not the first, not the last; scaled is the largest of all, as a scale that is not
-  // finite makes the largest score of another part.  (Step by step for all sets, each of which has a step's latency to itself
-  // otherwise.)
+  // these are not the first, not the last.  The largest of all heads is scaled, not each part's: by a
+  // scale that is not finite the larger of two scaled ones would be another.  (Step by step for all
+  // sets, each of which has a step's latency to itself otherwise.)
   template <int kTiles>
   static __device__ __forceinline__ void score(const Select &a, const RowSet (&set)[kTiles], const i4 (&sum)[kTiles],
                                                float scale, int b, bool in, int64_t next, bool add, bool more) {
@@ -1099,7 +1099,7 @@ size_t score_bytes(const cascade_kv_format_t *f, const cascade_kv_batch_t *b) {
   return sizeof(float) * ((size_t)b->n_entries + 16 * (size_t)b->n) * f->kv_heads;
 }
 constexpr size_t kRoom = 256;      // of a workspace before them
-constexpr int kMostRun = 32768;    // new tokens of a request that are ever scored at one time: a grid's second dimension
+constexpr int kMostRun = 32768;    // new tokens of a request that are scored at one time: a grid's second dimension
 // The most new tokens of a request.
 int most_tokens(const cascade_kv_batch_t *b) { return std::min(b->max_new, b->n_tokens); }
 
@@ -1174,7 +1174,8 @@ extern "C" int cascade_kv_select(const cascade_kv_pool_t *pool, int32_t layer, c
     return CASCADE_EINVAL;
   if ((args->dtype != CASCADE_BF16 && args->dtype != CASCADE_F16) || args->q_heads < 1 ||
       args->q_heads % format->kv_heads || args->q_heads / format->kv_heads > 128 || args->sink < 0 ||
-      args->most_blocks < 0 || args->recent < 1 || args->keep > 65536 || (int64_t)args->sink + args->recent > args->keep)
+      args->recent < 1 || args->most_blocks < 0 || args->keep > 65536 ||
+      (int64_t)args->sink + args->recent > args->keep)
     return CASCADE_EINVAL;
   if (!workspace || ((uintptr_t)workspace & 255)) return CASCADE_EINVAL;
   const int64_t rows = (int64_t)batch->n_tokens * format->kv_heads;

@@ -140,7 +140,8 @@ def test_scores_over_4_gib(dev):
     kv = dev.DeviceKvPool(pool.cuda(), h, d, bt, bounds=True)
     slack, first = 1 << 25, int(b["rows"][1])
     g = on_gpu(b)
-    g["slots"] = torch.cat([g["slots"][:first], torch.zeros(slack, dtype=torch.int32, device="cuda"), g["slots"][first:]])
+    gap = torch.zeros(slack, dtype=torch.int32, device="cuda")
+    g["slots"] = torch.cat([g["slots"][:first], gap, g["slots"][first:]])
     g["rows"] = torch.cat([g["rows"][:1], g["rows"][1:] + slack])
     got, op = select_in(dev, kv, q.cuda(), g, keep, 1, 1, 4 * one_token(g, h) + 256)
     assert op.ws_bytes > 1 << 32
